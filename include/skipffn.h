@@ -278,6 +278,62 @@ int skipffn_token_merge(const void* x, const int32_t* seg_host, int64_t S, int64
 int skipffn_token_merge_backward(const void* grad_out, const int32_t* seg_host, int64_t S, int64_t C,
                                  int64_t k, const int32_t* assign, void* grad_x, void* stream);
 
+/* ---- attention over whole prompts (the first half of the decoder layer) -----------------
+ * The block's input h_attn comes from attention, which every token takes part in, skipped ones
+ * too (Section 4.2).  For every sequence of a packed batch and every query head
+ *     out_i = sum_j P_ij v_j,   P_ij = softmax over j of (scale * q_i . k_j)
+ * over the keys j that query i sees: all nk of its sequence, or with causal != 0 those with
+ * j <= i + (nk - nq), i.e. the nq queries are the last of nk tokens (nk > nq: new tokens after a
+ * cached beginning; nk < nq: the first nq - nk queries see nothing).  A query that sees no key
+ * gives a zero row and zero gradients.  Query head h reads key/value head h / (Hq / Hkv).
+ *   skipffn_heads  a bf16 tensor by token, head and column, element (t, h, d) at
+ *                  data[t * token_stride + h * head_stride + d]: [T, H, D], a column range of the
+ *                  projections' output [T, (Hq + 2 Hkv) D], or a cache [H, capacity, D].  Strides are
+ *                  in elements, multiples of 8, not negative (0 repeats an input's rows or heads);
+ *                  token_stride < 2^22.  data is 16-byte aligned.  The struct is read on the host
+ *                  during the call.
+ *   q [Tq, Hq, D], k and v [Tk, Hkv, D], out [Tq, Hq, D] OUT (memory of its own: what it spans meets none
+ *                  of q, k, v; heads and rows of it are apart)
+ *   seg_q, seg_k   i32 [n_seq + 1] device: sequence s has the queries seg_q[s] .. seg_q[s+1]) and the
+ *                  keys seg_k[s] .. seg_k[s+1]); seg_k = NULL: the same as seg_q.  Lengths need not be
+ *                  known on the host, may be 0; bounds are clamped to [0, Tq], [0, Tk].  Rows of out
+ *                  that belong to no sequence are left as they were.
+ *   scale          > 0, finite (1 / sqrt(D))
+ *   saved          NULL (inference) or skipffn_attn_saved_bytes(Tq, Hq) bytes OUT (log-sum-exp, f32)
+ *   workspace      at least skipffn_attn_forward_workspace_bytes(...) bytes (NULL where that is 0)
+ * D % 8 == 0, 8 <= D <= 128, Hq a multiple of Hkv, n_seq <= 65535.  Scores, softmax sums and products are
+ * accumulated in fp32; the weights P are rounded to bf16 before they meet v (the matrix cores' operand
+ * type).  Deterministic: every sum has a fixed order. */
+typedef struct skipffn_heads {
+    void* data;
+    int64_t token_stride, head_stride;
+} skipffn_heads;
+size_t skipffn_attn_saved_bytes(int64_t Tq, int64_t Hq);
+size_t skipffn_attn_forward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D);
+int skipffn_attn_forward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D,
+                         const skipffn_heads* q, const skipffn_heads* k, const skipffn_heads* v,
+                         const skipffn_heads* out, const int32_t* seg_q, const int32_t* seg_k,
+                         int causal, float scale, void* saved,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of the above for L with dL/dout = grad_out [Tq, Hq, D]: with dP_ij = grad_out_i . v_j and
+ * dS_ij = P_ij (dP_ij - grad_out_i . out_i),
+ *     grad_q_i = scale sum_j dS_ij k_j,  grad_k_j = scale sum_i dS_ij q_i,  grad_v_j = sum_i P_ij grad_out_i,
+ * the last two summed over the query heads of a key/value head too (in fp32, rounded once).
+ *   out, saved     what the forward call wrote for the same inputs
+ *   grad_q [Tq, Hq, D], grad_k and grad_v [Tk, Hkv, D] OUT, overwritten; rows that belong to no sequence
+ *                  are left as they were.  They may be column ranges of one tensor; what they span
+ *                  meets none of the inputs.
+ *   workspace      at least skipffn_attn_backward_workspace_bytes(...)
+ * Deterministic. */
+size_t skipffn_attn_backward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D);
+int skipffn_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D,
+                          const skipffn_heads* q, const skipffn_heads* k, const skipffn_heads* v,
+                          const skipffn_heads* out, const skipffn_heads* grad_out,
+                          const int32_t* seg_q, const int32_t* seg_k, int causal, float scale,
+                          const void* saved, const skipffn_heads* grad_q, const skipffn_heads* grad_k,
+                          const skipffn_heads* grad_v, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- layout of `saved`, for tests that compare stage by stage -------------
  * Byte offsets of the sections inside a saved buffer for (R_max, C, I):
  * offsets[0] x rows bf16 [R, C]; [1] normalised rows bf16 [R, C];

@@ -610,3 +610,67 @@ def token_merge(x_bits, seg, k):
         avg[lo:hi] = r["avg"]
     return {"out_bits": f64_to_bf16_bits(out), "merged": out, "kept": kept, "assign": assign, "avg": avg}
 
+
+
+# ---- attention (the first half of the decoder layer; what the skip KV-cache is read by) ----------------
+def attn_weights(S, causal):
+    """Softmax by rows of scores S [nq, nk]; with causal, row i sees the keys j <= i + nk - nq.  A row that
+    sees no key has weights 0."""
+    nq, nk = S.shape
+    sees = np.ones((nq, nk), dtype=bool)
+    if causal:
+        sees = np.arange(nk)[None, :] <= np.arange(nq)[:, None] + (nk - nq)
+    P = np.zeros((nq, nk))
+    rows = np.flatnonzero(sees.any(axis=1))
+    if len(rows):
+        # a score that is not seen has no part in anything, whatever it is
+        T = np.where(sees[rows], np.where(sees, S, 0.0)[rows], -np.inf)
+        E = np.exp(T - T.max(axis=1, keepdims=True))
+        P[rows] = E / E.sum(axis=1, keepdims=True)
+    return P
+
+
+def attn_forward_real(q, k, v, causal, scale):
+    """One sequence: q [nq, Hq, D], k, v [nk, Hkv, D] float64 -> out [nq, Hq, D], weights [Hq, nq, nk]."""
+    nq, Hq, D = q.shape
+    nk, Hkv, _ = k.shape
+    out, P = np.zeros((nq, Hq, D)), np.zeros((Hq, nq, nk))
+    for h in range(Hq):
+        kh = h // (Hq // Hkv)
+        P[h] = attn_weights(scale * (q[:, h] @ k[:, kh].T), causal)
+        out[:, h] = P[h] @ v[:, kh]
+    return out, P
+
+
+def attn_backward_real(q, k, v, grad_out, causal, scale):
+    """Gradients of sum(out * grad_out) for one sequence; also dS [Hq, nq, nk], the gradient of the scaled scores."""
+    out, P = attn_forward_real(q, k, v, causal, scale)
+    Hq, Hkv = q.shape[1], k.shape[1]
+    dq, dk, dv, dS = np.zeros(q.shape), np.zeros(k.shape), np.zeros(v.shape), np.zeros(P.shape)
+    for h in range(Hq):
+        kh = h // (Hq // Hkv)
+        dP = grad_out[:, h] @ v[:, kh].T
+        dS[h] = P[h] * (dP - (P[h] * dP).sum(axis=1, keepdims=True))
+        dq[:, h] = scale * (dS[h] @ k[:, kh])
+        dk[:, kh] += scale * (dS[h].T @ q[:, h])
+        dv[:, kh] += P[h].T @ grad_out[:, h]
+    return {"out": out, "P": P, "dS": dS, "dq": dq, "dk": dk, "dv": dv}
+
+
+def attn_decode_real(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, scale):
+    """One query a sequence: q [n, Hq, D] over the rows prefix_seg[g] .. prefix_seg[g+1]) of its group's prefix
+    [Tp, Hkv, D] (group g has the sequences group_off[g] .. group_off[g+1])) and the first suffix_len of its own rows
+    [n, cap, Hkv, D] -> out [n, Hq, D], and per sequence the keys' rows (k, v) and weights [Hq, keys]."""
+    out, seen = np.zeros(q.shape), []
+    group = np.full(len(q), -1)
+    for g in range(len(group_off) - 1):
+        group[group_off[g]:group_off[g + 1]] = g
+    for i in range(len(q)):
+        own = slice(0, suffix_len[i])
+        pre = slice(prefix_seg[group[i]], prefix_seg[group[i] + 1]) if group[i] >= 0 else slice(0, 0)
+        k = np.concatenate([prefix_k[pre], suffix_k[i, own]])
+        v = np.concatenate([prefix_v[pre], suffix_v[i, own]])
+        o, P = attn_forward_real(q[i:i + 1], k, v, False, scale)
+        out[i] = o[0]
+        seen.append((k, v, P[:, 0]))
+    return out, seen

@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import (POINTER, c_char_p, c_double, c_float, c_int, c_int32, c_int64,
+from ctypes import (POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64,
                     c_size_t, c_uint32, c_void_p)
 
 import torch
@@ -25,6 +25,11 @@ FLAG_BALANCED_SPLIT = 0x8
 FLAG_VALIDATE_IDX = 0x10
 
 OK, EINVAL, ESHAPE, EWORKSPACE, EHIP, EUNSUPPORTED, EIDX = range(7)
+
+class Heads(Structure):
+    """skipffn_heads: where element (token, head, column) of a bf16 tensor lies."""
+    _fields_ = [("data", c_void_p), ("token_stride", c_int64), ("head_stride", c_int64)]
+
 
 # every symbol include/skipffn.h declares: (restype, argtypes)
 _SIGNATURES = {
@@ -62,6 +67,13 @@ _SIGNATURES = {
                                     c_void_p, c_void_p, c_void_p, c_size_t, c_void_p]),
     "skipffn_token_merge_backward": (c_int, [c_void_p, POINTER(c_int32), c_int64, c_int64, c_int64, c_void_p,
                                              c_void_p, c_void_p]),
+    "skipffn_attn_saved_bytes": (c_size_t, [c_int64, c_int64]),
+    "skipffn_attn_forward_workspace_bytes": (c_size_t, [c_int64] * 6),
+    "skipffn_attn_forward": (c_int, [c_int64] * 6 + [POINTER(Heads)] * 4 + [c_void_p, c_void_p, c_int, c_float, c_void_p, c_void_p,
+                                                                           c_size_t, c_void_p]),
+    "skipffn_attn_backward_workspace_bytes": (c_size_t, [c_int64] * 6),
+    "skipffn_attn_backward": (c_int, [c_int64] * 6 + [POINTER(Heads)] * 5 + [c_void_p, c_void_p, c_int, c_float, c_void_p] +
+                              [POINTER(Heads)] * 3 + [c_void_p, c_size_t, c_void_p]),
     "skipffn_probe_mfma": (c_int, [c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p]),
     "skipffn_saved_layout": (c_int, [c_int64, c_int64, c_int64, POINTER(c_size_t)]),
     "skipffn_status_string": (c_char_p, [c_int]),
@@ -288,6 +300,69 @@ def skipffn_token_merge_backward(grad_out, seg, assign, grad_x):
     _check(lib().skipffn_token_merge_backward(_ptr(grad_out), arr, len(seg) - 1, grad_out.shape[2],
                                               grad_out.shape[1], _ptr(assign), _ptr(grad_x), _stream()),
            "skipffn_token_merge_backward")
+
+
+def _heads(t, where):
+    """A tensor [tokens, heads, columns] whose columns lie together, as the library takes it."""
+    if t.dim() != 3 or t.dtype != torch.bfloat16 or (t.stride(2) != 1 and t.shape[2] > 1):
+        raise ValueError(f"{where}: a bfloat16 tensor [tokens, heads, columns] with contiguous columns is wanted")
+    return byref(Heads(t.data_ptr(), t.stride(0), t.stride(1)))
+
+
+def _same(where, *pairs):
+    for got, want in pairs:
+        if tuple(got) != tuple(want):
+            raise ValueError(f"{where}: a tensor of shape {tuple(want)} is wanted, got {tuple(got)}")
+
+
+def skipffn_attn_saved_bytes(Tq, Hq) -> int:
+    return lib().skipffn_attn_saved_bytes(Tq, Hq)
+
+
+def skipffn_attn_forward_workspace_bytes(Tq, Tk, n_seq, Hq, Hkv, D) -> int:
+    return lib().skipffn_attn_forward_workspace_bytes(Tq, Tk, n_seq, Hq, Hkv, D)
+
+
+def skipffn_attn_backward_workspace_bytes(Tq, Tk, n_seq, Hq, Hkv, D) -> int:
+    return lib().skipffn_attn_backward_workspace_bytes(Tq, Tk, n_seq, Hq, Hkv, D)
+
+
+def _attn_sizes(q, k, v, seg_q, seg_k, saved, where):
+    """(Tq, Tk, n_seq, Hq, Hkv, D); the library sees pointers, so what they hold is checked here."""
+    Tq, Hq, D = q.shape
+    Tk, Hkv = k.shape[:2]
+    _same(where, (k.shape, (Tk, Hkv, D)), (v.shape, (Tk, Hkv, D)))
+    for seg in (seg_q, seg_k):
+        if seg is not None and (seg.dtype != torch.int32 or not seg.is_contiguous() or seg.numel() != seg_q.numel() or seg.numel() < 1):
+            raise ValueError(f"{where}: seg_q and seg_k are contiguous int32 tensors of n_seq + 1 offsets")
+    if saved is not None and _nbytes(saved) < lib().skipffn_attn_saved_bytes(Tq, Hq):
+        raise ValueError(f"{where}: saved holds less than skipffn_attn_saved_bytes({Tq}, {Hq})")
+    return Tq, Tk, seg_q.numel() - 1, Hq, Hkv, D
+
+
+def skipffn_attn_forward(q, k, v, out, seg_q, seg_k=None, *, causal=True, scale=None, saved=None, workspace=None):
+    """q, out bf16 [Tq, Hq, D]; k, v bf16 [Tk, Hkv, D] (any token and head strides); seg_q, seg_k i32 [n_seq + 1].
+    scale: None is 1 / sqrt(D)."""
+    where = "skipffn_attn_forward"
+    sizes = _attn_sizes(q, k, v, seg_q, seg_k, saved, where)
+    _same(where, (out.shape, q.shape))
+    _check(lib().skipffn_attn_forward(*sizes, _heads(q, where), _heads(k, where), _heads(v, where), _heads(out, where), _ptr(seg_q),
+                                      _ptr(seg_k), int(bool(causal)), sizes[-1] ** -0.5 if scale is None else scale, _ptr(saved),
+                                      _ptr(workspace), _nbytes(workspace), _stream()), where)
+
+
+def skipffn_attn_backward(q, k, v, out, grad_out, seg_q, seg_k, saved, grad_q, grad_k, grad_v, *, causal=True, scale=None,
+                          workspace=None):
+    """out and saved from the forward call with the same q, k, v, seg_q, seg_k, causal and scale; grad_out and grad_q as q,
+    grad_k and grad_v as k."""
+    where = "skipffn_attn_backward"
+    sizes = _attn_sizes(q, k, v, seg_q, seg_k, saved, where)
+    _same(where, *((t.shape, q.shape) for t in (out, grad_out, grad_q)), *((t.shape, k.shape) for t in (grad_k, grad_v)))
+    _check(lib().skipffn_attn_backward(*sizes, _heads(q, where), _heads(k, where), _heads(v, where), _heads(out, where),
+                                       _heads(grad_out, where), _ptr(seg_q), _ptr(seg_k), int(bool(causal)),
+                                       sizes[-1] ** -0.5 if scale is None else scale, _ptr(saved), _heads(grad_q, where),
+                                       _heads(grad_k, where), _heads(grad_v, where), _ptr(workspace), _nbytes(workspace), _stream()),
+           where)
 
 
 def skipffn_probe_mfma(blocks, iters, random_operands, out, clocks):

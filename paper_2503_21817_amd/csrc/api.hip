@@ -4,6 +4,7 @@
 // in include/skipffn.h.
 #include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <mutex>
 #include <vector>
 
@@ -103,7 +104,8 @@ const char* kernel_class_name(int kc) {
         "compact", "gather_rmsnorm", "gemm_gate_up_swiglu", "gemm_down", "resid_scatter",
         "passthrough_copy", "gather_rows", "gemm_dh_swiglu_bwd+dw_down", "gemm_dw_gate_up",
         "gemm_dxn", "rmsnorm_bwd_scatter", "fill_zero", "kv_compact", "summary_fwd", "summary_bwd", "select_retained", "token_merge",
-        "gemm_dxn+dw_gate_up"};
+        "gemm_dxn+dw_gate_up",
+        "attn_fwd", "attn_bwd", "attn_decode"};
     return (kc >= 0 && kc < KC_COUNT) ? names[kc] : "?";
 }
 
@@ -814,6 +816,124 @@ int skipffn_token_merge_backward(const void* grad_out, const int32_t* seg_host, 
                                    assign, static_cast<bf16_t*>(grad_x), s);
     }
     profile_mark_end(KC_MERGE, s);
+    return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
+}
+
+// ---- attention ---------------------------------------------------------------------------------------
+namespace {
+int check_attn(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, float scale) {
+    if (Tq < 0 || Tk < 0 || n_seq < 0 || Hq <= 0 || Hkv <= 0 || D <= 0 || !(scale > 0.0f) || !std::isfinite(scale)) return SKIPFFN_EINVAL;
+    if (Hq % Hkv != 0 || (D & 7) || D > ATTN_MAX_D || n_seq > 65535 || Hq > 65535 || Tq >= (1 << 30) || Tk >= (1 << 30)) return SKIPFFN_ESHAPE;
+    // a grid of workgroups by queries, one by keys, as launch_attn_* form them
+    if ((Tq / 32 + 2 * n_seq) * Hq >= (1ll << 31) || (Tk / 32 + 2 * n_seq) * Hkv >= (1ll << 31)) return SKIPFFN_ESHAPE;
+    return SKIPFFN_OK;
+}
+// bytes from the first element to past the last one
+int64_t heads_span(const skipffn_heads* t, int64_t T, int64_t H, int64_t D) {
+    return T <= 0 || H <= 0 ? 0 : ((T - 1) * t->token_stride + (H - 1) * t->head_stride + D) * 2;
+}
+int check_heads(const skipffn_heads* t, int64_t T, int64_t H, int64_t D, bool written) {
+    if (t == nullptr) return SKIPFFN_EINVAL;
+    if (t->token_stride < 0 || t->head_stride < 0 || (T > 0 && bad_ptr(t->data))) return SKIPFFN_EINVAL;
+    if ((t->token_stride & 7) || (t->head_stride & 7) || t->token_stride >= (1 << 22) || t->head_stride >= ((int64_t)1 << 44)) return SKIPFFN_ESHAPE;
+    // rows and heads of a result are apart: tokens inside a head's range, or heads inside a token's
+    if (written && !((H == 1 || t->head_stride >= D) && (T <= 1 || t->token_stride >= (H - 1) * t->head_stride + D)) &&
+        !((T <= 1 || t->token_stride >= D) && (H == 1 || t->head_stride >= (T - 1) * t->token_stride + D)))
+        return SKIPFFN_EINVAL;
+    return SKIPFFN_OK;
+}
+bool heads_meet(const skipffn_heads* a, int64_t Ta, int64_t Ha, const skipffn_heads* b, int64_t Tb, int64_t Hb, int64_t D) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a->data), y = reinterpret_cast<uintptr_t>(b->data);
+    return x < y + (uintptr_t)heads_span(b, Tb, Hb, D) && y < x + (uintptr_t)heads_span(a, Ta, Ha, D);
+}
+bool bad_seg(const int32_t* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+const bf16_t* in(const skipffn_heads* t) { return static_cast<const bf16_t*>(t->data); }
+bf16_t* to(const skipffn_heads* t) { return static_cast<bf16_t*>(t->data); }
+AttnArgs attn_args(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, const skipffn_heads* q,
+                   const skipffn_heads* k, const skipffn_heads* v, const skipffn_heads* out, const int32_t* seg_q,
+                   const int32_t* seg_k, int causal, float scale, float* lse) {
+    AttnArgs a{};
+    a.Tq = (int)Tq; a.Tk = (int)Tk; a.n_seq = (int)n_seq; a.Hq = (int)Hq; a.Hkv = (int)Hkv; a.D = (int)D;
+    a.causal = causal != 0;
+    a.scale = scale; a.scale_log2 = scale * 1.4426950408889634f;
+    a.q = in(q); a.k = in(k); a.v = in(v); a.out = to(out);
+    a.q_tok = (int)q->token_stride; a.k_tok = (int)k->token_stride; a.v_tok = (int)v->token_stride; a.o_tok = (int)out->token_stride;
+    a.q_head = q->head_stride; a.k_head = k->head_stride; a.v_head = v->head_stride; a.o_head = out->head_stride;
+    a.seg_q = seg_q; a.seg_k = seg_k == nullptr ? seg_q : seg_k;
+    a.lse = lse;
+    return a;
+}
+}  // namespace
+
+size_t skipffn_attn_saved_bytes(int64_t Tq, int64_t Hq) {
+    if (Tq < 0 || Hq <= 0) return 0;
+    return align_up((size_t)Tq * Hq * 4) + 256;
+}
+size_t skipffn_attn_forward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D) {
+    return 0;
+}
+size_t skipffn_attn_backward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D) {
+    if (check_attn(Tq, Tk, n_seq, Hq, Hkv, D, 1.0f) != SKIPFFN_OK) return 0;
+    return align_up((size_t)Tq * Hq * 4) + 256;
+}
+
+int skipffn_attn_forward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D,
+                         const skipffn_heads* q, const skipffn_heads* k, const skipffn_heads* v, const skipffn_heads* out,
+                         const int32_t* seg_q, const int32_t* seg_k, int causal, float scale, void* saved,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+    int st = check_attn(Tq, Tk, n_seq, Hq, Hkv, D, scale);
+    if (st != SKIPFFN_OK) return st;
+    if ((st = check_heads(q, Tq, Hq, D, false)) || (st = check_heads(k, Tk, Hkv, D, false)) || (st = check_heads(v, Tk, Hkv, D, false)) ||
+        (st = check_heads(out, Tq, Hq, D, true)))
+        return st;
+    if (seg_k == nullptr && Tq != Tk) return SKIPFFN_EINVAL;
+    if (n_seq == 0 || Tq == 0) return SKIPFFN_OK;
+    if (bad_seg(seg_q) || (seg_k != nullptr && bad_seg(seg_k)) || (saved != nullptr && !aligned16(saved))) return SKIPFFN_EINVAL;
+    if (heads_meet(out, Tq, Hq, q, Tq, Hq, D) || heads_meet(out, Tq, Hq, k, Tk, Hkv, D) || heads_meet(out, Tq, Hq, v, Tk, Hkv, D))
+        return SKIPFFN_EINVAL;
+    hipStream_t s = (hipStream_t)stream;
+    const AttnArgs a = attn_args(Tq, Tk, n_seq, Hq, Hkv, D, q, k, v, out, seg_q, seg_k, causal, scale, static_cast<float*>(saved));
+    profile_mark_begin(KC_ATTN_FWD, s);
+    hipError_t e = launch_attn_forward(a, s);
+    profile_mark_end(KC_ATTN_FWD, s);
+    return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
+}
+
+int skipffn_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D,
+                          const skipffn_heads* q, const skipffn_heads* k, const skipffn_heads* v, const skipffn_heads* out,
+                          const skipffn_heads* grad_out, const int32_t* seg_q, const int32_t* seg_k, int causal, float scale,
+                          const void* saved, const skipffn_heads* grad_q, const skipffn_heads* grad_k, const skipffn_heads* grad_v,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+    int st = check_attn(Tq, Tk, n_seq, Hq, Hkv, D, scale);
+    if (st != SKIPFFN_OK) return st;
+    if ((st = check_heads(q, Tq, Hq, D, false)) || (st = check_heads(k, Tk, Hkv, D, false)) || (st = check_heads(v, Tk, Hkv, D, false)) ||
+        (st = check_heads(out, Tq, Hq, D, false)) || (st = check_heads(grad_out, Tq, Hq, D, false)) || (st = check_heads(grad_q, Tq, Hq, D, true)) ||
+        (st = check_heads(grad_k, Tk, Hkv, D, true)) || (st = check_heads(grad_v, Tk, Hkv, D, true)))
+        return st;
+    if (seg_k == nullptr && Tq != Tk) return SKIPFFN_EINVAL;
+    if (n_seq == 0 || (Tq == 0 && Tk == 0)) return SKIPFFN_OK;
+    if (bad_seg(seg_q) || (seg_k != nullptr && bad_seg(seg_k)) || (Tq > 0 && bad_ptr(saved))) return SKIPFFN_EINVAL;
+    const skipffn_heads* ins[5] = {q, out, grad_out, k, v};
+    const skipffn_heads* outs[3] = {grad_q, grad_k, grad_v};
+    for (int o = 0; o < 3; ++o) {
+        const int64_t To = o == 0 ? Tq : Tk, Ho = o == 0 ? Hq : Hkv;
+        for (int i = 0; i < 5; ++i)
+            if (heads_meet(outs[o], To, Ho, ins[i], i < 3 ? Tq : Tk, i < 3 ? Hq : Hkv, D)) return SKIPFFN_EINVAL;
+        if (To > 0 && outs[o]->data == outs[(o + 1) % 3]->data) return SKIPFFN_EINVAL;
+    }
+    if (Tq > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < align_up((size_t)Tq * Hq * 4))) return SKIPFFN_EWORKSPACE;
+    hipStream_t s = (hipStream_t)stream;
+    const AttnArgs a = attn_args(Tq, Tk, n_seq, Hq, Hkv, D, q, k, v, out, seg_q, seg_k, causal, scale,
+                                 const_cast<float*>(static_cast<const float*>(saved)));
+    AttnGrads gr{};
+    gr.go = in(grad_out); gr.go_tok = (int)grad_out->token_stride; gr.go_head = grad_out->head_stride;
+    gr.dq = to(grad_q); gr.dk = to(grad_k); gr.dv = to(grad_v);
+    gr.dq_tok = (int)grad_q->token_stride; gr.dk_tok = (int)grad_k->token_stride; gr.dv_tok = (int)grad_v->token_stride;
+    gr.dq_head = grad_q->head_stride; gr.dk_head = grad_k->head_stride; gr.dv_head = grad_v->head_stride;
+    gr.delta = static_cast<float*>(workspace);
+    profile_mark_begin(KC_ATTN_BWD, s);
+    hipError_t e = launch_attn_backward(a, gr, s);
+    profile_mark_end(KC_ATTN_BWD, s);
     return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
 }
 

@@ -1,0 +1,246 @@
+// Attention over whole prompts, backward.  With P_ij = exp(S_ij - lse_i), S = scale Q K^T, and delta_i = dO_i . o_i
+// (= sum_j P_ij dP_ij, as o is the normalised output):
+//     dP = dO V^T,  dS = P (dP - delta),  dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO
+// with dK and dV summed over the query heads of a key/value head.  P is computed again from the saved log-sum-exp, so nothing of
+// size queries x keys is kept.  Two kernels, each the owner of what it writes, so that no sum depends on an order of atomics:
+// one by queries (dQ, and delta on the way), one by keys (dK, dV).  That is 7 products for the 5 that one kernel would take, and
+// no fp32 traffic for partial dQ.
+#include "attn.hpp"
+
+namespace skipffn {
+
+constexpr int DQ_KEYS = 64;
+
+// ---- dQ, delta: a wavefront has a unit of 32 queries of one head, as in the forward kernel ------------------------------------
+template <int DP>
+__global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs P, const AttnGrads G) {
+    constexpr int TILE = DQ_KEYS * tile_row_bytes<DP>();
+    __shared__ __align__(16) char smem[4 * TILE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int kvh = (int)blockIdx.x % P.Hkv, g = P.Hq / P.Hkv;
+    int seq, item, q0, q1, k0, k1;
+    if (!locate_item(P.seg_q, P.n_seq, P.Tq, (int)blockIdx.x / P.Hkv,
+                     [&](int n) { return ((n + ATT_ROWS - 1) / ATT_ROWS * g + ATT_WAVES - 1) / ATT_WAVES; }, seq, item, q0, q1))
+        return;
+    seg_bounds(P.seg_k, seq, P.Tk, k0, k1);
+    const int nq = q1 - q0, nk = k1 - k0, ahead = nk - nq;
+    const int units = (nq + ATT_ROWS - 1) / ATT_ROWS * g;
+    const int first = units - 1 - item * ATT_WAVES, unit = first - wave;
+    const int row0 = unit >= 0 ? unit / g * ATT_ROWS : 0, head = kvh * g + (unit >= 0 ? unit % g : 0);
+    auto keys_of = [&](int row) { const int n = P.causal ? row + 1 + ahead : nk; return n < nk ? n : nk; };
+    const int last = first / g * ATT_ROWS + ATT_ROWS;
+    const int tiles = (max(keys_of((last < nq ? last : nq) - 1), 0) + DQ_KEYS - 1) / DQ_KEYS;
+    const int wave_end = unit >= 0 ? keys_of((row0 + ATT_ROWS < nq ? row0 + ATT_ROWS : nq) - 1) : 0;
+    const int all_see = keys_of(row0);
+    const int row = row0 + (lane & 31);
+    const bool row_ok = unit >= 0 && row < nq;
+    const int row_keys = keys_of(row);
+
+    bf16x8 qf[DP / 16], gf[DP / 16];
+    float delta = 0.0f, lse = INFINITY;
+    {
+        const uint32_t r = (uint32_t)(lane & 31) * 2u;
+        const int64_t t = q0 + row0;
+        load_rows<DP>(make_rsrc(P.q + head * P.q_head + t * P.q_tok, 0x7fffffffu), r * (uint32_t)P.q_tok, row_ok, P.D, lane, qf);
+        load_rows<DP>(make_rsrc(G.go + head * G.go_head + t * G.go_tok, 0x7fffffffu), r * (uint32_t)G.go_tok, row_ok, P.D, lane, gf);
+        bf16x8 of[DP / 16];
+        load_rows<DP>(make_rsrc(P.out + head * P.o_head + t * P.o_tok, 0x7fffffffu), r * (uint32_t)P.o_tok, row_ok, P.D, lane, of);
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d) {
+            float a[8], b[8];
+            unpack_bf16x8(gf[d], a);
+            unpack_bf16x8(of[d], b);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) delta = fmaf(a[j], b[j], delta);
+        }
+        delta = halves_sum(delta);
+        if (row_ok) {
+            const int64_t at = (int64_t)head * P.Tq + q0 + row;
+            lse = P.lse[at];
+            if (h == 0) G.delta[at] = delta;
+        }
+    }
+    const HeadRows K{P.k + kvh * P.k_head + (int64_t)k0 * P.k_tok, P.k_tok}, V{P.v + kvh * P.v_head + (int64_t)k0 * P.v_tok, P.v_tok};
+    const uint32_t k_off = TileLoad<DP, DQ_KEYS>::first(tid, P.k_tok, P.D), v_off = TileLoad<DP, DQ_KEYS>::first(tid, P.v_tok, P.D);
+    TileLoad<DP, DQ_KEYS> lk, lv;
+    f32x16 acc[DP / 32] = {};
+    const float c = P.scale_log2;
+    if (tiles > 0) {
+        lk.load(K, 0, nk, P.D, k_off);
+        lv.load(V, 0, nk, P.D, v_off);
+        lk.store(smem, tid);
+        lv.store(smem + TILE, tid);
+    }
+    __syncthreads();
+    for (int t = 0; t < tiles; ++t) {
+        char* tk = smem + (t & 1) * 2 * TILE;
+        char* tv = tk + TILE;
+        if (t + 1 < tiles) {
+            lk.load(K, (t + 1) * DQ_KEYS, nk, P.D, k_off);
+            lv.load(V, (t + 1) * DQ_KEYS, nk, P.D, v_off);
+        }
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const int key0 = t * DQ_KEYS + kb * 32;
+            if (key0 >= wave_end) continue;
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d)
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d, lane), qf[d], s, 0, 0, 0);
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d)
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tv, kb * 32, d, lane), gf[d], dp, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse)) * (dp[i] - delta);
+            if (key0 + 32 > all_see) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (key0 + 8 * (i >> 2) + 4 * h + (i & 3) >= row_keys) s[i] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 ds = pack_frag(s, k);
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db)
+                    acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tk, kb * 32 + k * 16, db, lane), ds, acc[db], 0, 0, 0);
+            }
+        }
+        if (t + 1 < tiles) {
+            char* nx = smem + ((t + 1) & 1) * 2 * TILE;
+            lk.store(nx, tid);
+            lv.store(nx + TILE, tid);
+        }
+        __syncthreads();
+    }
+    if (row_ok) store_cols<DP>(G.dq + head * G.dq_head + (int64_t)(q0 + row) * G.dq_tok, acc, P.scale, P.D, h);
+}
+
+// ---- dK, dV: a wavefront has 32 keys and goes over the queries that see them, head by head of its group -------------------------
+constexpr int DKV_KEYS = ATT_WAVES * 32, DKV_ROWS = 32;
+
+template <int DP>
+__global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs P, const AttnGrads G) {
+    constexpr int ROWB = tile_row_bytes<DP>(), TILE = DKV_ROWS * ROWB, STAGE = 2 * TILE + 2 * DKV_ROWS * 4;
+    __shared__ __align__(16) char smem[DKV_KEYS * ROWB + 2 * STAGE];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int kvh = (int)blockIdx.x % P.Hkv, g = P.Hq / P.Hkv;
+    int seq, item, q0, q1, k0, k1;
+    if (!locate_item(P.seg_k, P.n_seq, P.Tk, (int)blockIdx.x / P.Hkv, [](int n) { return (n + DKV_KEYS - 1) / DKV_KEYS; }, seq, item, k0, k1))
+        return;
+    seg_bounds(P.seg_q, seq, P.Tq, q0, q1);
+    const int nq = q1 - q0, nk = k1 - k0, ahead = nk - nq;
+    const int key0 = item * DKV_KEYS + wave * 32, key = key0 + (lane & 31);
+    // row i sees key j if j <= i + ahead
+    const int row_first = P.causal ? max(item * DKV_KEYS - ahead, 0) / DKV_ROWS : 0;
+    const int row_tiles = max((nq + DKV_ROWS - 1) / DKV_ROWS - row_first, 0), steps = row_tiles * g;
+
+    char* tv = smem;
+    char* stage = smem + DKV_KEYS * ROWB;
+    bf16x8 kf[DP / 16];
+    {
+        const HeadRows V{P.v + kvh * P.v_head + (int64_t)k0 * P.v_tok, P.v_tok};
+        TileLoad<DP, DKV_KEYS> lv;
+        lv.load(V, item * DKV_KEYS, nk, P.D, TileLoad<DP, DKV_KEYS>::first(tid, P.v_tok, P.D));
+        load_rows<DP>(make_rsrc(P.k + kvh * P.k_head + (int64_t)(k0 + key0) * P.k_tok, 0x7fffffffu), (uint32_t)((lane & 31) * P.k_tok) * 2u,
+                      key < nk, P.D, lane, kf);
+        lv.store(tv, tid);
+    }
+    const uint32_t q_off = TileLoad<DP, DKV_ROWS>::first(tid, P.q_tok, P.D), g_off = TileLoad<DP, DKV_ROWS>::first(tid, G.go_tok, P.D);
+    TileLoad<DP, DKV_ROWS> lq, lg;
+    float stat = 0.0f;                                   // thread t < 32: row t's log-sum-exp, t of 32 .. 63: delta
+    auto load = [&](int n) {
+        const int head = kvh * g + n / row_tiles, r0 = (row_first + n % row_tiles) * DKV_ROWS;
+        lq.load(HeadRows{P.q + head * P.q_head + (int64_t)q0 * P.q_tok, P.q_tok}, r0, nq, P.D, q_off);
+        lg.load(HeadRows{G.go + head * G.go_head + (int64_t)q0 * G.go_tok, G.go_tok}, r0, nq, P.D, g_off);
+        if (tid < 64) {
+            const int r = r0 + (tid & 31);
+            const float* src = tid < 32 ? P.lse : G.delta;
+            stat = r < nq ? src[(int64_t)head * P.Tq + q0 + r] : (tid < 32 ? INFINITY : 0.0f);
+        }
+    };
+    auto store = [&](int n) {
+        char* st = stage + (n & 1) * STAGE;
+        lq.store(st, tid);
+        lg.store(st + TILE, tid);
+        if (tid < 64) reinterpret_cast<float*>(st + 2 * TILE)[tid] = stat;
+    };
+    f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
+    const float c = P.scale_log2;
+    if (steps > 0) {
+        load(0);
+        store(0);
+    }
+    __syncthreads();
+    for (int n = 0; n < steps; ++n) {
+        char* tq = stage + (n & 1) * STAGE;
+        char* tg = tq + TILE;
+        const float* st = reinterpret_cast<const float*>(tq + 2 * TILE);
+        if (n + 1 < steps) load(n + 1);
+        const int r0 = (row_first + n % row_tiles) * DKV_ROWS;
+        if (key0 < nk && (!P.causal || key0 <= min(r0 + DKV_ROWS, nq) - 1 + ahead)) {
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d)
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tq, 0, d, lane), kf[d], s, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 8 * i + 4 * h);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[4 * i + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * i + j], c, -lse[j]));
+            }
+            const bool masked = P.causal && key0 + 31 > r0 + ahead;
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (key > r0 + 8 * (i >> 2) + 4 * h + (i & 3) + ahead) s[i] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 p = pack_frag(s, k);
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db)
+                    dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tg, k * 16, db, lane), p, dv[db], 0, 0, 0);
+            }
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d)
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tg, 0, d, lane), frag_rows<DP>(tv, wave * 32, d, lane), dp, 0, 0, 0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 delta = *reinterpret_cast<const f32x4*>(st + DKV_ROWS + 8 * i + 4 * h);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[4 * i + j] *= dp[4 * i + j] - delta[j];
+            }
+            if (masked) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (key > r0 + 8 * (i >> 2) + 4 * h + (i & 3) + ahead) s[i] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const bf16x8 ds = pack_frag(s, k);
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db)
+                    dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tq, k * 16, db, lane), ds, dk[db], 0, 0, 0);
+            }
+        }
+        if (n + 1 < steps) store(n + 1);
+        __syncthreads();
+    }
+    if (key < nk) {
+        store_cols<DP>(G.dk + kvh * G.dk_head + (int64_t)(k0 + key) * G.dk_tok, dk, P.scale, P.D, h);
+        store_cols<DP>(G.dv + kvh * G.dv_head + (int64_t)(k0 + key) * G.dv_tok, dv, 1.0f, P.D, h);
+    }
+}
+
+hipError_t launch_attn_backward(const AttnArgs& a, const AttnGrads& gr, hipStream_t s) {
+    const dim3 gq((uint32_t)attn_query_workgroups(a)), gk((uint32_t)(((int64_t)a.Tk / DKV_KEYS + a.n_seq) * a.Hkv));
+    if (a.D <= 64) attn_dq_kernel<64><<<gq, ATT_THREADS, 0, s>>>(a, gr);
+    else attn_dq_kernel<128><<<gq, ATT_THREADS, 0, s>>>(a, gr);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (a.D <= 64) attn_dkv_kernel<64><<<gk, ATT_THREADS, 0, s>>>(a, gr);
+    else attn_dkv_kernel<128><<<gk, ATT_THREADS, 0, s>>>(a, gr);
+    return hipGetLastError();
+}
+
+}  // namespace skipffn

@@ -30,6 +30,9 @@ enum KernelClass : int {
     KC_SELECT,
     KC_MERGE,
     KC_GEMM_DXN_DW,
+    KC_ATTN_FWD,
+    KC_ATTN_BWD,
+    KC_ATTN_DECODE,
     KC_COUNT
 };
 const char* kernel_class_name(int kc);
@@ -164,6 +167,28 @@ hipError_t count_rows_init();    // raises the dynamic-LDS limits (once per proc
 hipError_t launch_gate_up_count(GemmArgs& args, hipStream_t s);
 // partial (for 16 slabs of 256 rows and 8 of the bound) or out0, e0, idx, as the plan of the count wants them
 hipError_t launch_down_count(GemmArgs& args, const RowPlans& plans, hipStream_t s);
+
+// ---- attention (attn_fwd.hip, attn_bwd.hip, attn_decode.hip) ----------------------------------------------------
+// Element (t, h, d) of a tensor lies at base[t * tok + h * head + d].  seg_q, seg_k: rows of every sequence.
+constexpr int ATTN_MAX_D = 128;
+struct AttnArgs {
+    int Tq, Tk, n_seq, Hq, Hkv, D, causal;
+    float scale, scale_log2;                      // scale_log2 = scale * log2(e): weights are powers of two of the products
+    const bf16_t* q; const bf16_t* k; const bf16_t* v; bf16_t* out;
+    int q_tok, k_tok, v_tok, o_tok;
+    int64_t q_head, k_head, v_head, o_head;
+    const int32_t* seg_q; const int32_t* seg_k;
+    float* lse;                                   // [Hq][Tq], base 2, or null; infinity: the row sees no key
+};
+struct AttnGrads {
+    const bf16_t* go; int go_tok; int64_t go_head;
+    bf16_t* dq; bf16_t* dk; bf16_t* dv;
+    int dq_tok, dk_tok, dv_tok;
+    int64_t dq_head, dk_head, dv_head;
+    float* delta;                                 // [Hq][Tq]
+};
+hipError_t launch_attn_forward(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_backward(const AttnArgs& a, const AttnGrads& g, hipStream_t s);
 
 // ---- GEMMs -----------------------------------------------------------------------
 hipError_t gemm_init();   // raises the dynamic-LDS limit of every instantiation (once per process)

@@ -1,0 +1,138 @@
+"""Attention over packed prompts and its gradients through the C ABI against the oracle, element by element within the
+bounds of attn_bounds."""
+import numpy as np
+import pytest
+import torch
+
+from attn_bounds import assert_within, grad_bounds, out_bound
+from oracle import skipffn_oracle as O
+from paper_2503_21817_amd import binding as B
+from helpers import bits_of, f64_of, to_dev_bf16
+
+pytestmark = pytest.mark.gpu
+
+BEHIND = 3           # rows behind the last sequence
+
+
+def offsets(lens):
+    return torch.tensor(np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)).cuda()
+
+
+def nbytes(n):
+    return torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+
+
+class Prompt:
+    """Inputs on the device in one of the layouts a program has them in: `fused` (column ranges of one projection's output),
+    `cache` (k, v by head), `plain` (a tensor each).  Behind the last sequence there are rows of NaN."""
+
+    def __init__(self, nq, nk, Hq, Hkv, D, layout="fused", seed=0, q_std=1.0):
+        rng = np.random.default_rng(seed + sum(nq) + D)
+        self.nq, self.nk, self.Hq, self.Hkv, self.D = list(nq), list(nk), Hq, Hkv, D
+        self.T, self.Tk = sum(nq) + BEHIND, sum(nk) + BEHIND
+        if layout == "fused":
+            assert nq == nk
+            self.all = self._bits(rng, self.T, Hq + 2 * Hkv)
+            t = to_dev_bf16(self.all)
+            self.q, self.k, self.v = t[:, :Hq], t[:, Hq:Hq + Hkv], t[:, Hq + Hkv:]
+            g = torch.full((self.T, Hq + 2 * Hkv, D), 7.0, dtype=torch.bfloat16, device="cuda")
+            self.dq, self.dk, self.dv = g[:, :Hq], g[:, Hq:Hq + Hkv], g[:, Hq + Hkv:]
+        else:
+            self.q = to_dev_bf16(self._bits(rng, self.T, Hq, q_std))
+            kv = [to_dev_bf16(self._bits(rng, self.Tk, Hkv)) for _ in range(2)]
+            if layout == "cache":
+                kv = [t.transpose(0, 1).contiguous().transpose(0, 1) for t in kv]
+            self.k, self.v = kv
+            self.dq, self.dk, self.dv = (torch.full_like(t, 7.0) for t in (self.q, self.k, self.v))
+        self.g = to_dev_bf16(self._bits(rng, self.T, Hq))
+        self.out = torch.full((self.T, Hq, D), 7.0, dtype=torch.bfloat16, device="cuda")
+        self.seg_q, self.seg_k = offsets(nq), None if nq == nk else offsets(nk)
+        self.saved = nbytes(B.skipffn_attn_saved_bytes(self.T, Hq))
+        sizes = (self.T, self.Tk, len(nq), Hq, Hkv, D)
+        self.fws, self.bws = nbytes(B.skipffn_attn_forward_workspace_bytes(*sizes)), nbytes(B.skipffn_attn_backward_workspace_bytes(*sizes))
+
+    def _bits(self, rng, T, H, std=1.0):
+        x = rng.standard_normal((T, H, self.D)) * std
+        x[T - BEHIND:] = np.nan
+        return O.f64_to_bf16_bits(x)
+
+    def forward(self, causal, scale, saved=True):
+        B.skipffn_attn_forward(self.q, self.k, self.v, self.out, self.seg_q, self.seg_k, causal=causal, scale=scale,
+                               saved=self.saved if saved else None, workspace=self.fws)
+
+    def backward(self, causal, scale):
+        B.skipffn_attn_backward(self.q, self.k, self.v, self.out, self.g, self.seg_q, self.seg_k, self.saved, self.dq, self.dk,
+                                self.dv, causal=causal, scale=scale, workspace=self.bws)
+
+    def check(self, causal, scale, gradients):
+        torch.cuda.synchronize()
+        f = {n: f64_of(getattr(self, n)) for n in ("q", "k", "v", "g", "out", "dq", "dk", "dv")}
+        aq = ak = 0
+        for s, (nq, nk) in enumerate(zip(self.nq, self.nk)):
+            rq, rk = slice(aq, aq + nq), slice(ak, ak + nk)
+            aq, ak = aq + nq, ak + nk
+            q, k, v, g = f["q"][rq], f["k"][rk], f["v"][rk], f["g"][rq]
+            b = O.attn_backward_real(q, k, v, g, causal, scale)
+            assert_within(f["out"][rq], b["out"], out_bound(b["P"], v, b["out"]), f"out, sequence {s}")
+            if gradients:
+                e = grad_bounds(q, k, v, g, scale, b)
+                for n, r in (("dq", rq), ("dk", rk), ("dv", rk)):
+                    assert_within(f[n][r], b[n], e[n], f"{n}, sequence {s}")
+        assert np.all(f["out"][aq:] == 7.0)
+        assert np.all(f["dq"][aq if gradients else 0:] == 7.0)
+        assert all(np.all(f[n][ak if gradients else 0:] == 7.0) for n in ("dk", "dv"))
+
+
+LENGTHS = [(1,), (31, 0, 33, 64), (129, 65, 1, 128), (300, 17), (63, 32, 2)]
+
+
+@pytest.mark.parametrize("lens", LENGTHS, ids=str)
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 2, 128), (3, 3, 64), (6, 2, 80), (5, 1, 40), (8, 2, 96), (2, 2, 8)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+def test_packed_sequences_forward_and_backward(lens, Hq, Hkv, D, causal):
+    print(f"attention {lens} heads {Hq}/{Hkv} D={D} causal={causal}", flush=True)
+    p = Prompt(lens, lens, Hq, Hkv, D, "fused")
+    p.forward(causal, D ** -0.5)
+    p.backward(causal, D ** -0.5)
+    p.check(causal, D ** -0.5, True)
+
+
+@pytest.mark.parametrize("nq,nk", [((1, 1, 1), (1, 300, 64)), ((40, 7), (333, 7)), ((50, 64, 3), (20, 63, 0)), ((5, 0, 9), (0, 70, 129)),
+                                   ((130,), (1000,))], ids=str)
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 128), (2, 2, 64), (6, 2, 72)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+@pytest.mark.parametrize("layout", ["cache", "plain"])
+def test_queries_after_or_beyond_their_keys(nq, nk, Hq, Hkv, D, causal, layout):
+    """More keys than queries (new tokens after cached ones), fewer (rows that see nothing), none."""
+    print(f"attention {nq} over {nk} heads {Hq}/{Hkv} D={D} causal={causal} {layout}", flush=True)
+    p = Prompt(nq, nk, Hq, Hkv, D, layout)
+    p.forward(causal, 0.11)
+    p.backward(causal, 0.11)
+    p.check(causal, 0.11, True)
+
+
+def test_inference_writes_no_statistics_and_the_same_rows():
+    p = Prompt((70, 200), (70, 200), 4, 2, 128)
+    p.forward(True, 0.1)
+    want = bits_of(p.out)
+    p.out.fill_(7.0)
+    p.saved.fill_(0xA5)
+    p.forward(True, 0.1, saved=False)
+    torch.cuda.synchronize()
+    assert np.array_equal(bits_of(p.out), want) and bool((p.saved == 0xA5).all())
+
+
+def test_peaked_softmax_and_large_scores():
+    """Queries of 30 times the usual size: weights of nearly 0 and 1, scores of some hundred, maxima that grow along the row."""
+    p = Prompt((257, 90), (257, 90), 2, 2, 64, "plain", q_std=30.0)
+    f = {n: f64_of(getattr(p, n)) for n in "qkv"}
+    p.forward(True, 0.125)
+    torch.cuda.synchronize()
+    got, a = f64_of(p.out), 0
+    for n in p.nq:
+        r = slice(a, a + n)
+        a += n
+        out, P = O.attn_forward_real(f["q"][r], f["k"][r], f["v"][r], True, 0.125)
+        # a score is off by up to 64 products of 2^-24 |q| |k| scale log2(e): |q| . |k| is about 64 x 30 x 0.64, so 0.0014 in the exponent
+        extra = 0.001 * 2 * np.stack([P[h] @ np.abs(f["v"][r][:, h]) for h in range(2)], axis=1)
+        assert_within(got[r], out, out_bound(P, f["v"][r], out) + extra, "out")
