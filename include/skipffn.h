@@ -334,6 +334,33 @@ int skipffn_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int
                           const void* saved, const skipffn_heads* grad_q, const skipffn_heads* grad_k,
                           const skipffn_heads* grad_v, void* workspace, size_t workspace_bytes, void* stream);
 
+/* Attention of one new token a sequence over the cache that is left (Section 4.3): the rows of a prefix
+ * that the sequences of a group share (several questions about one image), then each sequence's own rows
+ * (its tokens so far, the new one's key and value among them).  The prefix is read once for the sequences that
+ * fit one product (32 rows of query heads), not once a sequence.
+ *   q, out [n_seq, Hq, D]     token = sequence; q's head_stride < 2^24
+ *   prefix_k, prefix_v        [Tp, Hkv, D], e.g. one layer of what skipffn_kv_compact wrote: head_stride =
+ *                             capacity * D.  Read only where n_groups > 0 and Tp > 0
+ *   prefix_seg  i32 [n_groups + 1] device: group i has the prefix rows prefix_seg[i] .. prefix_seg[i+1])
+ *   group_off   i32 [n_groups + 1] device, ascending from 0: group i has the sequences group_off[i] ..
+ *                             group_off[i+1]); sequences from group_off[n_groups] on have no prefix.
+ *                             n_groups == 0: no sequence has one (both may be NULL)
+ *   suffix_k, suffix_v        [n_seq][suffix_capacity, Hkv, D], sequence s suffix_k_seq (suffix_v_seq) elements
+ *                             after the one before it.  Not read where suffix_capacity == 0
+ *   suffix_len  i32 [n_seq] device: own rows of every sequence (clamped to 0 .. suffix_capacity)
+ * A sequence with no rows at all gives a zero row.  Types, scale and shapes as above; out may not meet q or
+ * the caches.  workspace: at least skipffn_attn_decode_workspace_bytes(...), which holds fp32 rows of the parts
+ * that long caches are cut into.  The parts depend on the bounds of the call (Tp, suffix_capacity, n_groups),
+ * not on the lengths on the device.  Deterministic. */
+size_t skipffn_attn_decode_workspace_bytes(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp,
+                                           int64_t suffix_capacity);
+int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp,
+                        int64_t suffix_capacity, const skipffn_heads* q, const skipffn_heads* prefix_k,
+                        const skipffn_heads* prefix_v, const int32_t* prefix_seg, const int32_t* group_off,
+                        const skipffn_heads* suffix_k, const skipffn_heads* suffix_v, int64_t suffix_k_seq, int64_t suffix_v_seq,
+                        const int32_t* suffix_len, const skipffn_heads* out, float scale,
+                        void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- layout of `saved`, for tests that compare stage by stage -------------
  * Byte offsets of the sections inside a saved buffer for (R_max, C, I):
  * offsets[0] x rows bf16 [R, C]; [1] normalised rows bf16 [R, C];

@@ -74,6 +74,9 @@ _SIGNATURES = {
     "skipffn_attn_backward_workspace_bytes": (c_size_t, [c_int64] * 6),
     "skipffn_attn_backward": (c_int, [c_int64] * 6 + [POINTER(Heads)] * 5 + [c_void_p, c_void_p, c_int, c_float, c_void_p] +
                               [POINTER(Heads)] * 3 + [c_void_p, c_size_t, c_void_p]),
+    "skipffn_attn_decode_workspace_bytes": (c_size_t, [c_int64] * 7),
+    "skipffn_attn_decode": (c_int, [c_int64] * 7 + [POINTER(Heads)] * 3 + [c_void_p] * 2 + [POINTER(Heads)] * 2 + [c_int64] * 2 +
+                            [c_void_p, POINTER(Heads), c_float, c_void_p, c_size_t, c_void_p]),
     "skipffn_probe_mfma": (c_int, [c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p]),
     "skipffn_saved_layout": (c_int, [c_int64, c_int64, c_int64, POINTER(c_size_t)]),
     "skipffn_status_string": (c_char_p, [c_int]),
@@ -302,11 +305,15 @@ def skipffn_token_merge_backward(grad_out, seg, assign, grad_x):
            "skipffn_token_merge_backward")
 
 
+def _stride(t, i):
+    return t.stride(i) if t.shape[i] > 1 else 0
+
+
 def _heads(t, where):
     """A tensor [tokens, heads, columns] whose columns lie together, as the library takes it."""
     if t.dim() != 3 or t.dtype != torch.bfloat16 or (t.stride(2) != 1 and t.shape[2] > 1):
         raise ValueError(f"{where}: a bfloat16 tensor [tokens, heads, columns] with contiguous columns is wanted")
-    return byref(Heads(t.data_ptr(), t.stride(0), t.stride(1)))
+    return byref(Heads(t.data_ptr(), _stride(t, 0), _stride(t, 1)))
 
 
 def _same(where, *pairs):
@@ -363,6 +370,41 @@ def skipffn_attn_backward(q, k, v, out, grad_out, seg_q, seg_k, saved, grad_q, g
                                        sizes[-1] ** -0.5 if scale is None else scale, _ptr(saved), _heads(grad_q, where),
                                        _heads(grad_k, where), _heads(grad_v, where), _ptr(workspace), _nbytes(workspace), _stream()),
            where)
+
+
+def skipffn_attn_decode_workspace_bytes(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity) -> int:
+    return lib().skipffn_attn_decode_workspace_bytes(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity)
+
+
+def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, *, scale=None,
+                        workspace=None):
+    """q, out bf16 [n_seq, Hq, D]; prefix_k, prefix_v bf16 [Tp, Hkv, D] with prefix_seg, group_off i32 [n_groups + 1], or all
+    four None; suffix_k, suffix_v bf16 [n_seq, capacity, Hkv, D] with suffix_len i32 [n_seq], or all three None.
+    scale: None is 1 / sqrt(D)."""
+    where = "skipffn_attn_decode"
+    n_seq, Hq, D = q.shape
+    if prefix_k is None and suffix_k is None:
+        raise ValueError(f"{where}: a prefix or own rows are wanted")
+    Hkv = (suffix_k if prefix_k is None else prefix_k).shape[-2]
+    Tp = n_groups = cap = seq_k = seq_v = 0
+    pk = pv = sk = sv = None
+    for t in (prefix_seg, group_off, suffix_len):
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+            raise ValueError(f"{where}: offsets and lengths are contiguous int32 tensors")
+    _same(where, (out.shape, q.shape))
+    if prefix_k is not None:
+        Tp, n_groups = prefix_k.shape[0], group_off.numel() - 1
+        _same(where, (prefix_k.shape, (Tp, Hkv, D)), (prefix_v.shape, (Tp, Hkv, D)), (prefix_seg.shape, (n_groups + 1,)))
+        pk, pv = _heads(prefix_k, where), _heads(prefix_v, where)
+    if suffix_k is not None:
+        cap = suffix_k.shape[1]
+        _same(where, (suffix_k.shape, (n_seq, cap, Hkv, D)), (suffix_v.shape, (n_seq, cap, Hkv, D)), (suffix_len.shape, (n_seq,)))
+        seq_k, seq_v = _stride(suffix_k, 0), _stride(suffix_v, 0)
+        if n_seq > 0:
+            sk, sv = _heads(suffix_k[0], where), _heads(suffix_v[0], where)
+    _check(lib().skipffn_attn_decode(n_seq, n_groups, Hq, Hkv, D, Tp, cap, _heads(q, where), pk, pv, _ptr(prefix_seg), _ptr(group_off),
+                                     sk, sv, seq_k, seq_v, _ptr(suffix_len), _heads(out, where), D ** -0.5 if scale is None else scale,
+                                     _ptr(workspace), _nbytes(workspace), _stream()), where)
 
 
 def skipffn_probe_mfma(blocks, iters, random_operands, out, clocks):

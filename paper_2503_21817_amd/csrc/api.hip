@@ -937,6 +937,85 @@ int skipffn_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int
     return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
 }
 
+namespace {
+int check_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t cap, float scale) {
+    if (n_groups < 0 || cap < 0) return SKIPFFN_EINVAL;
+    const int st = check_attn(n_seq, Tp, n_groups, Hq, Hkv, D, scale);
+    if (st != SKIPFFN_OK) return st;
+    if (n_groups > 65534 || cap >= (1 << 30) || (n_seq + n_groups + 1) * Hq >= (1ll << 31)) return SKIPFFN_ESHAPE;
+    return SKIPFFN_OK;
+}
+struct DecodeWs { int splits; size_t part, stat, total; };
+DecodeWs decode_ws(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t cap) {
+    DecodeWs W{};
+    W.splits = attn_decode_splits(n_seq, n_groups, Hq, Hkv, Tp, cap, num_cus());
+    if (W.splits == 1) return W;
+    const size_t rows = (size_t)n_seq * Hq * W.splits;
+    W.part = 0;
+    W.stat = align_up(rows * attn_padded_columns((int)D) * 4);
+    W.total = W.stat + align_up(rows * 8);
+    return W;
+}
+}  // namespace
+
+size_t skipffn_attn_decode_workspace_bytes(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp,
+                                           int64_t suffix_capacity) {
+    if (check_decode(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, 1.0f) != SKIPFFN_OK) return 0;
+    return decode_ws(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity).total;
+}
+
+int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t suffix_capacity,
+                        const skipffn_heads* q, const skipffn_heads* prefix_k, const skipffn_heads* prefix_v, const int32_t* prefix_seg,
+                        const int32_t* group_off, const skipffn_heads* suffix_k, const skipffn_heads* suffix_v, int64_t suffix_k_seq,
+                        int64_t suffix_v_seq, const int32_t* suffix_len, const skipffn_heads* out, float scale,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    int st = check_decode(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, scale);
+    if (st != SKIPFFN_OK) return st;
+    if ((st = check_heads(q, n_seq, Hq, D, false)) || (st = check_heads(out, n_seq, Hq, D, true))) return st;
+    if (q->head_stride >= (1 << 24)) return SKIPFFN_ESHAPE;
+    const int64_t cap = suffix_capacity, Tg = n_groups > 0 ? Tp : 0;
+    if (n_groups > 0 && (bad_seg(group_off) || bad_seg(prefix_seg))) return SKIPFFN_EINVAL;
+    if (Tg > 0 && ((st = check_heads(prefix_k, Tg, Hkv, D, false)) || (st = check_heads(prefix_v, Tg, Hkv, D, false)))) return st;
+    if (cap > 0) {
+        if ((st = check_heads(suffix_k, cap, Hkv, D, false)) || (st = check_heads(suffix_v, cap, Hkv, D, false))) return st;
+        if (suffix_k_seq < 0 || suffix_v_seq < 0 || bad_seg(suffix_len)) return SKIPFFN_EINVAL;
+        if ((suffix_k_seq & 7) || (suffix_v_seq & 7) || suffix_k_seq >= ((int64_t)1 << 44) || suffix_v_seq >= ((int64_t)1 << 44)) return SKIPFFN_ESHAPE;
+    }
+    if (n_seq == 0) return SKIPFFN_OK;
+    const uintptr_t o0 = reinterpret_cast<uintptr_t>(out->data), o1 = o0 + (uintptr_t)heads_span(out, n_seq, Hq, D);
+    auto meets = [&](const skipffn_heads* t, int64_t T, int64_t H, int64_t more) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(t->data);
+        return o0 < x + (uintptr_t)(more * 2 + heads_span(t, T, H, D)) && x < o1;
+    };
+    if (meets(q, n_seq, Hq, 0) || (Tg > 0 && (meets(prefix_k, Tg, Hkv, 0) || meets(prefix_v, Tg, Hkv, 0))) ||
+        (cap > 0 && (meets(suffix_k, cap, Hkv, (n_seq - 1) * suffix_k_seq) || meets(suffix_v, cap, Hkv, (n_seq - 1) * suffix_v_seq))))
+        return SKIPFFN_EINVAL;
+    const DecodeWs W = decode_ws(n_seq, n_groups, Hq, Hkv, D, Tp, cap);
+    if (W.total > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < W.total)) return SKIPFFN_EWORKSPACE;
+    hipStream_t s = (hipStream_t)stream;
+    AttnDecodeArgs a{};
+    a.n_seq = (int)n_seq; a.n_groups = (int)n_groups; a.Hq = (int)Hq; a.Hkv = (int)Hkv; a.D = (int)D;
+    a.Tp = (int)Tg; a.cap = (int)cap; a.splits = W.splits;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.q = in(q); a.q_tok = (int)q->token_stride; a.q_head = q->head_stride;
+    a.out = to(out); a.o_tok = (int)out->token_stride; a.o_head = out->head_stride;
+    if (Tg > 0) {
+        a.pk = in(prefix_k); a.pk_tok = (int)prefix_k->token_stride; a.pk_head = prefix_k->head_stride;
+        a.pv = in(prefix_v); a.pv_tok = (int)prefix_v->token_stride; a.pv_head = prefix_v->head_stride;
+    }
+    if (cap > 0) {
+        a.sk = in(suffix_k); a.sk_tok = (int)suffix_k->token_stride; a.sk_head = suffix_k->head_stride; a.sk_seq = suffix_k_seq;
+        a.sv = in(suffix_v); a.sv_tok = (int)suffix_v->token_stride; a.sv_head = suffix_v->head_stride; a.sv_seq = suffix_v_seq;
+    }
+    a.prefix_seg = prefix_seg; a.group_off = group_off; a.suffix_len = suffix_len;
+    char* ws = static_cast<char*>(workspace);
+    a.part = reinterpret_cast<float*>(ws + W.part); a.stat = reinterpret_cast<float*>(ws + W.stat);
+    profile_mark_begin(KC_ATTN_DECODE, s);
+    hipError_t e = launch_attn_decode(a, s);
+    profile_mark_end(KC_ATTN_DECODE, s);
+    return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
+}
+
 // ---- measurement aid ---------------------------------------------------------------------------------
 int skipffn_probe_mfma(int64_t blocks, int64_t iters, int random_operands, float* out, int64_t* clocks,
                        void* stream) {

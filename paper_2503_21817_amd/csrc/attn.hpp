@@ -41,13 +41,13 @@ struct HeadRows { const bf16_t* base; int stride; };
 
 // A tile of N rows on its way through registers: issued as buffer loads, stored to LDS a tile later.  Rows at and past `rows`
 // and columns at and past the head's read zeros (so a masked weight of 0 never meets what lies there).
-template <int DP, int N>
+template <int DP, int N, int THREADS = ATT_THREADS>
 struct TileLoad {
     static constexpr int CH = tile_row_bytes<DP>() / 16;        // 16-byte chunks of a row in LDS
-    static constexpr int PER = N * CH / ATT_THREADS;
-    static_assert(N * CH % ATT_THREADS == 0, "whole rows");
+    static constexpr int PER = N * CH / THREADS;
+    static_assert(N * CH % THREADS == 0, "whole rows");
     u32x4 v[PER];
-    // byte offset of the thread's first chunk, or none for a chunk past the head's columns; the next ones are ATT_THREADS / CH rows on
+    // byte offset of the thread's first chunk, or none for a chunk past the head's columns; the next ones are THREADS / CH rows on
     static __device__ __forceinline__ uint32_t first(int tid, int stride, int D) {
         const int c = tid % CH;
         return c * 8 < D ? (uint32_t)((tid / CH) * stride + c * 8) * 2u : kOobOffset;
@@ -58,12 +58,12 @@ struct TileLoad {
             make_rsrc(h.base + (int64_t)row0 * h.stride, n > 0 ? (uint32_t)((n - 1) * h.stride + D) * 2u : 0u);
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, (int)(off + (uint32_t)(i * (ATT_THREADS / CH) * h.stride) * 2u), 0, 0);
+            v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, (int)(off + (uint32_t)(i * (THREADS / CH) * h.stride) * 2u), 0, 0);
     }
     __device__ __forceinline__ void store(char* tile, int tid) const {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
-            *reinterpret_cast<u32x4*>(tile + tile_off<DP>(tid / CH + i * (ATT_THREADS / CH), tid % CH)) = v[i];
+            *reinterpret_cast<u32x4*>(tile + tile_off<DP>(tid / CH + i * (THREADS / CH), tid % CH)) = v[i];
     }
 };
 
@@ -126,16 +126,16 @@ __device__ __forceinline__ void store_cols(bf16_t* row, const f32x16 (&acc)[DP /
 }
 
 // ---- which sequence a workgroup works on ---------------------------------------------------------------
-// Sequence s has items(its length) workgroups; workgroup q of all -> s, its index among the sequence's, and the sequence's rows.
-// False past the last one.  A lane takes a sequence, a prefix sum over the lanes finds the workgroup's (whole wavefronts).
-template <class Items>
-__device__ __forceinline__ bool locate_item(const int32_t* __restrict__ seg, int S, int n_tok, int q, const Items& items,
-                                            int& s, int& item, int& t0, int& t1) {
+// Set s has items(its length) workgroups; workgroup q of all -> s, its index among the set's, and the set's bounds, which
+// bounds(s, b, e) gives.  False past the last one.  A lane takes a set, a prefix sum over the lanes finds the workgroup's (whole
+// wavefronts).
+template <class Bounds, class Items>
+__device__ __forceinline__ bool locate_in(int S, int q, const Bounds& bounds, const Items& items, int& s, int& item, int& t0, int& t1) {
     const int lane = threadIdx.x & 63;
     int cc = 0;
     for (int i0 = 0; i0 < S; i0 += 64) {
         int b = 0, e = 0;
-        if (i0 + lane < S) seg_bounds(seg, i0 + lane, n_tok, b, e);
+        if (i0 + lane < S) bounds(i0 + lane, b, e);
         const int nc = items(e - b);
         const int incl = wave_inclusive_sum(nc);
         const uint64_t past = __ballot(q < cc + incl);
@@ -150,6 +150,11 @@ __device__ __forceinline__ bool locate_item(const int32_t* __restrict__ seg, int
         cc += __builtin_amdgcn_readlane(incl, 63);
     }
     return false;
+}
+template <class Items>
+__device__ __forceinline__ bool locate_item(const int32_t* __restrict__ seg, int S, int n_tok, int q, const Items& items,
+                                            int& s, int& item, int& t0, int& t1) {
+    return locate_in(S, q, [&](int i, int& b, int& e) { seg_bounds(seg, i, n_tok, b, e); }, items, s, item, t0, t1);
 }
 
 // Workgroups of a kernel by queries: at least what the sequences take, whatever their lengths (the sum of ceil(ceil(n / 32) g / 4))

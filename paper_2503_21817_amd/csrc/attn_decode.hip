@@ -1,0 +1,251 @@
+// Attention of single new tokens over a cache: the rows of the prefix that the sequences of a group share, then each sequence's own.
+//
+// The rows of a product are (sequence, query head) pairs: as many sequences of a group as fill 32 rows with the heads of one
+// key/value head, so that a prefix is read once for all of them.  Their keys are one list of tiles of 32: the prefix's, seen by
+// every row, then each sequence's own, seen by its rows alone.  The list is cut into `splits` even parts, one a workgroup, and
+// a part is dealt out to the four wavefronts, each with tiles of its own in LDS (nothing is waited for but a wavefront's own loads);
+// the wavefronts' maxima, sums and rows are joined in LDS, those of the parts by a second kernel.  Bound by the reads of the cache.
+#include <algorithm>
+
+#include "attn.hpp"
+
+namespace skipffn {
+
+constexpr int DEC_KEYS = 32;
+
+template <int DP>
+__global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnDecodeArgs P) {
+    constexpr int ROWB = tile_row_bytes<DP>(), TILE = DEC_KEYS * ROWB;
+    static_assert(2 * TILE >= DP * 32 * 4, "a wavefront's sums fit where its tiles were");
+    __shared__ __align__(16) char smem[ATT_WAVES * 2 * TILE];
+    __shared__ float stat[ATT_WAVES][2][32];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+    const int g = P.Hq / P.Hkv, members = g >= 32 ? 1 : 32 / g, head_blocks = (g + 31) / 32;
+    // blockIdx.x: key/value head, then block of its query heads, then sequences; blockIdx.y: part
+    int b = (int)blockIdx.x;
+    const int kvh = b % P.Hkv; b /= P.Hkv;
+    const int hb = b % head_blocks; b /= head_blocks;
+    int group, item, s0, s1;
+    if (!locate_in(P.n_groups + 1, b,
+                   [&](int i, int& lo, int& hi) {
+                       if (i < P.n_groups) { seg_bounds(P.group_off, i, P.n_seq, lo, hi); return; }
+                       hi = P.n_seq;                                             // those of no group
+                       lo = P.n_groups > 0 ? min(max(P.group_off[P.n_groups], 0), P.n_seq) : 0;
+                   },
+                   [&](int n) { return (n + members - 1) / members; }, group, item, s0, s1))
+        return;
+    s0 += item * members;
+    const int ns = min(s1 - s0, members), heads = min(g - hb * 32, 32), rows = ns * heads;
+    int p0 = 0, p1 = 0;
+    if (group < P.n_groups && P.Tp > 0) seg_bounds(P.prefix_seg, group, P.Tp, p0, p1);
+    const int prefix_tiles = (p1 - p0 + DEC_KEYS - 1) / DEC_KEYS;
+    // lane i: own keys of sequence s0 + i and the tiles up to it
+    const int own_keys = lane < ns && P.cap > 0 ? min(max(P.suffix_len[s0 + lane], 0), P.cap) : 0;
+    const int own_tiles = (own_keys + DEC_KEYS - 1) / DEC_KEYS, own_sum = wave_inclusive_sum(own_tiles);
+    const int tiles = prefix_tiles + __builtin_amdgcn_readlane(own_sum, 63);
+    const int z = (int)blockIdx.y;
+    const int t_first = (int)((int64_t)tiles * z / P.splits) + wave, t_end = (int)((int64_t)tiles * (z + 1) / P.splits);
+
+    const int r = lane & 31, member = r / heads, head = kvh * g + hb * 32 + r % heads;
+    bf16x8 qf[DP / 16];
+    load_rows<DP>(make_rsrc(P.q + (int64_t)s0 * P.q_tok + (int64_t)(kvh * g + hb * 32) * P.q_head, 0x7fffffffu),
+                  (uint32_t)(member * P.q_tok + (r % heads) * (int)P.q_head) * 2u, r < rows, P.D, lane, qf);
+
+    char* tk = smem + wave * 2 * TILE;
+    char* tv = tk + TILE;
+    typedef TileLoad<DP, DEC_KEYS, 64> Load;
+    const uint32_t pk_off = Load::first(lane, P.pk_tok, P.D), pv_off = Load::first(lane, P.pv_tok, P.D);
+    const uint32_t sk_off = Load::first(lane, P.sk_tok, P.D), sv_off = Load::first(lane, P.sv_tok, P.D);
+    Load lk, lv;
+    int next_keys = 0, next_of = -1;                     // of the tile under way: its keys, and whose they are (-1: all rows')
+    auto load = [&](int t) {
+        if (t < prefix_tiles) {
+            next_of = -1;
+            next_keys = min(p1 - p0 - t * DEC_KEYS, DEC_KEYS);
+            lk.load(HeadRows{P.pk + kvh * P.pk_head + (int64_t)p0 * P.pk_tok, P.pk_tok}, t * DEC_KEYS, p1 - p0, P.D, pk_off);
+            lv.load(HeadRows{P.pv + kvh * P.pv_head + (int64_t)p0 * P.pv_tok, P.pv_tok}, t * DEC_KEYS, p1 - p0, P.D, pv_off);
+        } else {
+            const int u = t - prefix_tiles, i = __builtin_ctzll(__ballot(u < own_sum));
+            const int k0 = (u - __builtin_amdgcn_readlane(own_sum - own_tiles, i)) * DEC_KEYS, n = __builtin_amdgcn_readlane(own_keys, i);
+            next_of = i;
+            next_keys = min(n - k0, DEC_KEYS);
+            lk.load(HeadRows{P.sk + (s0 + i) * P.sk_seq + kvh * P.sk_head, P.sk_tok}, k0, n, P.D, sk_off);
+            lv.load(HeadRows{P.sv + (s0 + i) * P.sv_seq + kvh * P.sv_head, P.sv_tok}, k0, n, P.D, sv_off);
+        }
+    };
+    f32x16 acc[DP / 32] = {};
+    float m = -INFINITY, l = 0.0f;
+    const float c = P.scale_log2;
+    if (t_first < t_end) load(t_first);
+    for (int t = t_first; t < t_end; t += ATT_WAVES) {
+        const int keys = next_keys;
+        const bool sees = next_of < 0 || member == next_of;
+        // a wavefront's LDS operations are done in order: its last tile has been read
+        lk.store(tk, lane);
+        lv.store(tv, lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (t + ATT_WAVES < t_end) load(t + ATT_WAVES);
+        f32x16 s = {};
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d)
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, 0, d, lane), qf[d], s, 0, 0, 0);
+        if (keys < DEC_KEYS) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + 4 * h + (i & 3) >= keys) s[i] = -INFINITY;
+        }
+        float top = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+        top = sees ? halves_max(top) : -INFINITY;
+        if (__ballot((top - m) * c > 8.0f || (m == -INFINITY && top != -INFINITY)) != 0) {
+            const float now = fmaxf(m, top), scale = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - now) * c);
+            l *= scale;
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[db][i] *= scale;
+            m = now;
+        }
+        const float mc = m == -INFINITY ? 0.0f : m * c;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[i] = sees ? __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc)) : 0.0f;
+            l += s[i];
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const bf16x8 p = pack_frag(s, k);
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tv, k * 16, db, lane), p, acc[db], 0, 0, 0);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    // join the wavefronts: [column][row] of each where its tiles were
+    l = halves_sum(l);
+    float* mine = reinterpret_cast<float*>(tk);
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mine[(db * 32 + 8 * (i >> 2) + 4 * h + (i & 3)) * 32 + r] = acc[db][i];
+    if (h == 0) {
+        stat[wave][0][r] = m;
+        stat[wave][1][r] = l;
+    }
+    __syncthreads();
+    constexpr int PER = DP / 8;                          // columns of a thread: eight threads a row
+    const int jr = tid & 31, jd = (tid >> 5) * PER;
+    if (jr >= rows) return;
+    float top = -INFINITY, w[ATT_WAVES], sum = 0.0f, o[PER];
+#pragma unroll
+    for (int i = 0; i < ATT_WAVES; ++i) top = fmaxf(top, stat[i][0][jr]);
+#pragma unroll
+    for (int i = 0; i < ATT_WAVES; ++i) {
+        w[i] = stat[i][0][jr] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((stat[i][0][jr] - top) * c);
+        sum += w[i] * stat[i][1][jr];
+    }
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        o[j] = 0.0f;
+#pragma unroll
+        for (int i = 0; i < ATT_WAVES; ++i) o[j] = fmaf(w[i], reinterpret_cast<const float*>(smem + i * 2 * TILE)[(jd + j) * 32 + jr], o[j]);
+    }
+    const int seq = s0 + jr / heads, hq = kvh * g + hb * 32 + jr % heads;
+    if (P.splits > 1) {
+        const int64_t at = ((int64_t)seq * P.Hq + hq) * P.splits + z;
+        if (jd == 0) {
+            P.stat[2 * at] = top;
+            P.stat[2 * at + 1] = sum;
+        }
+#pragma unroll
+        for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(P.part + at * DP + jd + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
+        return;
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;   // a row that sees no key is zero
+    bf16_t* out = P.out + (int64_t)seq * P.o_tok + hq * P.o_head;
+#pragma unroll
+    for (int j = 0; j < PER; j += 8)
+        if (jd + j < P.D) {
+            u32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = pack_bf16x2(o[j + 2 * i] * inv, o[j + 2 * i + 1] * inv);
+            *reinterpret_cast<u32x4*>(out + jd + j) = v;
+        }
+}
+
+// The parts of a row: a wavefront a row, a lane a part's statistics and then DP / 64 columns
+template <int DP>
+__global__ __launch_bounds__(ATT_THREADS) void attn_join_kernel(const AttnDecodeArgs P) {
+    const int lane = threadIdx.x & 63;
+    const int64_t row = (int64_t)blockIdx.x * ATT_WAVES + (threadIdx.x >> 6);
+    if (row >= (int64_t)P.n_seq * P.Hq) return;
+    constexpr int V = DP / 64;
+    float m = -INFINITY, l = 0.0f;
+    if (lane < P.splits) {
+        m = P.stat[2 * (row * P.splits + lane)];
+        l = P.stat[2 * (row * P.splits + lane) + 1];
+    }
+    float top = m;
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    const float w = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * P.scale_log2);
+    const float sum = wave_sum(w * l);
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    float o[V] = {};
+    const float* part = P.part + row * P.splits * DP + lane * V;
+    for (int i0 = 0; i0 < P.splits; i0 += 8) {           // eight parts' loads under way; past the last one, the last again, unused
+        float x[8][V];
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int j = 0; j < V; ++j) x[u][j] = part[(int64_t)min(i0 + u, P.splits - 1) * DP + j];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            if (i0 + u >= P.splits) break;
+            const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i0 + u));
+#pragma unroll
+            for (int j = 0; j < V; ++j) o[j] = fmaf(wi, x[u][j], o[j]);
+        }
+    }
+    if (lane * V >= P.D) return;
+    bf16_t* out = P.out + row / P.Hq * P.o_tok + row % P.Hq * P.o_head + lane * V;
+    if constexpr (V == 2) *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(o[0] * inv, o[1] * inv);
+    else *out = f32_to_bf16(o[0] * inv);
+}
+
+namespace {
+int64_t decode_blocks(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv) {
+    const int64_t g = Hq / Hkv, members = g >= 32 ? 1 : 32 / g;
+    // the sum of ceil(n / members) over the groups and the sequences of none
+    return std::min(n_seq, n_seq / members + n_groups + 1) * Hkv * ((g + 31) / 32);
+}
+}  // namespace
+
+int attn_padded_columns(int D) { return D <= 64 ? 64 : 128; }
+
+// As many parts as give every compute unit two workgroups, but none of fewer than 4 tiles a wavefront of the longest list that
+// the bounds allow on average
+int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t Tp, int64_t cap, int ncu) {
+    if (n_seq <= 0) return 1;
+    const int64_t g = Hq / Hkv, members = g >= 32 ? 1 : 32 / g;
+    const int64_t blocks = std::max<int64_t>(std::max(n_groups, (n_seq + members - 1) / members), 1) * Hkv * ((g + 31) / 32);
+    const int64_t shared = std::max<int64_t>(1, std::min(members, n_groups > 0 ? n_seq / n_groups : members));
+    const int64_t keys = (n_groups > 0 ? Tp / n_groups : 0) + shared * cap;
+    const int64_t want = (2 * (int64_t)ncu + blocks - 1) / blocks, most = keys / (DEC_KEYS * ATT_WAVES * 2);
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), DEC_MAX_SPLITS));
+}
+
+hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s) {
+    const dim3 grid((uint32_t)decode_blocks(a.n_seq, a.n_groups, a.Hq, a.Hkv), (uint32_t)a.splits);
+    if (a.D <= 64) attn_decode_kernel<64><<<grid, ATT_THREADS, 0, s>>>(a);
+    else attn_decode_kernel<128><<<grid, ATT_THREADS, 0, s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    const uint32_t wgs = (uint32_t)(((int64_t)a.n_seq * a.Hq + ATT_WAVES - 1) / ATT_WAVES);
+    if (a.D <= 64) attn_join_kernel<64><<<wgs, ATT_THREADS, 0, s>>>(a);
+    else attn_join_kernel<128><<<wgs, ATT_THREADS, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace skipffn

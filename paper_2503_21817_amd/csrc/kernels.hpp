@@ -187,6 +187,22 @@ struct AttnGrads {
     int64_t dq_head, dk_head, dv_head;
     float* delta;                                 // [Hq][Tq]
 };
+// One query a sequence.  Group i has the sequences group_off[i] .. group_off[i + 1]) and the prefix rows prefix_seg[i] ..; sequences
+// from group_off[n_groups] on have no prefix.  Own rows: element (sequence, t, h, d) at sk[sequence * sk_seq + t * sk_tok + h * sk_head + d].
+constexpr int DEC_MAX_SPLITS = 64;
+struct AttnDecodeArgs {
+    int n_seq, n_groups, Hq, Hkv, D, Tp, cap, splits;
+    float scale_log2;
+    const bf16_t* q; bf16_t* out; int q_tok, o_tok; int64_t q_head, o_head;
+    const bf16_t* pk; const bf16_t* pv; int pk_tok, pv_tok; int64_t pk_head, pv_head;
+    const bf16_t* sk; const bf16_t* sv; int sk_tok, sv_tok; int64_t sk_head, sv_head, sk_seq, sv_seq;
+    const int32_t* prefix_seg; const int32_t* group_off; const int32_t* suffix_len;
+    float* part; float* stat;                     // splits > 1: [n_seq][Hq][splits][columns], [n_seq][Hq][splits][2]
+};
+// parts that the keys of a sequence are cut into
+int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t Tp, int64_t cap, int ncu);
+int attn_padded_columns(int D);                   // columns of a row of part
+hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s);
 hipError_t launch_attn_forward(const AttnArgs& a, hipStream_t s);
 hipError_t launch_attn_backward(const AttnArgs& a, const AttnGrads& g, hipStream_t s);
 
