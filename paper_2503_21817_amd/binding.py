@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import (POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_int32, c_int64,
+from ctypes import (POINTER, addressof, c_char_p, c_double, c_float, c_int, c_int32, c_int64,
                     c_size_t, c_uint32, c_void_p)
 
 import torch
@@ -25,11 +25,6 @@ FLAG_BALANCED_SPLIT = 0x8
 FLAG_VALIDATE_IDX = 0x10
 
 OK, EINVAL, ESHAPE, EWORKSPACE, EHIP, EUNSUPPORTED, EIDX = range(7)
-
-class Heads(Structure):
-    """skipffn_heads: where element (token, head, column) of a bf16 tensor lies."""
-    _fields_ = [("data", c_void_p), ("token_stride", c_int64), ("head_stride", c_int64)]
-
 
 # every symbol include/skipffn.h declares: (restype, argtypes)
 _SIGNATURES = {
@@ -69,14 +64,14 @@ _SIGNATURES = {
                                              c_void_p, c_void_p]),
     "skipffn_attn_saved_bytes": (c_size_t, [c_int64, c_int64]),
     "skipffn_attn_forward_workspace_bytes": (c_size_t, [c_int64] * 6),
-    "skipffn_attn_forward": (c_int, [c_int64] * 6 + [POINTER(Heads)] * 4 + [c_void_p, c_void_p, c_int, c_float, c_void_p, c_void_p,
+    "skipffn_attn_forward": (c_int, [c_int64] * 6 + [c_void_p] * 4 + [c_void_p, c_void_p, c_int, c_float, c_void_p, c_void_p,
                                                                            c_size_t, c_void_p]),
     "skipffn_attn_backward_workspace_bytes": (c_size_t, [c_int64] * 6),
-    "skipffn_attn_backward": (c_int, [c_int64] * 6 + [POINTER(Heads)] * 5 + [c_void_p, c_void_p, c_int, c_float, c_void_p] +
-                              [POINTER(Heads)] * 3 + [c_void_p, c_size_t, c_void_p]),
+    "skipffn_attn_backward": (c_int, [c_int64] * 6 + [c_void_p] * 5 + [c_void_p, c_void_p, c_int, c_float, c_void_p] +
+                              [c_void_p] * 3 + [c_void_p, c_size_t, c_void_p]),
     "skipffn_attn_decode_workspace_bytes": (c_size_t, [c_int64] * 7),
-    "skipffn_attn_decode": (c_int, [c_int64] * 7 + [POINTER(Heads)] * 3 + [c_void_p] * 2 + [POINTER(Heads)] * 2 + [c_int64] * 2 +
-                            [c_void_p, POINTER(Heads), c_float, c_void_p, c_size_t, c_void_p]),
+    "skipffn_attn_decode": (c_int, [c_int64] * 7 + [c_void_p] * 3 + [c_void_p] * 2 + [c_void_p] * 2 + [c_int64] * 2 +
+                            [c_void_p, c_void_p, c_float, c_void_p, c_size_t, c_void_p]),
     "skipffn_probe_mfma": (c_int, [c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p]),
     "skipffn_saved_layout": (c_int, [c_int64, c_int64, c_int64, POINTER(c_size_t)]),
     "skipffn_status_string": (c_char_p, [c_int]),
@@ -129,7 +124,8 @@ def _ptr(t):
 
 
 def _stream():
-    return c_void_p(torch.cuda.current_stream().cuda_stream)
+    # the handle that torch.cuda.current_stream().cuda_stream wraps, without the objects around it: 0.3 us for 2
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 def _rargs(R, num_retained):
@@ -305,21 +301,44 @@ def skipffn_token_merge_backward(grad_out, seg, assign, grad_x):
            "skipffn_token_merge_backward")
 
 
-def _stride(t, i):
-    return t.stride(i) if t.shape[i] > 1 else 0
+def _device(t, where):
+    """The device of the call's tensors, which has to be the current one: its stream is what the library works on."""
+    d = t.get_device()
+    if d < 0 or d != torch.cuda.current_device():
+        raise ValueError(f"{where}: tensors on the current GPU are wanted")
+    return d
 
 
-def _heads(t, where):
-    """A tensor [tokens, heads, columns] whose columns lie together, as the library takes it."""
-    if t.dim() != 3 or t.dtype != torch.bfloat16 or (t.stride(2) != 1 and t.shape[2] > 1):
-        raise ValueError(f"{where}: a bfloat16 tensor [tokens, heads, columns] with contiguous columns is wanted")
-    return byref(Heads(t.data_ptr(), _stride(t, 0), _stride(t, 1)))
+def _heads(where, device, *tensors):
+    """What the library takes as skipffn_heads of tensors [tokens, heads, columns] whose columns lie together: the array that
+    holds them, and the address of each."""
+    v = []
+    for t, shape in tensors:
+        s, n = t.stride(), t.shape
+        if n != shape or t.dtype != torch.bfloat16 or t.get_device() != device or (s[2] != 1 and n[2] > 1):
+            raise ValueError(f"{where}: a bfloat16 tensor {tuple(shape)} on the device of the call, with contiguous columns, is wanted")
+        # a stride that nothing is apart by is whatever the tensor was cut from
+        v += (t.data_ptr(), s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0)
+    a = (c_int64 * len(v))(*v)
+    at = addressof(a)
+    return a, [at + 24 * i for i in range(len(tensors))]
 
 
-def _same(where, *pairs):
-    for got, want in pairs:
-        if tuple(got) != tuple(want):
-            raise ValueError(f"{where}: a tensor of shape {tuple(want)} is wanted, got {tuple(got)}")
+def _ints(t, n, where, device):
+    """Address of a contiguous int32 tensor of n values on the device."""
+    if t.dtype != torch.int32 or t.numel() != n or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{where}: a contiguous int32 tensor of {n} values on the device of the call is wanted")
+    return t.data_ptr()
+
+
+def _buffer(t, least, where, device):
+    """(address, bytes) of a workspace or a saved buffer, or of none."""
+    if t is None:
+        return None, 0
+    n = t.numel() * t.element_size()
+    if n < least or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{where}: a contiguous buffer of at least {least} bytes on the device of the call is wanted")
+    return t.data_ptr(), n
 
 
 def skipffn_attn_saved_bytes(Tq, Hq) -> int:
@@ -334,28 +353,20 @@ def skipffn_attn_backward_workspace_bytes(Tq, Tk, n_seq, Hq, Hkv, D) -> int:
     return lib().skipffn_attn_backward_workspace_bytes(Tq, Tk, n_seq, Hq, Hkv, D)
 
 
-def _attn_sizes(q, k, v, seg_q, seg_k, saved, where):
-    """(Tq, Tk, n_seq, Hq, Hkv, D); the library sees pointers, so what they hold is checked here."""
-    Tq, Hq, D = q.shape
-    Tk, Hkv = k.shape[:2]
-    _same(where, (k.shape, (Tk, Hkv, D)), (v.shape, (Tk, Hkv, D)))
-    for seg in (seg_q, seg_k):
-        if seg is not None and (seg.dtype != torch.int32 or not seg.is_contiguous() or seg.numel() != seg_q.numel() or seg.numel() < 1):
-            raise ValueError(f"{where}: seg_q and seg_k are contiguous int32 tensors of n_seq + 1 offsets")
-    if saved is not None and _nbytes(saved) < lib().skipffn_attn_saved_bytes(Tq, Hq):
-        raise ValueError(f"{where}: saved holds less than skipffn_attn_saved_bytes({Tq}, {Hq})")
-    return Tq, Tk, seg_q.numel() - 1, Hq, Hkv, D
-
-
 def skipffn_attn_forward(q, k, v, out, seg_q, seg_k=None, *, causal=True, scale=None, saved=None, workspace=None):
     """q, out bf16 [Tq, Hq, D]; k, v bf16 [Tk, Hkv, D] (any token and head strides); seg_q, seg_k i32 [n_seq + 1].
     scale: None is 1 / sqrt(D)."""
     where = "skipffn_attn_forward"
-    sizes = _attn_sizes(q, k, v, seg_q, seg_k, saved, where)
-    _same(where, (out.shape, q.shape))
-    _check(lib().skipffn_attn_forward(*sizes, _heads(q, where), _heads(k, where), _heads(v, where), _heads(out, where), _ptr(seg_q),
-                                      _ptr(seg_k), int(bool(causal)), sizes[-1] ** -0.5 if scale is None else scale, _ptr(saved),
-                                      _ptr(workspace), _nbytes(workspace), _stream()), where)
+    dev = _device(q, where)
+    (Tq, Hq, D), (Tk, Hkv, _) = q.shape, k.shape
+    kv = (Tk, Hkv, D)
+    hold, (hq, hk, hv, ho) = _heads(where, dev, (q, q.shape), (k, kv), (v, kv), (out, q.shape))
+    n1 = seg_q.numel()
+    ws, ws_bytes = _buffer(workspace, 0, where, dev)
+    sv = None if saved is None else _buffer(saved, Tq * Hq * 4, where, dev)[0]
+    _check(lib().skipffn_attn_forward(Tq, Tk, n1 - 1, Hq, Hkv, D, hq, hk, hv, ho, _ints(seg_q, n1, where, dev),
+                                      None if seg_k is None else _ints(seg_k, n1, where, dev), 1 if causal else 0,
+                                      D ** -0.5 if scale is None else scale, sv, ws, ws_bytes, _stream()), where)
 
 
 def skipffn_attn_backward(q, k, v, out, grad_out, seg_q, seg_k, saved, grad_q, grad_k, grad_v, *, causal=True, scale=None,
@@ -363,13 +374,17 @@ def skipffn_attn_backward(q, k, v, out, grad_out, seg_q, seg_k, saved, grad_q, g
     """out and saved from the forward call with the same q, k, v, seg_q, seg_k, causal and scale; grad_out and grad_q as q,
     grad_k and grad_v as k."""
     where = "skipffn_attn_backward"
-    sizes = _attn_sizes(q, k, v, seg_q, seg_k, saved, where)
-    _same(where, *((t.shape, q.shape) for t in (out, grad_out, grad_q)), *((t.shape, k.shape) for t in (grad_k, grad_v)))
-    _check(lib().skipffn_attn_backward(*sizes, _heads(q, where), _heads(k, where), _heads(v, where), _heads(out, where),
-                                       _heads(grad_out, where), _ptr(seg_q), _ptr(seg_k), int(bool(causal)),
-                                       sizes[-1] ** -0.5 if scale is None else scale, _ptr(saved), _heads(grad_q, where),
-                                       _heads(grad_k, where), _heads(grad_v, where), _ptr(workspace), _nbytes(workspace), _stream()),
-           where)
+    dev = _device(q, where)
+    (Tq, Hq, D), (Tk, Hkv, _) = q.shape, k.shape
+    qs, kv = q.shape, (Tk, Hkv, D)
+    hold, (hq, hk, hv, ho, hg, gq, gk, gv) = _heads(where, dev, (q, qs), (k, kv), (v, kv), (out, qs), (grad_out, qs), (grad_q, qs),
+                                                    (grad_k, kv), (grad_v, kv))
+    n1 = seg_q.numel()
+    ws, ws_bytes = _buffer(workspace, 0, where, dev)
+    _check(lib().skipffn_attn_backward(Tq, Tk, n1 - 1, Hq, Hkv, D, hq, hk, hv, ho, hg, _ints(seg_q, n1, where, dev),
+                                       None if seg_k is None else _ints(seg_k, n1, where, dev), 1 if causal else 0,
+                                       D ** -0.5 if scale is None else scale, _buffer(saved, Tq * Hq * 4, where, dev)[0], gq, gk, gv,
+                                       ws, ws_bytes, _stream()), where)
 
 
 def skipffn_attn_decode_workspace_bytes(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity) -> int:
@@ -382,29 +397,32 @@ def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, 
     four None; suffix_k, suffix_v bf16 [n_seq, capacity, Hkv, D] with suffix_len i32 [n_seq], or all three None.
     scale: None is 1 / sqrt(D)."""
     where = "skipffn_attn_decode"
+    dev = _device(q, where)
     n_seq, Hq, D = q.shape
     if prefix_k is None and suffix_k is None:
         raise ValueError(f"{where}: a prefix or own rows are wanted")
     Hkv = (suffix_k if prefix_k is None else prefix_k).shape[-2]
     Tp = n_groups = cap = seq_k = seq_v = 0
-    pk = pv = sk = sv = None
-    for t in (prefix_seg, group_off, suffix_len):
-        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
-            raise ValueError(f"{where}: offsets and lengths are contiguous int32 tensors")
-    _same(where, (out.shape, q.shape))
+    seg = off = lens = None
+    given = [(q, q.shape), (out, q.shape)]
     if prefix_k is not None:
         Tp, n_groups = prefix_k.shape[0], group_off.numel() - 1
-        _same(where, (prefix_k.shape, (Tp, Hkv, D)), (prefix_v.shape, (Tp, Hkv, D)), (prefix_seg.shape, (n_groups + 1,)))
-        pk, pv = _heads(prefix_k, where), _heads(prefix_v, where)
-    if suffix_k is not None:
+        seg, off = _ints(prefix_seg, n_groups + 1, where, dev), _ints(group_off, n_groups + 1, where, dev)
+        given += [(prefix_k, (Tp, Hkv, D)), (prefix_v, (Tp, Hkv, D))]
+    if suffix_k is not None and n_seq > 0:
         cap = suffix_k.shape[1]
-        _same(where, (suffix_k.shape, (n_seq, cap, Hkv, D)), (suffix_v.shape, (n_seq, cap, Hkv, D)), (suffix_len.shape, (n_seq,)))
-        seq_k, seq_v = _stride(suffix_k, 0), _stride(suffix_v, 0)
-        if n_seq > 0:
-            sk, sv = _heads(suffix_k[0], where), _heads(suffix_v[0], where)
-    _check(lib().skipffn_attn_decode(n_seq, n_groups, Hq, Hkv, D, Tp, cap, _heads(q, where), pk, pv, _ptr(prefix_seg), _ptr(group_off),
-                                     sk, sv, seq_k, seq_v, _ptr(suffix_len), _heads(out, where), D ** -0.5 if scale is None else scale,
-                                     _ptr(workspace), _nbytes(workspace), _stream()), where)
+        if suffix_k.shape != (n_seq, cap, Hkv, D) or suffix_v.shape != suffix_k.shape:
+            raise ValueError(f"{where}: own rows are tensors [{n_seq}, capacity, {Hkv}, {D}]")
+        lens = _ints(suffix_len, n_seq, where, dev)
+        if n_seq > 1:
+            seq_k, seq_v = suffix_k.stride(0), suffix_v.stride(0)
+        given += [(suffix_k[0], (cap, Hkv, D)), (suffix_v[0], (cap, Hkv, D))]
+    hold, at = _heads(where, dev, *given)
+    pk, pv = at[2:4] if prefix_k is not None else (None, None)
+    sk, sv = at[-2:] if suffix_k is not None and n_seq > 0 else (None, None)
+    ws, ws_bytes = _buffer(workspace, 0, where, dev)
+    _check(lib().skipffn_attn_decode(n_seq, n_groups, Hq, Hkv, D, Tp, cap, at[0], pk, pv, seg, off, sk, sv, seq_k, seq_v, lens, at[1],
+                                     D ** -0.5 if scale is None else scale, ws, ws_bytes, _stream()), where)
 
 
 def skipffn_probe_mfma(blocks, iters, random_operands, out, clocks):

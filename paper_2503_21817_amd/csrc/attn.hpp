@@ -67,20 +67,30 @@ struct TileLoad {
     }
 };
 
-// Operand with the contraction along the columns: lane l holds row row0 + l % 32 and columns 16 c + 8 (l / 32) .. + 7
+// Operands from a tile at LDS address `tile` (a multiple of a row's bytes), in 32-bit LDS addresses: the lane's part of an address is
+// added once a tile, the chunk then an exclusive or and the rows an immediate offset, so that no register holds an address a chunk.
+//
+// With the contraction along the columns: lane l holds row row0 + l % 32 and columns 16 c + 8 (l / 32) .. + 7; row0 % 32 == 0
+typedef __attribute__((address_space(3))) const bf16x8* lds_bf16x8_ptr;
 template <int DP>
-__device__ __forceinline__ bf16x8 frag_rows(const char* tile, int row0, int c, int lane) {
-    return *reinterpret_cast<const bf16x8*>(tile + tile_off<DP>(row0 + (lane & 31), 2 * c + (lane >> 5)));
+__device__ __forceinline__ uint32_t rows_lane(int lane) { return tile_off<DP>(lane & 31, lane >> 5); }
+template <int DP>
+__device__ __forceinline__ bf16x8 frag_rows(uint32_t at, int row0, int c) {
+    return *(lds_bf16x8_ptr)(uintptr_t)((at ^ (uint32_t)(c << 5)) + (uint32_t)(row0 * tile_row_bytes<DP>()));
 }
-// Operand with the contraction along the tokens: lane l holds column 32 db + l % 32 of the tokens row0 + 4 (l / 32) .. + 3 and
-// row0 + 8 + 4 (l / 32) .. + 3, the order in which the result of a product lies in registers 8 k .. 8 k + 7
+// With the contraction along the tokens: lane l holds column 32 db + l % 32 of the tokens row0 + 4 (l / 32) .. + 3 and
+// row0 + 8 + 4 (l / 32) .. + 3, the order in which the result of a product lies in registers 8 k .. 8 k + 7; row0 % 16 == 0
 template <int DP>
-__device__ __forceinline__ bf16x8 frag_cols(char* tile, int row0, int db, int lane) {
-    const int r = row0 + 4 * (lane >> 5) + ((lane & 15) >> 2);
-    const int chunk = 4 * db + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), half = (lane & 1) * 8;
-    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr)(tile + tile_off<DP>(r, chunk) + half));
-    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr)(tile + tile_off<DP>(r + 8, chunk) + half));
-    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+__device__ __forceinline__ uint32_t cols_lane(int lane) {
+    return tile_off<DP>(4 * (lane >> 5) + ((lane & 15) >> 2), 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) + (uint32_t)(lane & 1) * 8u;
+}
+template <int DP>
+__device__ __forceinline__ bf16x8 frag_cols(uint32_t at, int row0, int db) {
+    const uint32_t lo = (at ^ (uint32_t)(db << 6)) + (uint32_t)(row0 * tile_row_bytes<DP>());
+    const uint32_t hi = (at ^ (uint32_t)(db << 6 | 32)) + (uint32_t)((row0 + 8) * tile_row_bytes<DP>());   // 8 rows on: tile_swz differs by 2
+    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr)(uintptr_t)lo);
+    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4_ptr)(uintptr_t)hi);
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 // registers 8 k .. 8 k + 7 of a product, rounded to bf16, as the operand that frag_cols goes with
 __device__ __forceinline__ bf16x8 pack_frag(const f32x16& p, int k) {
@@ -125,6 +135,29 @@ __device__ __forceinline__ void store_cols(bf16_t* row, const f32x16 (&acc)[DP /
         }
 }
 
+// The same for the 32 rows of a wavefront, by way of LDS (32 rows of a tile): rows leave in whole 256 (128) bytes instead of pieces of 8
+template <int DP>
+__device__ __forceinline__ void store_rows(bf16_t* base, int stride, int rows, const f32x16 (&acc)[DP / 32], float scale, int D, int lane, char* lds) {
+    constexpr int CH = tile_row_bytes<DP>() / 16;
+    const int r = lane & 31, h = lane >> 5;
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const u32x2 w = {pack_bf16x2(acc[db][4 * i] * scale, acc[db][4 * i + 1] * scale),
+                             pack_bf16x2(acc[db][4 * i + 2] * scale, acc[db][4 * i + 3] * scale)};
+            *reinterpret_cast<u32x2*>(lds + tile_off<DP>(r, db * 4 + i) + 8 * h) = w;
+        }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const int c = lane % CH;
+#pragma unroll
+    for (int i = 0; i < 32 * CH / 64; ++i) {
+        const int row = lane / CH + i * (64 / CH);
+        const u32x4 v = *reinterpret_cast<const u32x4*>(lds + tile_off<DP>(row, c));
+        if (row < rows && c * 8 < D) *reinterpret_cast<u32x4*>(base + (int64_t)row * stride + c * 8) = v;
+    }
+}
+
 // ---- which sequence a workgroup works on ---------------------------------------------------------------
 // Set s has items(its length) workgroups; workgroup q of all -> s, its index among the set's, and the set's bounds, which
 // bounds(s, b, e) gives.  False past the last one.  A lane takes a set, a prefix sum over the lanes finds the workgroup's (whole
@@ -151,10 +184,76 @@ __device__ __forceinline__ bool locate_in(int S, int q, const Bounds& bounds, co
     }
     return false;
 }
-template <class Items>
-__device__ __forceinline__ bool locate_item(const int32_t* __restrict__ seg, int S, int n_tok, int q, const Items& items,
-                                            int& s, int& item, int& t0, int& t1) {
-    return locate_in(S, q, [&](int i, int& b, int& e) { seg_bounds(seg, i, n_tok, b, e); }, items, s, item, t0, t1);
+// The workgroups of a kernel over packed sequences, the longest first whatever sequence they belong to: the last ones to start are
+// the shortest, and the chip empties evenly.  Workgroup j of a sequence has the level top - j num / den (rounded down), in
+// 32s of rows that it goes over (num = 0: all the same), so that cnt(L) = ceil((top - L + 1) den / num) of a sequence's have at least L; a search over L finds
+// the level of workgroup q, a prefix sum its sequence.  For up to 64 sequences, a lane each; with more of them (each then a small
+// part of the whole) workgroups go sequence by sequence.  rows(lengths of a sequence) gives its workgroups and top.
+struct SeqItem { int seq, item, q0, q1, k0, k1; };
+template <class Rows>
+__device__ __forceinline__ bool locate_longest(const AttnArgs& P, int q, int num, int den, const Rows& rows, SeqItem& it) {
+    const int lane = threadIdx.x & 63;
+    if (P.n_seq > 64) {
+        int cc = 0;
+        for (int i0 = 0; i0 < P.n_seq; i0 += 64) {
+            int qb = 0, qe = 0, kb = 0, ke = 0, n = 0, top = 0;
+            if (i0 + lane < P.n_seq) {
+                seg_bounds(P.seg_q, i0 + lane, P.Tq, qb, qe);
+                seg_bounds(P.seg_k, i0 + lane, P.Tk, kb, ke);
+                rows(qe - qb, ke - kb, n, top);
+            }
+            const int incl = wave_inclusive_sum(n);
+            const uint64_t past = __ballot(q < cc + incl);
+            if (past != 0) {
+                const int l = __builtin_ctzll(past);
+                it = {i0 + l, q - cc - __builtin_amdgcn_readlane(incl - n, l), __builtin_amdgcn_readlane(qb, l), __builtin_amdgcn_readlane(qe, l),
+                      __builtin_amdgcn_readlane(kb, l), __builtin_amdgcn_readlane(ke, l)};
+                return true;
+            }
+            cc += __builtin_amdgcn_readlane(incl, 63);
+        }
+        return false;
+    }
+    int qb = 0, qe = 0, kb = 0, ke = 0, n = 0, top = 0;
+    if (lane < P.n_seq) {
+        seg_bounds(P.seg_q, lane, P.Tq, qb, qe);
+        seg_bounds(P.seg_k, lane, P.Tk, kb, ke);
+        rows(qe - qb, ke - kb, n, top);
+    }
+    auto at_least = [&](int L) { const int c = top < L ? 0 : num == 0 ? n : ((top - L + 1) * den + num - 1) / num; return c < n ? c : n; };
+    int l = 0, item = q, sum = wave_inclusive_sum(n);
+    if (q >= __builtin_amdgcn_readlane(sum, 63)) return false;
+    if (P.n_seq > 1) {
+        // levels of all workgroups lie in (lo, hi]; workgroup q's is the largest L whose workgroups of at least L are more than q
+        int hi = n > 0 ? top : -(1 << 30), lo = n > 0 ? top - ((n - 1) * num) / den - 1 : 1 << 30;
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) {
+            hi = max(hi, __shfl_xor(hi, off, 64));
+            lo = min(lo, __shfl_xor(lo, off, 64));
+        }
+        hi = __builtin_amdgcn_readfirstlane(hi) + 1;             // none has it
+        lo = __builtin_amdgcn_readfirstlane(lo) + 1;             // all have it
+        while (hi - lo > 1) {
+            const int mid = lo + ((hi - lo) >> 1);
+            if (__builtin_amdgcn_readlane(wave_inclusive_sum(at_least(mid)), 63) > q) lo = mid;
+            else hi = mid;
+        }
+        const int before = at_least(lo + 1), here = at_least(lo) - before;
+        const int r = q - __builtin_amdgcn_readlane(wave_inclusive_sum(before), 63);
+        const int incl = wave_inclusive_sum(here);
+        l = __builtin_ctzll(__ballot(r < incl));
+        item = r - __builtin_amdgcn_readlane(incl - here, l) + __builtin_amdgcn_readlane(before, l);
+    }
+    it = {l, item, __builtin_amdgcn_readlane(qb, l), __builtin_amdgcn_readlane(qe, l), __builtin_amdgcn_readlane(kb, l), __builtin_amdgcn_readlane(ke, l)};
+    return true;
+}
+// workgroup of a kernel by queries: four units of 32 rows of a head, g heads a block of rows, from a sequence's end
+__device__ __forceinline__ bool locate_queries(const AttnArgs& P, int q, int g, SeqItem& it) {
+    return locate_longest(P, q, P.causal ? ATT_WAVES : 0, g,
+                          [&](int nq, int nk, int& n, int& top) {
+                              n = ((nq + ATT_ROWS - 1) / ATT_ROWS * g + ATT_WAVES - 1) / ATT_WAVES;
+                              top = (nk + 31) / 32;
+                          }, it);
 }
 
 // Workgroups of a kernel by queries: at least what the sequences take, whatever their lengths (the sum of ceil(ceil(n / 32) g / 4))

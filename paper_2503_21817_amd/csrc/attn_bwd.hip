@@ -15,14 +15,12 @@ constexpr int DQ_KEYS = 64;
 template <int DP>
 __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs P, const AttnGrads G) {
     constexpr int TILE = DQ_KEYS * tile_row_bytes<DP>();
-    __shared__ __align__(16) char smem[4 * TILE];
+    __shared__ __align__(256) char smem[4 * TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int kvh = (int)blockIdx.x % P.Hkv, g = P.Hq / P.Hkv;
-    int seq, item, q0, q1, k0, k1;
-    if (!locate_item(P.seg_q, P.n_seq, P.Tq, (int)blockIdx.x / P.Hkv,
-                     [&](int n) { return ((n + ATT_ROWS - 1) / ATT_ROWS * g + ATT_WAVES - 1) / ATT_WAVES; }, seq, item, q0, q1))
-        return;
-    seg_bounds(P.seg_k, seq, P.Tk, k0, k1);
+    SeqItem it;
+    if (!locate_queries(P, (int)blockIdx.x / P.Hkv, g, it)) return;
+    const int item = it.item, q0 = it.q0, q1 = it.q1, k0 = it.k0, k1 = it.k1;
     const int nq = q1 - q0, nk = k1 - k0, ahead = nk - nq;
     const int units = (nq + ATT_ROWS - 1) / ATT_ROWS * g;
     const int first = units - 1 - item * ATT_WAVES, unit = first - wave;
@@ -63,6 +61,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs 
     const HeadRows K{P.k + kvh * P.k_head + (int64_t)k0 * P.k_tok, P.k_tok}, V{P.v + kvh * P.v_head + (int64_t)k0 * P.v_tok, P.v_tok};
     const uint32_t k_off = TileLoad<DP, DQ_KEYS>::first(tid, P.k_tok, P.D), v_off = TileLoad<DP, DQ_KEYS>::first(tid, P.v_tok, P.D);
     TileLoad<DP, DQ_KEYS> lk, lv;
+    const uint32_t rows_at = lds_addr_of(smem) + rows_lane<DP>(lane), cols_at = lds_addr_of(smem) + cols_lane<DP>(lane);
     f32x16 acc[DP / 32] = {};
     const float c = P.scale_log2;
     if (tiles > 0) {
@@ -73,8 +72,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs 
     }
     __syncthreads();
     for (int t = 0; t < tiles; ++t) {
-        char* tk = smem + (t & 1) * 2 * TILE;
-        char* tv = tk + TILE;
+        const uint32_t stage = (uint32_t)(t & 1) * (2 * TILE), tk = rows_at + stage, tv = tk + TILE, tkc = cols_at + stage;
         if (t + 1 < tiles) {
             lk.load(K, (t + 1) * DQ_KEYS, nk, P.D, k_off);
             lv.load(V, (t + 1) * DQ_KEYS, nk, P.D, v_off);
@@ -86,10 +84,10 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs 
             f32x16 s = {}, dp = {};
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d, lane), qf[d], s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d), qf[d], s, 0, 0, 0);
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d)
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tv, kb * 32, d, lane), gf[d], dp, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tv, kb * 32, d), gf[d], dp, 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse)) * (dp[i] - delta);
             if (key0 + 32 > all_see) {
@@ -102,7 +100,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs 
                 const bf16x8 ds = pack_frag(s, k);
 #pragma unroll
                 for (int db = 0; db < DP / 32; ++db)
-                    acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tk, kb * 32 + k * 16, db, lane), ds, acc[db], 0, 0, 0);
+                    acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tkc, kb * 32 + k * 16, db), ds, acc[db], 0, 0, 0);
             }
         }
         if (t + 1 < tiles) {
@@ -121,13 +119,14 @@ constexpr int DKV_KEYS = ATT_WAVES * 32, DKV_ROWS = 32;
 template <int DP>
 __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs P, const AttnGrads G) {
     constexpr int ROWB = tile_row_bytes<DP>(), TILE = DKV_ROWS * ROWB, STAGE = 2 * TILE + 2 * DKV_ROWS * 4;
-    __shared__ __align__(16) char smem[DKV_KEYS * ROWB + 2 * STAGE];
+    __shared__ __align__(256) char smem[DKV_KEYS * ROWB + 2 * STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int kvh = (int)blockIdx.x % P.Hkv, g = P.Hq / P.Hkv;
-    int seq, item, q0, q1, k0, k1;
-    if (!locate_item(P.seg_k, P.n_seq, P.Tk, (int)blockIdx.x / P.Hkv, [](int n) { return (n + DKV_KEYS - 1) / DKV_KEYS; }, seq, item, k0, k1))
+    SeqItem it;
+    if (!locate_longest(P, (int)blockIdx.x / P.Hkv, P.causal ? ATT_WAVES : 0, 1,
+                        [](int nq, int nk, int& n, int& top) { n = (nk + DKV_KEYS - 1) / DKV_KEYS; top = (nq + 31) / 32; }, it))
         return;
-    seg_bounds(P.seg_q, seq, P.Tq, q0, q1);
+    const int item = it.item, q0 = it.q0, q1 = it.q1, k0 = it.k0, k1 = it.k1;
     const int nq = q1 - q0, nk = k1 - k0, ahead = nk - nq;
     const int key0 = item * DKV_KEYS + wave * 32, key = key0 + (lane & 31);
     // row i sees key j if j <= i + ahead
@@ -149,7 +148,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
     TileLoad<DP, DKV_ROWS> lq, lg;
     float stat = 0.0f;                                   // thread t < 32: row t's log-sum-exp, t of 32 .. 63: delta
     auto load = [&](int n) {
-        const int head = kvh * g + n / row_tiles, r0 = (row_first + n % row_tiles) * DKV_ROWS;
+        const int head = kvh * g + n % g, r0 = (row_first + row_tiles - 1 - n / g) * DKV_ROWS;
         lq.load(HeadRows{P.q + head * P.q_head + (int64_t)q0 * P.q_tok, P.q_tok}, r0, nq, P.D, q_off);
         lg.load(HeadRows{G.go + head * G.go_head + (int64_t)q0 * G.go_tok, G.go_tok}, r0, nq, P.D, g_off);
         if (tid < 64) {
@@ -164,6 +163,8 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
         lg.store(st + TILE, tid);
         if (tid < 64) reinterpret_cast<float*>(st + 2 * TILE)[tid] = stat;
     };
+    const uint32_t v_at = lds_addr_of(tv) + (uint32_t)(wave * 32 * ROWB) + rows_lane<DP>(lane);
+    const uint32_t rows_at = lds_addr_of(stage) + rows_lane<DP>(lane), cols_at = lds_addr_of(stage) + cols_lane<DP>(lane);
     f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
     const float c = P.scale_log2;
     if (steps > 0) {
@@ -172,22 +173,22 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
     }
     __syncthreads();
     for (int n = 0; n < steps; ++n) {
-        char* tq = stage + (n & 1) * STAGE;
-        char* tg = tq + TILE;
-        const float* st = reinterpret_cast<const float*>(tq + 2 * TILE);
+        const uint32_t at = (uint32_t)(n & 1) * STAGE, tq = rows_at + at, tg = tq + TILE, tqc = cols_at + at, tgc = tqc + TILE;
+        const float* st = reinterpret_cast<const float*>(stage + at + 2 * TILE);
         if (n + 1 < steps) load(n + 1);
-        const int r0 = (row_first + n % row_tiles) * DKV_ROWS;
+        const int r0 = (row_first + row_tiles - 1 - n / g) * DKV_ROWS;
         if (key0 < nk && (!P.causal || key0 <= min(r0 + DKV_ROWS, nq) - 1 + ahead)) {
             f32x16 s = {}, dp = {};
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tq, 0, d, lane), kf[d], s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tq, 0, d), kf[d], s, 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 8 * i + 4 * h);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) s[4 * i + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * i + j], c, -lse[j]));
             }
+            __builtin_amdgcn_sched_barrier(0);
             const bool masked = P.causal && key0 + 31 > r0 + ahead;
             if (masked) {
 #pragma unroll
@@ -199,11 +200,12 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
                 const bf16x8 p = pack_frag(s, k);
 #pragma unroll
                 for (int db = 0; db < DP / 32; ++db)
-                    dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tg, k * 16, db, lane), p, dv[db], 0, 0, 0);
+                    dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tgc, k * 16, db), p, dv[db], 0, 0, 0);
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d)
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tg, 0, d, lane), frag_rows<DP>(tv, wave * 32, d, lane), dp, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tg, 0, d), frag_rows<DP>(v_at, 0, d), dp, 0, 0, 0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const f32x4 delta = *reinterpret_cast<const f32x4*>(st + DKV_ROWS + 8 * i + 4 * h);
@@ -215,12 +217,13 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
                 for (int i = 0; i < 16; ++i)
                     if (key > r0 + 8 * (i >> 2) + 4 * h + (i & 3) + ahead) s[i] = 0.0f;
             }
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const bf16x8 ds = pack_frag(s, k);
 #pragma unroll
                 for (int db = 0; db < DP / 32; ++db)
-                    dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tq, k * 16, db, lane), ds, dk[db], 0, 0, 0);
+                    dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tqc, k * 16, db), ds, dk[db], 0, 0, 0);
             }
         }
         if (n + 1 < steps) store(n + 1);

@@ -17,7 +17,7 @@ template <int DP>
 __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnDecodeArgs P) {
     constexpr int ROWB = tile_row_bytes<DP>(), TILE = DEC_KEYS * ROWB;
     static_assert(2 * TILE >= DP * 32 * 4, "a wavefront's sums fit where its tiles were");
-    __shared__ __align__(16) char smem[ATT_WAVES * 2 * TILE];
+    __shared__ __align__(256) char smem[ATT_WAVES * 2 * TILE];
     __shared__ float stat[ATT_WAVES][2][32];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int g = P.Hq / P.Hkv, members = g >= 32 ? 1 : 32 / g, head_blocks = (g + 31) / 32;
@@ -53,6 +53,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnD
 
     char* tk = smem + wave * 2 * TILE;
     char* tv = tk + TILE;
+    const uint32_t rows_at = lds_addr_of(tk) + rows_lane<DP>(lane), cols_at = lds_addr_of(tv) + cols_lane<DP>(lane);
     typedef TileLoad<DP, DEC_KEYS, 64> Load;
     const uint32_t pk_off = Load::first(lane, P.pk_tok, P.D), pv_off = Load::first(lane, P.pv_tok, P.D);
     const uint32_t sk_off = Load::first(lane, P.sk_tok, P.D), sv_off = Load::first(lane, P.sv_tok, P.D);
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnD
         f32x16 s = {};
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, 0, d, lane), qf[d], s, 0, 0, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(rows_at, 0, d), qf[d], s, 0, 0, 0);
         if (keys < DEC_KEYS) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnD
             const bf16x8 p = pack_frag(s, k);
 #pragma unroll
             for (int db = 0; db < DP / 32; ++db)
-                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tv, k * 16, db, lane), p, acc[db], 0, 0, 0);
+                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(cols_at, k * 16, db), p, acc[db], 0, 0, 0);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }

@@ -14,14 +14,12 @@ constexpr int FWD_KEYS = 64;
 template <int DP>
 __global__ __launch_bounds__(ATT_THREADS, 2) void attn_fwd_kernel(const AttnArgs P) {
     constexpr int TILE = FWD_KEYS * tile_row_bytes<DP>();
-    __shared__ __align__(16) char smem[4 * TILE];
+    __shared__ __align__(256) char smem[4 * TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int kvh = (int)blockIdx.x % P.Hkv, g = P.Hq / P.Hkv;
-    int seq, item, q0, q1, k0, k1;
-    if (!locate_item(P.seg_q, P.n_seq, P.Tq, (int)blockIdx.x / P.Hkv,
-                     [&](int n) { return ((n + ATT_ROWS - 1) / ATT_ROWS * g + ATT_WAVES - 1) / ATT_WAVES; }, seq, item, q0, q1))
-        return;
-    seg_bounds(P.seg_k, seq, P.Tk, k0, k1);
+    SeqItem it;
+    if (!locate_queries(P, (int)blockIdx.x / P.Hkv, g, it)) return;
+    const int item = it.item, q0 = it.q0, q1 = it.q1, k0 = it.k0, k1 = it.k1;
     const int nq = q1 - q0, nk = k1 - k0, ahead = nk - nq;
     const int units = (nq + ATT_ROWS - 1) / ATT_ROWS * g;
     const int first = units - 1 - item * ATT_WAVES, unit = first - wave;          // wave 0 has the latest queries
@@ -43,6 +41,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_fwd_kernel(const AttnArgs
     const HeadRows K{P.k + kvh * P.k_head + (int64_t)k0 * P.k_tok, P.k_tok}, V{P.v + kvh * P.v_head + (int64_t)k0 * P.v_tok, P.v_tok};
     const uint32_t k_off = TileLoad<DP, FWD_KEYS>::first(tid, P.k_tok, P.D), v_off = TileLoad<DP, FWD_KEYS>::first(tid, P.v_tok, P.D);
     TileLoad<DP, FWD_KEYS> lk, lv;
+    const uint32_t rows_at = lds_addr_of(smem) + rows_lane<DP>(lane), cols_at = lds_addr_of(smem) + TILE + cols_lane<DP>(lane);
 
     f32x16 acc[DP / 32] = {};
     float m = -INFINITY, l = 0.0f;
@@ -55,8 +54,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_fwd_kernel(const AttnArgs
     }
     __syncthreads();
     for (int t = 0; t < tiles; ++t) {
-        char* tk = smem + (t & 1) * 2 * TILE;
-        char* tv = tk + TILE;
+        const uint32_t stage = (uint32_t)(t & 1) * (2 * TILE), tk = rows_at + stage, tv = cols_at + stage;
         if (t + 1 < tiles) {
             lk.load(K, (t + 1) * FWD_KEYS, nk, P.D, k_off);
             lv.load(V, (t + 1) * FWD_KEYS, nk, P.D, v_off);
@@ -68,7 +66,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_fwd_kernel(const AttnArgs
                 s[kb] = f32x16{};
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d)
-                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d, lane), qf[d], s[kb], 0, 0, 0);
+                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d), qf[d], s[kb], 0, 0, 0);
             }
             if ((t + 1) * FWD_KEYS > all_see) {
 #pragma unroll
@@ -109,7 +107,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_fwd_kernel(const AttnArgs
                     const bf16x8 p = pack_frag(s[kb], k);
 #pragma unroll
                     for (int db = 0; db < DP / 32; ++db)
-                        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tv, kb * 32 + k * 16, db, lane), p, acc[db], 0, 0, 0);
+                        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tv, kb * 32 + k * 16, db), p, acc[db], 0, 0, 0);
                 }
         }
         if (t + 1 < tiles) {
@@ -120,10 +118,11 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_fwd_kernel(const AttnArgs
         __syncthreads();
     }
     l = halves_sum(l);
-    if (!row_ok) return;
+    if (unit < 0) return;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;          // a row that sees no key is zero
-    store_cols<DP>(P.out + head * P.o_head + (int64_t)(q0 + row) * P.o_tok, acc, inv, P.D, h);
-    if (P.lse != nullptr && h == 0)
+    store_rows<DP>(P.out + head * P.o_head + (int64_t)(q0 + row0) * P.o_tok, P.o_tok, min(nq - row0, ATT_ROWS), acc, inv, P.D, lane,
+                   smem + wave * 32 * tile_row_bytes<DP>());
+    if (P.lse != nullptr && h == 0 && row_ok)
         P.lse[(int64_t)head * P.Tq + q0 + row] = l == 0.0f ? INFINITY : fmaf(m, c, __builtin_amdgcn_logf(l));
 }
 
