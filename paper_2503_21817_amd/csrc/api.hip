@@ -894,7 +894,7 @@ int skipffn_attn_forward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int6
     hipStream_t s = (hipStream_t)stream;
     const AttnArgs a = attn_args(Tq, Tk, n_seq, Hq, Hkv, D, q, k, v, out, seg_q, seg_k, causal, scale, static_cast<float*>(saved));
     profile_mark_begin(KC_ATTN_FWD, s);
-    hipError_t e = launch_attn_forward(a, s);
+    hipError_t e = launch_attn_forward(a, num_cus(), s);
     profile_mark_end(KC_ATTN_FWD, s);
     return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
 }

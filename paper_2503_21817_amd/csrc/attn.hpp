@@ -191,8 +191,7 @@ __device__ __forceinline__ bool locate_in(int S, int q, const Bounds& bounds, co
 // part of the whole) workgroups go sequence by sequence.  rows(lengths of a sequence) gives its workgroups and top.
 struct SeqItem { int seq, item, q0, q1, k0, k1; };
 template <class Rows>
-__device__ __forceinline__ bool locate_longest(const AttnArgs& P, int q, int num, int den, const Rows& rows, SeqItem& it) {
-    const int lane = threadIdx.x & 63;
+__device__ __forceinline__ bool locate_longest(const AttnArgs& P, int lane, int q, int num, int den, const Rows& rows, SeqItem& it) {
     if (P.n_seq > 64) {
         int cc = 0;
         for (int i0 = 0; i0 < P.n_seq; i0 += 64) {
@@ -248,12 +247,46 @@ __device__ __forceinline__ bool locate_longest(const AttnArgs& P, int q, int num
     return true;
 }
 // workgroup of a kernel by queries: four units of 32 rows of a head, g heads a block of rows, from a sequence's end
-__device__ __forceinline__ bool locate_queries(const AttnArgs& P, int q, int g, SeqItem& it) {
-    return locate_longest(P, q, P.causal ? ATT_WAVES : 0, g,
+__device__ __forceinline__ bool locate_queries(const AttnArgs& P, int lane, int q, int g, SeqItem& it) {
+    return locate_longest(P, lane, q, P.causal ? ATT_WAVES : 0, g,
                           [&](int nq, int nk, int& n, int& top) {
                               n = ((nq + ATT_ROWS - 1) / ATT_ROWS * g + ATT_WAVES - 1) / ATT_WAVES;
                               top = (nk + 31) / 32;
                           }, it);
+}
+
+// The same value, which the compiler takes for another one: what is computed from it inside a loop is not kept in registers around the loop
+__device__ __forceinline__ int unhoisted(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// A persistent workgroup's k-th piece of `blocks` pieces of work, the longest first: the order is turned round every other time, so
+// that who had the longest of one round has the shortest of the next; eight neighbours stay eight neighbours (an XCD each).
+__device__ __forceinline__ int piece_of(int k) {
+    const int w = (int)blockIdx.x, n = (int)gridDim.x;
+    return k * n + ((k & 1) && (n & 7) == 0 ? n - 8 - (w & ~7) + (w & 7) : w);
+}
+
+// What a wavefront works on in a kernel by queries: 32 rows of a head
+struct QueryUnit {
+    int head, row0, tiles, wave_end, all_see;            // tiles: of the workgroup; keys that the last row, the first row see
+    bool any;
+};
+template <int KEYS>
+__device__ __forceinline__ QueryUnit query_unit(const AttnArgs& P, const SeqItem& it, int kvh, int wave) {
+    const int g = P.Hq / P.Hkv, nq = it.q1 - it.q0, nk = it.k1 - it.k0;
+    const int units = (nq + ATT_ROWS - 1) / ATT_ROWS * g;
+    const int first = units - 1 - it.item * ATT_WAVES, unit = first - wave;       // wave 0 has the latest queries
+    auto keys_of = [&](int row) { const int n = P.causal ? row + 1 + nk - nq : nk; return n < nk ? n : nk; };   // may be < 0
+    QueryUnit u;
+    u.any = unit >= 0;
+    u.row0 = u.any ? unit / g * ATT_ROWS : 0;
+    u.head = kvh * g + (u.any ? unit % g : 0);
+    u.tiles = (max(keys_of(min(first / g * ATT_ROWS + ATT_ROWS, nq) - 1), 0) + KEYS - 1) / KEYS;
+    u.wave_end = u.any ? keys_of(min(u.row0 + ATT_ROWS, nq) - 1) : 0;
+    u.all_see = keys_of(u.row0);
+    return u;
 }
 
 // Workgroups of a kernel by queries: at least what the sequences take, whatever their lengths (the sum of ceil(ceil(n / 32) g / 4))

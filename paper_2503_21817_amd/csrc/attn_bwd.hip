@@ -19,7 +19,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int kvh = (int)blockIdx.x % P.Hkv, g = P.Hq / P.Hkv;
     SeqItem it;
-    if (!locate_queries(P, (int)blockIdx.x / P.Hkv, g, it)) return;
+    if (!locate_queries(P, lane, (int)blockIdx.x / P.Hkv, g, it)) return;
     const int item = it.item, q0 = it.q0, q1 = it.q1, k0 = it.k0, k1 = it.k1;
     const int nq = q1 - q0, nk = k1 - k0, ahead = nk - nq;
     const int units = (nq + ATT_ROWS - 1) / ATT_ROWS * g;
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int kvh = (int)blockIdx.x % P.Hkv, g = P.Hq / P.Hkv;
     SeqItem it;
-    if (!locate_longest(P, (int)blockIdx.x / P.Hkv, P.causal ? ATT_WAVES : 0, 1,
+    if (!locate_longest(P, lane, (int)blockIdx.x / P.Hkv, P.causal ? ATT_WAVES : 0, 1,
                         [](int nq, int nk, int& n, int& top) { n = (nk + DKV_KEYS - 1) / DKV_KEYS; top = (nq + 31) / 32; }, it))
         return;
     const int item = it.item, q0 = it.q0, q1 = it.q1, k0 = it.k0, k1 = it.k1;
@@ -148,7 +148,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
     TileLoad<DP, DKV_ROWS> lq, lg;
     float stat = 0.0f;                                   // thread t < 32: row t's log-sum-exp, t of 32 .. 63: delta
     auto load = [&](int n) {
-        const int head = kvh * g + n % g, r0 = (row_first + row_tiles - 1 - n / g) * DKV_ROWS;
+        const int head = kvh * g + n / row_tiles, r0 = (row_first + row_tiles - 1 - n % row_tiles) * DKV_ROWS;
         lq.load(HeadRows{P.q + head * P.q_head + (int64_t)q0 * P.q_tok, P.q_tok}, r0, nq, P.D, q_off);
         lg.load(HeadRows{G.go + head * G.go_head + (int64_t)q0 * G.go_tok, G.go_tok}, r0, nq, P.D, g_off);
         if (tid < 64) {
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
         const uint32_t at = (uint32_t)(n & 1) * STAGE, tq = rows_at + at, tg = tq + TILE, tqc = cols_at + at, tgc = tqc + TILE;
         const float* st = reinterpret_cast<const float*>(stage + at + 2 * TILE);
         if (n + 1 < steps) load(n + 1);
-        const int r0 = (row_first + row_tiles - 1 - n / g) * DKV_ROWS;
+        const int r0 = (row_first + row_tiles - 1 - n % row_tiles) * DKV_ROWS;
         if (key0 < nk && (!P.causal || key0 <= min(r0 + DKV_ROWS, nq) - 1 + ahead)) {
             f32x16 s = {}, dp = {};
 #pragma unroll
@@ -188,7 +188,6 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
 #pragma unroll
                 for (int j = 0; j < 4; ++j) s[4 * i + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * i + j], c, -lse[j]));
             }
-            __builtin_amdgcn_sched_barrier(0);
             const bool masked = P.causal && key0 + 31 > r0 + ahead;
             if (masked) {
 #pragma unroll
@@ -202,7 +201,6 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
                 for (int db = 0; db < DP / 32; ++db)
                     dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tgc, k * 16, db), p, dv[db], 0, 0, 0);
             }
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d)
                 dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tg, 0, d), frag_rows<DP>(v_at, 0, d), dp, 0, 0, 0);
@@ -217,7 +215,6 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
                 for (int i = 0; i < 16; ++i)
                     if (key > r0 + 8 * (i >> 2) + 4 * h + (i & 3) + ahead) s[i] = 0.0f;
             }
-            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const bf16x8 ds = pack_frag(s, k);

@@ -11,125 +11,147 @@ namespace skipffn {
 
 constexpr int FWD_KEYS = 64;
 
+// Workgroups that fit a compute unit at a time
+template <int DP> constexpr int fwd_per_cu() { return DP <= 64 ? 3 : 2; }
+
 template <int DP>
-__global__ __launch_bounds__(ATT_THREADS, 2) void attn_fwd_kernel(const AttnArgs P) {
+__global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel(const AttnArgs P, const int blocks) {
     constexpr int TILE = FWD_KEYS * tile_row_bytes<DP>();
     __shared__ __align__(256) char smem[4 * TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-    const int kvh = (int)blockIdx.x % P.Hkv, g = P.Hq / P.Hkv;
+    const int g = P.Hq / P.Hkv;
+    int kvh, turn = 0;
     SeqItem it;
-    if (!locate_queries(P, (int)blockIdx.x / P.Hkv, g, it)) return;
-    const int item = it.item, q0 = it.q0, q1 = it.q1, k0 = it.k0, k1 = it.k1;
-    const int nq = q1 - q0, nk = k1 - k0, ahead = nk - nq;
-    const int units = (nq + ATT_ROWS - 1) / ATT_ROWS * g;
-    const int first = units - 1 - item * ATT_WAVES, unit = first - wave;          // wave 0 has the latest queries
-    const int row0 = unit >= 0 ? unit / g * ATT_ROWS : 0, head = kvh * g + (unit >= 0 ? unit % g : 0);
-    auto keys_of = [&](int row) { const int n = P.causal ? row + 1 + ahead : nk; return n < nk ? n : nk; };   // of a query; may be < 0
-    const int last = first / g * ATT_ROWS + ATT_ROWS;
-    const int tiles = (max(keys_of((last < nq ? last : nq) - 1), 0) + FWD_KEYS - 1) / FWD_KEYS;
-    const int wave_end = unit >= 0 ? keys_of((row0 + ATT_ROWS < nq ? row0 + ATT_ROWS : nq) - 1) : 0;
-    const int all_see = keys_of(row0);                                           // keys before it are seen by every row
-
-    const int row = row0 + (lane & 31);
-    const bool row_ok = unit >= 0 && row < nq;
-    const int row_keys = keys_of(row);
-    bf16x8 qf[DP / 16];
-    {
-        const __amdgpu_buffer_rsrc_t rq = make_rsrc(P.q + head * P.q_head + (int64_t)(q0 + row0) * P.q_tok, 0x7fffffffu);
-        load_rows<DP>(rq, (uint32_t)((lane & 31) * P.q_tok) * 2u, row_ok, P.D, lane, qf);
-    }
-    const HeadRows K{P.k + kvh * P.k_head + (int64_t)k0 * P.k_tok, P.k_tok}, V{P.v + kvh * P.v_head + (int64_t)k0 * P.v_tok, P.v_tok};
+    auto locate = [&](int k, int& head, SeqItem& to) {
+        const int piece = piece_of(k);
+        if (piece >= blocks) return false;
+        head = piece % P.Hkv;
+        return locate_queries(P, unhoisted(lane), piece / P.Hkv, g, to);
+    };
     const uint32_t k_off = TileLoad<DP, FWD_KEYS>::first(tid, P.k_tok, P.D), v_off = TileLoad<DP, FWD_KEYS>::first(tid, P.v_tok, P.D);
-    TileLoad<DP, FWD_KEYS> lk, lv;
     const uint32_t rows_at = lds_addr_of(smem) + rows_lane<DP>(lane), cols_at = lds_addr_of(smem) + TILE + cols_lane<DP>(lane);
-
-    f32x16 acc[DP / 32] = {};
-    float m = -INFINITY, l = 0.0f;
-    const float c = P.scale_log2;
-    if (tiles > 0) {
-        lk.load(K, 0, nk, P.D, k_off);
-        lv.load(V, 0, nk, P.D, v_off);
-        lk.store(smem, tid);
-        lv.store(smem + TILE, tid);
-    }
-    __syncthreads();
-    for (int t = 0; t < tiles; ++t) {
-        const uint32_t stage = (uint32_t)(t & 1) * (2 * TILE), tk = rows_at + stage, tv = cols_at + stage;
-        if (t + 1 < tiles) {
-            lk.load(K, (t + 1) * FWD_KEYS, nk, P.D, k_off);
-            lv.load(V, (t + 1) * FWD_KEYS, nk, P.D, v_off);
+    TileLoad<DP, FWD_KEYS> lk, lv;
+    auto load_tile = [&](const SeqItem& s, int head, int t) {
+        lk.load(HeadRows{P.k + head * P.k_head + (int64_t)s.k0 * P.k_tok, P.k_tok}, t * FWD_KEYS, s.k1 - s.k0, P.D, k_off);
+        lv.load(HeadRows{P.v + head * P.v_head + (int64_t)s.k0 * P.v_tok, P.v_tok}, t * FWD_KEYS, s.k1 - s.k0, P.D, v_off);
+    };
+    bf16x8 qf[DP / 16];
+    auto load_q = [&](const SeqItem& s, const QueryUnit& u) {
+        const int ln = unhoisted(lane);
+        load_rows<DP>(make_rsrc(P.q + u.head * P.q_head + (int64_t)(s.q0 + u.row0) * P.q_tok, 0x7fffffffu), (uint32_t)((ln & 31) * P.q_tok) * 2u,
+                      u.any && u.row0 + (ln & 31) < s.q1 - s.q0, P.D, ln, qf);
+    };
+    if (!locate(0, kvh, it)) return;
+    QueryUnit u = query_unit<FWD_KEYS>(P, it, kvh, wave);
+    load_q(it, u);
+    if (u.tiles > 0) load_tile(it, kvh, 0);
+    int stage = 0;                                       // which of the two tiles in LDS
+    for (;;) {
+        SeqItem next_it;
+        int next_kvh = 0;
+        const bool more = locate(++turn, next_kvh, next_it);
+        const QueryUnit next = more ? query_unit<FWD_KEYS>(P, next_it, next_kvh, wave) : QueryUnit{};
+        const int nq = it.q1 - it.q0, nk = it.k1 - it.k0, row = u.row0 + (lane & 31);
+        const int row_keys = P.causal ? min(row + 1 + nk - nq, nk) : nk;
+        f32x16 acc[DP / 32] = {};
+        float m = -INFINITY, l = 0.0f;
+        const float c = P.scale_log2;
+        if (u.tiles > 0) {
+            lk.store(smem + stage * 2 * TILE, tid);
+            lv.store(smem + stage * 2 * TILE + TILE, tid);
+            __syncthreads();
+        } else if (next.tiles > 0) {
+            load_tile(next_it, next_kvh, 0);
         }
-        if (t * FWD_KEYS < wave_end) {
-            f32x16 s[2];
+        for (int t = 0; t < u.tiles; ++t) {
+            const uint32_t at = (uint32_t)stage * (2 * TILE), tk = rows_at + at, tv = cols_at + at;
+            const bool last = t + 1 == u.tiles;
+            if (!last) load_tile(it, kvh, t + 1);
+            else if (next.tiles > 0) load_tile(next_it, next_kvh, 0);
+            if (t * FWD_KEYS < u.wave_end) {
+                f32x16 s[2];
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                s[kb] = f32x16{};
+                for (int kb = 0; kb < 2; ++kb) {
+                    s[kb] = f32x16{};
 #pragma unroll
-                for (int d = 0; d < DP / 16; ++d)
-                    s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d), qf[d], s[kb], 0, 0, 0);
-            }
-            if ((t + 1) * FWD_KEYS > all_see) {
+                    for (int d = 0; d < DP / 16; ++d)
+                        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d), qf[d], s[kb], 0, 0, 0);
+                }
+                __builtin_amdgcn_s_setprio(0);
+                if ((t + 1) * FWD_KEYS > u.all_see) {
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (t * FWD_KEYS + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= row_keys) s[kb][i] = -INFINITY;
+                }
+                float top = s[0][0];
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (t * FWD_KEYS + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= row_keys) s[kb][i] = -INFINITY;
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-            top = halves_max(top);
-            // The maximum may lag by up to a factor 2^8 of the weights, which bf16 and the fp32 sums hold as exactly: the sums are
-            // seldom scaled again
-            if (__ballot((top - m) * c > 8.0f || (m == -INFINITY && top != -INFINITY)) != 0) {
-                const float now = fmaxf(m, top), scale = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - now) * c);
-                l *= scale;
-#pragma unroll
-                for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[db][i] *= scale;
-                m = now;
-            }
-            const float mc = m == -INFINITY ? 0.0f : m * c;
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -mc));
-                    l += s[kb][i];
-                }
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const bf16x8 p = pack_frag(s[kb], k);
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+                top = halves_max(top);
+                // The maximum may lag by up to a factor 2^8 of the weights, which bf16 and the fp32 sums hold as exactly: the sums are
+                // seldom scaled again
+                if (__ballot((top - m) * c > 8.0f || (m == -INFINITY && top != -INFINITY)) != 0) {
+                    const float now = fmaxf(m, top), scale = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - now) * c);
+                    l *= scale;
 #pragma unroll
                     for (int db = 0; db < DP / 32; ++db)
-                        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tv, kb * 32 + k * 16, db), p, acc[db], 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[db][i] *= scale;
+                    m = now;
                 }
+                const float mc = m == -INFINITY ? 0.0f : m * c;
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -mc));
+                        l += s[kb][i];
+                    }
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const bf16x8 p = pack_frag(s[kb], k);
+#pragma unroll
+                        for (int db = 0; db < DP / 32; ++db)
+                            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tv, kb * 32 + k * 16, db), p, acc[db], 0, 0, 0);
+                    }
+            }
+            if (!last) {
+                stage ^= 1;
+                lk.store(smem + stage * 2 * TILE, tid);
+                lv.store(smem + stage * 2 * TILE + TILE, tid);
+                __syncthreads();
+            }
         }
-        if (t + 1 < tiles) {
-            char* nx = smem + ((t + 1) & 1) * 2 * TILE;
-            lk.store(nx, tid);
-            lv.store(nx + TILE, tid);
+        if (more) load_q(next_it, next);
+        l = halves_sum(l);
+        if (u.any) {
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // a row that sees no key is zero
+            // by way of the tile that no wavefront reads any more
+            store_rows<DP>(P.out + u.head * P.o_head + (int64_t)(it.q0 + u.row0) * P.o_tok, P.o_tok, min(nq - u.row0, ATT_ROWS), acc, inv, P.D,
+                           unhoisted(lane), smem + (stage ^ 1) * 2 * TILE + wave * 32 * tile_row_bytes<DP>());
+            if (P.lse != nullptr && h == 0 && row < nq)
+                P.lse[(int64_t)u.head * P.Tq + it.q0 + row] = l == 0.0f ? INFINITY : fmaf(m, c, __builtin_amdgcn_logf(l));
         }
-        __syncthreads();
+        if (!more) return;
+        __syncthreads();                                 // both tiles have been read
+        it = next_it;
+        kvh = next_kvh;
+        u = next;
     }
-    l = halves_sum(l);
-    if (unit < 0) return;
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;          // a row that sees no key is zero
-    store_rows<DP>(P.out + head * P.o_head + (int64_t)(q0 + row0) * P.o_tok, P.o_tok, min(nq - row0, ATT_ROWS), acc, inv, P.D, lane,
-                   smem + wave * 32 * tile_row_bytes<DP>());
-    if (P.lse != nullptr && h == 0 && row_ok)
-        P.lse[(int64_t)head * P.Tq + q0 + row] = l == 0.0f ? INFINITY : fmaf(m, c, __builtin_amdgcn_logf(l));
 }
 
-hipError_t launch_attn_forward(const AttnArgs& a, hipStream_t s) {
-    const dim3 grid((uint32_t)attn_query_workgroups(a));
-    if (a.D <= 64) attn_fwd_kernel<64><<<grid, ATT_THREADS, 0, s>>>(a);
-    else attn_fwd_kernel<128><<<grid, ATT_THREADS, 0, s>>>(a);
+hipError_t launch_attn_forward(const AttnArgs& a, int ncu, hipStream_t s) {
+    const int64_t blocks = attn_query_workgroups(a);
+    const int64_t fit = (int64_t)ncu * (a.D <= 64 ? fwd_per_cu<64>() : fwd_per_cu<128>()) / 8 * 8;
+    const dim3 grid((uint32_t)(blocks < fit ? blocks : fit));
+    if (a.D <= 64) attn_fwd_kernel<64><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
+    else attn_fwd_kernel<128><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
     return hipGetLastError();
 }
 

@@ -203,7 +203,7 @@ struct AttnDecodeArgs {
 int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t Tp, int64_t cap, int ncu);
 int attn_padded_columns(int D);                   // columns of a row of part
 hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s);
-hipError_t launch_attn_forward(const AttnArgs& a, hipStream_t s);
+hipError_t launch_attn_forward(const AttnArgs& a, int ncu, hipStream_t s);
 hipError_t launch_attn_backward(const AttnArgs& a, const AttnGrads& g, hipStream_t s);
 
 // ---- GEMMs -----------------------------------------------------------------------
