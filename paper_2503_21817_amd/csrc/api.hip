@@ -861,7 +861,18 @@ AttnArgs attn_args(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hk
     a.q_head = q->head_stride; a.k_head = k->head_stride; a.v_head = v->head_stride; a.o_head = out->head_stride;
     a.seg_q = seg_q; a.seg_k = seg_k == nullptr ? seg_q : seg_k;
     a.lse = lse;
+    a.splits = 1;
     return a;
+}
+// workspace of rows (of a head) whose keys are cut into parts
+struct PartsWs { int splits; size_t part, stat, total; };
+PartsWs parts_ws(int64_t rows, int64_t D, int splits) {
+    PartsWs W{};
+    W.splits = splits;
+    if (splits == 1) return W;
+    W.stat = align_up((size_t)rows * splits * attn_padded_columns((int)D) * 4);
+    W.total = W.stat + align_up((size_t)rows * splits * 8);
+    return W;
 }
 }  // namespace
 
@@ -870,7 +881,8 @@ size_t skipffn_attn_saved_bytes(int64_t Tq, int64_t Hq) {
     return align_up((size_t)Tq * Hq * 4) + 256;
 }
 size_t skipffn_attn_forward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D) {
-    return 0;
+    if (check_attn(Tq, Tk, n_seq, Hq, Hkv, D, 1.0f) != SKIPFFN_OK) return 0;
+    return parts_ws(Tq * Hq, D, attn_forward_splits(Tq, Tk, n_seq, Hq, Hkv, D, num_cus())).total;
 }
 size_t skipffn_attn_backward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D) {
     if (check_attn(Tq, Tk, n_seq, Hq, Hkv, D, 1.0f) != SKIPFFN_OK) return 0;
@@ -891,8 +903,13 @@ int skipffn_attn_forward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int6
     if (bad_seg(seg_q) || (seg_k != nullptr && bad_seg(seg_k)) || (saved != nullptr && !aligned16(saved))) return SKIPFFN_EINVAL;
     if (heads_meet(out, Tq, Hq, q, Tq, Hq, D) || heads_meet(out, Tq, Hq, k, Tk, Hkv, D) || heads_meet(out, Tq, Hq, v, Tk, Hkv, D))
         return SKIPFFN_EINVAL;
+    const PartsWs W = parts_ws(Tq * Hq, D, attn_forward_splits(Tq, Tk, n_seq, Hq, Hkv, D, num_cus()));
+    if (W.total > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < W.total)) return SKIPFFN_EWORKSPACE;
     hipStream_t s = (hipStream_t)stream;
-    const AttnArgs a = attn_args(Tq, Tk, n_seq, Hq, Hkv, D, q, k, v, out, seg_q, seg_k, causal, scale, static_cast<float*>(saved));
+    AttnArgs a = attn_args(Tq, Tk, n_seq, Hq, Hkv, D, q, k, v, out, seg_q, seg_k, causal, scale, static_cast<float*>(saved));
+    a.splits = W.splits;
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + W.part);
+    a.stat = reinterpret_cast<float*>(static_cast<char*>(workspace) + W.stat);
     profile_mark_begin(KC_ATTN_FWD, s);
     hipError_t e = launch_attn_forward(a, num_cus(), s);
     profile_mark_end(KC_ATTN_FWD, s);
@@ -945,23 +962,12 @@ int check_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64
     if (n_groups > 65534 || cap >= (1 << 30) || (n_seq + n_groups + 1) * Hq >= (1ll << 31)) return SKIPFFN_ESHAPE;
     return SKIPFFN_OK;
 }
-struct DecodeWs { int splits; size_t part, stat, total; };
-DecodeWs decode_ws(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t cap) {
-    DecodeWs W{};
-    W.splits = attn_decode_splits(n_seq, n_groups, Hq, Hkv, Tp, cap, num_cus());
-    if (W.splits == 1) return W;
-    const size_t rows = (size_t)n_seq * Hq * W.splits;
-    W.part = 0;
-    W.stat = align_up(rows * attn_padded_columns((int)D) * 4);
-    W.total = W.stat + align_up(rows * 8);
-    return W;
-}
 }  // namespace
 
 size_t skipffn_attn_decode_workspace_bytes(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp,
                                            int64_t suffix_capacity) {
     if (check_decode(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, 1.0f) != SKIPFFN_OK) return 0;
-    return decode_ws(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity).total;
+    return parts_ws(n_seq * Hq, D, attn_decode_splits(n_seq, n_groups, Hq, Hkv, Tp, suffix_capacity, num_cus())).total;
 }
 
 int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t suffix_capacity,
@@ -990,7 +996,7 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
     if (meets(q, n_seq, Hq, 0) || (Tg > 0 && (meets(prefix_k, Tg, Hkv, 0) || meets(prefix_v, Tg, Hkv, 0))) ||
         (cap > 0 && (meets(suffix_k, cap, Hkv, (n_seq - 1) * suffix_k_seq) || meets(suffix_v, cap, Hkv, (n_seq - 1) * suffix_v_seq))))
         return SKIPFFN_EINVAL;
-    const DecodeWs W = decode_ws(n_seq, n_groups, Hq, Hkv, D, Tp, cap);
+    const PartsWs W = parts_ws(n_seq * Hq, D, attn_decode_splits(n_seq, n_groups, Hq, Hkv, Tp, cap, num_cus()));
     if (W.total > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < W.total)) return SKIPFFN_EWORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     AttnDecodeArgs a{};

@@ -270,11 +270,12 @@ __device__ __forceinline__ int piece_of(int k) {
 
 // What a wavefront works on in a kernel by queries: 32 rows of a head
 struct QueryUnit {
-    int head, row0, tiles, wave_end, all_see;            // tiles: of the workgroup; keys that the last row, the first row see
+    int head, row0, wave_end, all_see;                   // keys that the last row, the first row see
+    int t0, t1;                                          // the workgroup's tiles of keys
     bool any;
 };
 template <int KEYS>
-__device__ __forceinline__ QueryUnit query_unit(const AttnArgs& P, const SeqItem& it, int kvh, int wave) {
+__device__ __forceinline__ QueryUnit query_unit(const AttnArgs& P, const SeqItem& it, int kvh, int wave, int part = 0, int parts = 1) {
     const int g = P.Hq / P.Hkv, nq = it.q1 - it.q0, nk = it.k1 - it.k0;
     const int units = (nq + ATT_ROWS - 1) / ATT_ROWS * g;
     const int first = units - 1 - it.item * ATT_WAVES, unit = first - wave;       // wave 0 has the latest queries
@@ -283,7 +284,9 @@ __device__ __forceinline__ QueryUnit query_unit(const AttnArgs& P, const SeqItem
     u.any = unit >= 0;
     u.row0 = u.any ? unit / g * ATT_ROWS : 0;
     u.head = kvh * g + (u.any ? unit % g : 0);
-    u.tiles = (max(keys_of(min(first / g * ATT_ROWS + ATT_ROWS, nq) - 1), 0) + KEYS - 1) / KEYS;
+    const int tiles = (max(keys_of(min(first / g * ATT_ROWS + ATT_ROWS, nq) - 1), 0) + KEYS - 1) / KEYS;
+    u.t0 = parts == 1 ? 0 : tiles * part / parts;
+    u.t1 = parts == 1 ? tiles : tiles * (part + 1) / parts;
     u.wave_end = u.any ? keys_of(min(u.row0 + ATT_ROWS, nq) - 1) : 0;
     u.all_see = keys_of(u.row0);
     return u;

@@ -175,46 +175,6 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnD
         }
 }
 
-// The parts of a row: a wavefront a row, a lane a part's statistics and then DP / 64 columns
-template <int DP>
-__global__ __launch_bounds__(ATT_THREADS) void attn_join_kernel(const AttnDecodeArgs P) {
-    const int lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * ATT_WAVES + (threadIdx.x >> 6);
-    if (row >= (int64_t)P.n_seq * P.Hq) return;
-    constexpr int V = DP / 64;
-    float m = -INFINITY, l = 0.0f;
-    if (lane < P.splits) {
-        m = P.stat[2 * (row * P.splits + lane)];
-        l = P.stat[2 * (row * P.splits + lane) + 1];
-    }
-    float top = m;
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
-    const float w = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * P.scale_log2);
-    const float sum = wave_sum(w * l);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-    float o[V] = {};
-    const float* part = P.part + row * P.splits * DP + lane * V;
-    for (int i0 = 0; i0 < P.splits; i0 += 8) {           // eight parts' loads under way; past the last one, the last again, unused
-        float x[8][V];
-#pragma unroll
-        for (int u = 0; u < 8; ++u)
-#pragma unroll
-            for (int j = 0; j < V; ++j) x[u][j] = part[(int64_t)min(i0 + u, P.splits - 1) * DP + j];
-#pragma unroll
-        for (int u = 0; u < 8; ++u) {
-            if (i0 + u >= P.splits) break;
-            const float wi = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), i0 + u));
-#pragma unroll
-            for (int j = 0; j < V; ++j) o[j] = fmaf(wi, x[u][j], o[j]);
-        }
-    }
-    if (lane * V >= P.D) return;
-    bf16_t* out = P.out + row / P.Hq * P.o_tok + row % P.Hq * P.o_head + lane * V;
-    if constexpr (V == 2) *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(o[0] * inv, o[1] * inv);
-    else *out = f32_to_bf16(o[0] * inv);
-}
-
 namespace {
 int64_t decode_blocks(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv) {
     const int64_t g = Hq / Hkv, members = g >= 32 ? 1 : 32 / g;
@@ -222,8 +182,6 @@ int64_t decode_blocks(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv) 
     return std::min(n_seq, n_seq / members + n_groups + 1) * Hkv * ((g + 31) / 32);
 }
 }  // namespace
-
-int attn_padded_columns(int D) { return D <= 64 ? 64 : 128; }
 
 // As many parts as give every compute unit two workgroups, but none of fewer than 4 tiles a wavefront of the longest list that
 // the bounds allow on average
@@ -234,7 +192,7 @@ int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv,
     const int64_t shared = std::max<int64_t>(1, std::min(members, n_groups > 0 ? n_seq / n_groups : members));
     const int64_t keys = (n_groups > 0 ? Tp / n_groups : 0) + shared * cap;
     const int64_t want = (2 * (int64_t)ncu + blocks - 1) / blocks, most = keys / (DEC_KEYS * ATT_WAVES * 2);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), DEC_MAX_SPLITS));
+    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), ATTN_MAX_SPLITS));
 }
 
 hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s) {
@@ -243,10 +201,11 @@ hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s) {
     else attn_decode_kernel<128><<<grid, ATT_THREADS, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    const uint32_t wgs = (uint32_t)(((int64_t)a.n_seq * a.Hq + ATT_WAVES - 1) / ATT_WAVES);
-    if (a.D <= 64) attn_join_kernel<64><<<wgs, ATT_THREADS, 0, s>>>(a);
-    else attn_join_kernel<128><<<wgs, ATT_THREADS, 0, s>>>(a);
-    return hipGetLastError();
+    AttnJoinArgs j{};
+    j.T = a.n_seq; j.Hq = a.Hq; j.D = a.D; j.splits = a.splits; j.scale_log2 = a.scale_log2;
+    j.part = a.part; j.stat = a.stat;
+    j.out = a.out; j.o_tok = a.o_tok; j.o_head = a.o_head;
+    return launch_attn_join(j, s);
 }
 
 }  // namespace skipffn

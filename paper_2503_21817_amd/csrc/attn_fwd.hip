@@ -14,19 +14,24 @@ constexpr int FWD_KEYS = 64;
 // Workgroups that fit a compute unit at a time
 template <int DP> constexpr int fwd_per_cu() { return DP <= 64 ? 3 : 2; }
 
-template <int DP>
+template <int DP, bool PARTS>
 __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel(const AttnArgs P, const int blocks) {
     constexpr int TILE = FWD_KEYS * tile_row_bytes<DP>();
     __shared__ __align__(256) char smem[4 * TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int g = P.Hq / P.Hkv;
-    int kvh, turn = 0;
+    int kvh, turn = 0, part = 0;                         // part: of the keys
     SeqItem it;
-    auto locate = [&](int k, int& head, SeqItem& to) {
-        const int piece = piece_of(k);
+    auto locate = [&](int k, int& head, int& z, SeqItem& to) {
+        int piece = piece_of(k);
         if (piece >= blocks) return false;
         head = piece % P.Hkv;
-        return locate_queries(P, unhoisted(lane), piece / P.Hkv, g, to);
+        piece /= P.Hkv;
+        if constexpr (PARTS) {
+            z = piece % P.splits;
+            piece /= P.splits;
+        }
+        return locate_queries(P, unhoisted(lane), piece, g, to);
     };
     const uint32_t k_off = TileLoad<DP, FWD_KEYS>::first(tid, P.k_tok, P.D), v_off = TileLoad<DP, FWD_KEYS>::first(tid, P.v_tok, P.D);
     const uint32_t rows_at = lds_addr_of(smem) + rows_lane<DP>(lane), cols_at = lds_addr_of(smem) + TILE + cols_lane<DP>(lane);
@@ -41,96 +46,129 @@ __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel
         load_rows<DP>(make_rsrc(P.q + u.head * P.q_head + (int64_t)(s.q0 + u.row0) * P.q_tok, 0x7fffffffu), (uint32_t)((ln & 31) * P.q_tok) * 2u,
                       u.any && u.row0 + (ln & 31) < s.q1 - s.q0, P.D, ln, qf);
     };
-    if (!locate(0, kvh, it)) return;
-    QueryUnit u = query_unit<FWD_KEYS>(P, it, kvh, wave);
+    if (!locate(0, kvh, part, it)) return;
+    QueryUnit u = query_unit<FWD_KEYS>(P, it, kvh, wave, part, PARTS ? P.splits : 1);
     load_q(it, u);
-    if (u.tiles > 0) load_tile(it, kvh, 0);
+    if (u.t0 < u.t1) load_tile(it, kvh, u.t0);
     int stage = 0;                                       // which of the two tiles in LDS
     for (;;) {
         SeqItem next_it;
-        int next_kvh = 0;
-        const bool more = locate(++turn, next_kvh, next_it);
-        const QueryUnit next = more ? query_unit<FWD_KEYS>(P, next_it, next_kvh, wave) : QueryUnit{};
+        int next_kvh = 0, next_part = 0;
+        const bool more = locate(++turn, next_kvh, next_part, next_it);
+        const QueryUnit next = more ? query_unit<FWD_KEYS>(P, next_it, next_kvh, wave, next_part, PARTS ? P.splits : 1) : QueryUnit{};
         const int nq = it.q1 - it.q0, nk = it.k1 - it.k0, row = u.row0 + (lane & 31);
         const int row_keys = P.causal ? min(row + 1 + nk - nq, nk) : nk;
         f32x16 acc[DP / 32] = {};
         float m = -INFINITY, l = 0.0f;
         const float c = P.scale_log2;
-        if (u.tiles > 0) {
+        if (u.t0 < u.t1) {
             lk.store(smem + stage * 2 * TILE, tid);
             lv.store(smem + stage * 2 * TILE + TILE, tid);
             __syncthreads();
-        } else if (next.tiles > 0) {
-            load_tile(next_it, next_kvh, 0);
+        } else if (next.t0 < next.t1) {
+            load_tile(next_it, next_kvh, next.t0);
         }
-        for (int t = 0; t < u.tiles; ++t) {
+        auto work_on = [&](int t) {
+            if (t * FWD_KEYS >= u.wave_end) return;
             const uint32_t at = (uint32_t)stage * (2 * TILE), tk = rows_at + at, tv = cols_at + at;
-            const bool last = t + 1 == u.tiles;
-            if (!last) load_tile(it, kvh, t + 1);
-            else if (next.tiles > 0) load_tile(next_it, next_kvh, 0);
-            if (t * FWD_KEYS < u.wave_end) {
-                f32x16 s[2];
+            // Operands are asked for a few products ahead and the order is held (left to itself the compiler reads each right before its
+            // product); products go before the other wavefront's exponentials.  1 x 16384 tokens 2127 -> 2030 us, 1 x 616 21.7 -> 17.8
+            f32x16 s[2];
+            constexpr int NK = DP / 16, AHEAD = 4;
+            {
+                bf16x8 kf[AHEAD];
+#pragma unroll
+                for (int i = 0; i < AHEAD; ++i) kf[i] = frag_rows<DP>(tk, i / NK * 32, i % NK);
                 __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) {
-                    s[kb] = f32x16{};
-#pragma unroll
-                    for (int d = 0; d < DP / 16; ++d)
-                        s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d), qf[d], s[kb], 0, 0, 0);
+                for (int i = 0; i < 2 * NK; ++i) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (i % NK == 0) s[i / NK] = f32x16{};
+                    s[i / NK] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], qf[i % NK], s[i / NK], 0, 0, 0);
+                    if (i + AHEAD < 2 * NK) kf[i % AHEAD] = frag_rows<DP>(tk, (i + AHEAD) / NK * 32, (i + AHEAD) % NK);
                 }
+                __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_setprio(0);
-                if ((t + 1) * FWD_KEYS > u.all_see) {
-#pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (t * FWD_KEYS + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= row_keys) s[kb][i] = -INFINITY;
-                }
-                float top = s[0][0];
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
-                top = halves_max(top);
-                // The maximum may lag by up to a factor 2^8 of the weights, which bf16 and the fp32 sums hold as exactly: the sums are
-                // seldom scaled again
-                if (__ballot((top - m) * c > 8.0f || (m == -INFINITY && top != -INFINITY)) != 0) {
-                    const float now = fmaxf(m, top), scale = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - now) * c);
-                    l *= scale;
-#pragma unroll
-                    for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[db][i] *= scale;
-                    m = now;
-                }
-                const float mc = m == -INFINITY ? 0.0f : m * c;
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -mc));
-                        l += s[kb][i];
-                    }
-#pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                    for (int k = 0; k < 2; ++k) {
-                        const bf16x8 p = pack_frag(s[kb], k);
-#pragma unroll
-                        for (int db = 0; db < DP / 32; ++db)
-                            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tv, kb * 32 + k * 16, db), p, acc[db], 0, 0, 0);
-                    }
             }
-            if (!last) {
-                stage ^= 1;
-                lk.store(smem + stage * 2 * TILE, tid);
-                lv.store(smem + stage * 2 * TILE + TILE, tid);
-                __syncthreads();
+            if ((t + 1) * FWD_KEYS > u.all_see) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (t * FWD_KEYS + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= row_keys) s[kb][i] = -INFINITY;
             }
+            float top = s[0][0];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
+            top = halves_max(top);
+            // The maximum may lag by up to a factor 2^8 of the weights, which bf16 and the fp32 sums hold as exactly: the sums are
+            // seldom scaled again
+            if (__ballot((top - m) * c > 8.0f || (m == -INFINITY && top != -INFINITY)) != 0) {
+                const float now = fmaxf(m, top), scale = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - now) * c);
+                l *= scale;
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[db][i] *= scale;
+                m = now;
+            }
+            const float mc = m == -INFINITY ? 0.0f : m * c;
+            auto weight = [&](int kb, int i) {
+                s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -mc));
+                l += s[kb][i];
+            };
+            constexpr int NV = DP / 32, VAHEAD = 3, STEPS = 4 * NV;
+            bf16x8 vf[VAHEAD], pf;
+#pragma unroll
+            for (int i = 0; i < VAHEAD; ++i) vf[i] = frag_cols<DP>(tv, i / NV * 16, i % NV);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) weight(0, i);    // of the first product's keys; the others beside the products
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (i % NV == 0) pf = pack_frag(s[i / NV >> 1], i / NV & 1);
+                acc[i % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % VAHEAD], pf, acc[i % NV], 0, 0, 0);
+                if (i + VAHEAD < STEPS) vf[i % VAHEAD] = frag_cols<DP>(tv, (i + VAHEAD) / NV * 16, (i + VAHEAD) % NV);
+                if (i < 3 * NV) {
+#pragma unroll
+                    for (int j = 0; j < 8 / NV; ++j) { const int w = 8 + i * (8 / NV) + j; weight(w >> 4, w & 15); }
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
+        };
+        for (int t = u.t0; t + 1 < u.t1; ++t) {
+            load_tile(it, kvh, t + 1);
+            work_on(t);
+            stage ^= 1;
+            lk.store(smem + stage * 2 * TILE, tid);
+            lv.store(smem + stage * 2 * TILE + TILE, tid);
+            __syncthreads();
+        }
+        if (u.t0 < u.t1) {
+            if (next.t0 < next.t1) load_tile(next_it, next_kvh, next.t0);
+            work_on(u.t1 - 1);
         }
         if (more) load_q(next_it, next);
         l = halves_sum(l);
-        if (u.any) {
+        if (PARTS && u.any) {
+            if (row < nq) {
+                const int64_t at = ((int64_t)(it.q0 + row) * P.Hq + u.head) * P.splits + part;
+                if (h == 0) {
+                    P.stat[2 * at] = m;
+                    P.stat[2 * at + 1] = l;
+                }
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<f32x4*>(P.part + at * DP + db * 32 + 8 * i + 4 * h) =
+                            f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]};
+            }
+        } else if (u.any) {
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // a row that sees no key is zero
             // by way of the tile that no wavefront reads any more
             store_rows<DP>(P.out + u.head * P.o_head + (int64_t)(it.q0 + u.row0) * P.o_tok, P.o_tok, min(nq - u.row0, ATT_ROWS), acc, inv, P.D,
@@ -142,17 +180,45 @@ __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel
         __syncthreads();                                 // both tiles have been read
         it = next_it;
         kvh = next_kvh;
+        part = next_part;
         u = next;
     }
 }
 
+// Few queries over many keys would leave most of the chip idle.  Parts cost a second kernel (about 4 us) and a row of fp32 written
+// and read again each (at about 4 TB/s), and save tiles of keys one after the other (about 1.2 us each)
+int attn_forward_splits(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int ncu) {
+    if (Tq <= 0 || Tk <= 0 || n_seq <= 0) return 1;
+    AttnArgs a{};
+    a.Tq = (int)Tq; a.n_seq = (int)n_seq; a.Hq = (int)Hq; a.Hkv = (int)Hkv;
+    const int64_t blocks = attn_query_workgroups(a), fit = (int64_t)ncu * 2;
+    const double tiles = (double)Tk / (double)n_seq / FWD_KEYS, row_us = (double)Tq * (double)Hq * (attn_padded_columns((int)D) * 8) / 4e6;
+    int best = 1;
+    double least = tiles * 1.2;
+    for (int n = 2; n <= 16 && n <= tiles && blocks * n <= fit; ++n) {
+        const double us = tiles * 1.2 / n + 4.0 + row_us * n;
+        if (us < least) { least = us; best = n; }
+    }
+    return best;
+}
+
 hipError_t launch_attn_forward(const AttnArgs& a, int ncu, hipStream_t s) {
-    const int64_t blocks = attn_query_workgroups(a);
+    const int64_t blocks = attn_query_workgroups(a) * a.splits;
     const int64_t fit = (int64_t)ncu * (a.D <= 64 ? fwd_per_cu<64>() : fwd_per_cu<128>()) / 8 * 8;
     const dim3 grid((uint32_t)(blocks < fit ? blocks : fit));
-    if (a.D <= 64) attn_fwd_kernel<64><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
-    else attn_fwd_kernel<128><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
-    return hipGetLastError();
+    if (a.splits == 1 && a.D <= 64) attn_fwd_kernel<64, false><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
+    else if (a.splits == 1) attn_fwd_kernel<128, false><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
+    else if (a.D <= 64) attn_fwd_kernel<64, true><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
+    else attn_fwd_kernel<128, true><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    AttnJoinArgs j{};
+    j.T = a.Tq; j.Hq = a.Hq; j.D = a.D; j.splits = a.splits; j.scale_log2 = a.scale_log2;
+    j.part = a.part; j.stat = a.stat;
+    j.out = a.out; j.o_tok = a.o_tok; j.o_head = a.o_head;
+    j.lse = a.lse;
+    j.seg = a.seg_q; j.n_seq = a.n_seq;
+    return launch_attn_join(j, s);
 }
 
 }  // namespace skipffn

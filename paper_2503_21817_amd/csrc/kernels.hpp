@@ -179,7 +179,21 @@ struct AttnArgs {
     int64_t q_head, k_head, v_head, o_head;
     const int32_t* seg_q; const int32_t* seg_k;
     float* lse;                                   // [Hq][Tq], base 2, or null; infinity: the row sees no key
+    int splits; float* part; float* stat;         // forward, splits > 1: as in AttnJoinArgs
 };
+// Rows whose keys are cut into parts: row (t, h), part z: statistics (largest score, sum of weights) at stat[2 * ((t * Hq + h) * splits + z)],
+// unnormalised columns at part[((t * Hq + h) * splits + z) * attn_padded_columns(D)]
+constexpr int ATTN_MAX_SPLITS = 64;
+struct AttnJoinArgs {
+    int T, Hq, D, splits;
+    float scale_log2;
+    const float* part; const float* stat;
+    bf16_t* out; int o_tok; int64_t o_head;
+    float* lse;                                   // or null
+    const int32_t* seg; int n_seq;                // null: every row; otherwise rows of the n_seq sequences, others are left as they were
+};
+int attn_padded_columns(int D);                   // columns of a row of part
+hipError_t launch_attn_join(const AttnJoinArgs& a, hipStream_t s);
 struct AttnGrads {
     const bf16_t* go; int go_tok; int64_t go_head;
     bf16_t* dq; bf16_t* dk; bf16_t* dv;
@@ -189,7 +203,6 @@ struct AttnGrads {
 };
 // One query a sequence.  Group i has the sequences group_off[i] .. group_off[i + 1]) and the prefix rows prefix_seg[i] ..; sequences
 // from group_off[n_groups] on have no prefix.  Own rows: element (sequence, t, h, d) at sk[sequence * sk_seq + t * sk_tok + h * sk_head + d].
-constexpr int DEC_MAX_SPLITS = 64;
 struct AttnDecodeArgs {
     int n_seq, n_groups, Hq, Hkv, D, Tp, cap, splits;
     float scale_log2;
@@ -197,12 +210,13 @@ struct AttnDecodeArgs {
     const bf16_t* pk; const bf16_t* pv; int pk_tok, pv_tok; int64_t pk_head, pv_head;
     const bf16_t* sk; const bf16_t* sv; int sk_tok, sv_tok; int64_t sk_head, sv_head, sk_seq, sv_seq;
     const int32_t* prefix_seg; const int32_t* group_off; const int32_t* suffix_len;
-    float* part; float* stat;                     // splits > 1: [n_seq][Hq][splits][columns], [n_seq][Hq][splits][2]
+    float* part; float* stat;                     // splits > 1: as in AttnJoinArgs
 };
 // parts that the keys of a sequence are cut into
 int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t Tp, int64_t cap, int ncu);
-int attn_padded_columns(int D);                   // columns of a row of part
 hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s);
+// parts that the keys of a query are cut into
+int attn_forward_splits(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int ncu);
 hipError_t launch_attn_forward(const AttnArgs& a, int ncu, hipStream_t s);
 hipError_t launch_attn_backward(const AttnArgs& a, const AttnGrads& g, hipStream_t s);
 
