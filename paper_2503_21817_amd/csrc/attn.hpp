@@ -119,23 +119,8 @@ __device__ __forceinline__ float halves_sum(float v) {
     return __uint_as_float(p[0]) + __uint_as_float(p[1]);
 }
 
-// A row of the result from the registers of a product [column][row]: lane l has the row l % 32 and columns 32 db + 8 i + 4 (l / 32) .. + 3
-template <int DP>
-__device__ __forceinline__ void store_cols(bf16_t* row, const f32x16 (&acc)[DP / 32], float scale, int D, int h) {
-#pragma unroll
-    for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int d = db * 32 + 8 * i + 4 * h;
-            if (d < D) {
-                const u32x2 w = {pack_bf16x2(acc[db][4 * i] * scale, acc[db][4 * i + 1] * scale),
-                                 pack_bf16x2(acc[db][4 * i + 2] * scale, acc[db][4 * i + 3] * scale)};
-                *reinterpret_cast<u32x2*>(row + d) = w;
-            }
-        }
-}
-
-// The same for the 32 rows of a wavefront, by way of LDS (32 rows of a tile): rows leave in whole 256 (128) bytes instead of pieces of 8
+// The rows of a wavefront from the registers of a product [column][row], lane l columns 32 db + 8 i + 4 (l / 32) .. + 3 of row l % 32, by way of
+// LDS (32 rows of a tile that nobody else uses): they leave in whole 256 (128) bytes instead of pieces of 8
 template <int DP>
 __device__ __forceinline__ void store_rows(bf16_t* base, int stride, int rows, const f32x16 (&acc)[DP / 32], float scale, int D, int lane, char* lds) {
     constexpr int CH = tile_row_bytes<DP>() / 16;
@@ -156,6 +141,7 @@ __device__ __forceinline__ void store_rows(bf16_t* base, int stride, int rows, c
         const u32x4 v = *reinterpret_cast<const u32x4*>(lds + tile_off<DP>(row, c));
         if (row < rows && c * 8 < D) *reinterpret_cast<u32x4*>(base + (int64_t)row * stride + c * 8) = v;
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
 // ---- which sequence a workgroup works on ---------------------------------------------------------------

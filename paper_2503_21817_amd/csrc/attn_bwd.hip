@@ -13,7 +13,7 @@ constexpr int DQ_KEYS = 64;
 
 // ---- dQ, delta: a wavefront has a unit of 32 queries of one head, as in the forward kernel ------------------------------------
 template <int DP>
-__global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs P, const AttnGrads G) {
+__global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dq_kernel(const AttnArgs P, const AttnGrads G) {
     constexpr int TILE = DQ_KEYS * tile_row_bytes<DP>();
     __shared__ __align__(256) char smem[4 * TILE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
@@ -52,11 +52,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs 
             for (int j = 0; j < 8; ++j) delta = fmaf(a[j], b[j], delta);
         }
         delta = halves_sum(delta);
-        if (row_ok) {
-            const int64_t at = (int64_t)head * P.Tq + q0 + row;
-            lse = P.lse[at];
-            if (h == 0) G.delta[at] = delta;
-        }
+        if (row_ok) lse = P.lse[(int64_t)head * P.Tq + q0 + row];
     }
     const HeadRows K{P.k + kvh * P.k_head + (int64_t)k0 * P.k_tok, P.k_tok}, V{P.v + kvh * P.v_head + (int64_t)k0 * P.v_tok, P.v_tok};
     const uint32_t k_off = TileLoad<DP, DQ_KEYS>::first(tid, P.k_tok, P.D), v_off = TileLoad<DP, DQ_KEYS>::first(tid, P.v_tok, P.D);
@@ -71,6 +67,28 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs 
         lv.store(smem + TILE, tid);
     }
     __syncthreads();
+    constexpr int N = DP / 16, NV = DP / 32;             // products of a score tile; of 16 keys with the columns
+    if (wave_end > 0 && wave_end <= DQ_KEYS) {
+        // Rows of few keys: out's rounding, which the sum over its columns carries into delta, would show in every dS of the row.  Their
+        // keys are all in the first tile: delta = sum_j P_ij dP_ij.
+        delta = 0.0f;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int d = 0; d < N; ++d) {
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(rows_at, kb * 32, d), qf[d], s, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(rows_at + TILE, kb * 32, d), gf[d], dp, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse)) * dp[i];
+                delta += kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) < row_keys ? w : 0.0f;
+            }
+        }
+        delta = halves_sum(delta);
+    }
+    if (row_ok && h == 0) G.delta[(int64_t)head * P.Tq + q0 + row] = delta;
     for (int t = 0; t < tiles; ++t) {
         const uint32_t stage = (uint32_t)(t & 1) * (2 * TILE), tk = rows_at + stage, tv = tk + TILE, tkc = cols_at + stage;
         if (t + 1 < tiles) {
@@ -82,12 +100,12 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs 
             const int key0 = t * DQ_KEYS + kb * 32;
             if (key0 >= wave_end) continue;
             f32x16 s = {}, dp = {};
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d), qf[d], s, 0, 0, 0);
+            for (int d = 0; d < N; ++d) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d), qf[d], s, 0, 0, 0);
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d)
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tv, kb * 32, d), gf[d], dp, 0, 0, 0);
+            for (int d = 0; d < N; ++d) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tv, kb * 32, d), gf[d], dp, 0, 0, 0);
+            __builtin_amdgcn_s_setprio(0);
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse)) * (dp[i] - delta);
             if (key0 + 32 > all_see) {
@@ -99,7 +117,7 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs 
             for (int k = 0; k < 2; ++k) {
                 const bf16x8 ds = pack_frag(s, k);
 #pragma unroll
-                for (int db = 0; db < DP / 32; ++db)
+                for (int db = 0; db < NV; ++db)
                     acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tkc, kb * 32 + k * 16, db), ds, acc[db], 0, 0, 0);
             }
         }
@@ -110,14 +128,16 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dq_kernel(const AttnArgs 
         }
         __syncthreads();
     }
-    if (row_ok) store_cols<DP>(G.dq + head * G.dq_head + (int64_t)(q0 + row) * G.dq_tok, acc, P.scale, P.D, h);
+    if (unit >= 0)
+        store_rows<DP>(G.dq + head * G.dq_head + (int64_t)(q0 + row0) * G.dq_tok, G.dq_tok, min(nq - row0, ATT_ROWS), acc, P.scale, P.D, lane,
+                       smem + wave * 32 * tile_row_bytes<DP>());
 }
 
 // ---- dK, dV: a wavefront has 32 keys and goes over the queries that see them, head by head of its group -------------------------
 constexpr int DKV_KEYS = ATT_WAVES * 32, DKV_ROWS = 32;
 
 template <int DP>
-__global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs P, const AttnGrads G) {
+__global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dkv_kernel(const AttnArgs P, const AttnGrads G) {
     constexpr int ROWB = tile_row_bytes<DP>(), TILE = DKV_ROWS * ROWB, STAGE = 2 * TILE + 2 * DKV_ROWS * 4;
     __shared__ __align__(256) char smem[DKV_KEYS * ROWB + 2 * STAGE];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
@@ -146,22 +166,21 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
     }
     const uint32_t q_off = TileLoad<DP, DKV_ROWS>::first(tid, P.q_tok, P.D), g_off = TileLoad<DP, DKV_ROWS>::first(tid, G.go_tok, P.D);
     TileLoad<DP, DKV_ROWS> lq, lg;
-    float stat = 0.0f;                                   // thread t < 32: row t's log-sum-exp, t of 32 .. 63: delta
+    const float* row_stat = (wave & 1) != 0 ? G.delta : P.lse;       // the first wavefront loads the log-sum-exps, the second delta
+    float stat = 0.0f;
     auto load = [&](int n) {
         const int head = kvh * g + n / row_tiles, r0 = (row_first + row_tiles - 1 - n % row_tiles) * DKV_ROWS;
         lq.load(HeadRows{P.q + head * P.q_head + (int64_t)q0 * P.q_tok, P.q_tok}, r0, nq, P.D, q_off);
         lg.load(HeadRows{G.go + head * G.go_head + (int64_t)q0 * G.go_tok, G.go_tok}, r0, nq, P.D, g_off);
-        if (tid < 64) {
-            const int r = r0 + (tid & 31);
-            const float* src = tid < 32 ? P.lse : G.delta;
-            stat = r < nq ? src[(int64_t)head * P.Tq + q0 + r] : (tid < 32 ? INFINITY : 0.0f);
-        }
+        // rows past the sequence's read 0: with q and grad_out of 0 they give weights of 1 on gradients of 0
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(row_stat + (int64_t)head * P.Tq + q0 + r0, (uint32_t)min(nq - r0, DKV_ROWS) * 4u);
+        stat = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, lane * 4, 0, 0));
     };
     auto store = [&](int n) {
         char* st = stage + (n & 1) * STAGE;
         lq.store(st, tid);
         lg.store(st + TILE, tid);
-        if (tid < 64) reinterpret_cast<float*>(st + 2 * TILE)[tid] = stat;
+        if (wave < 2 && lane < DKV_ROWS) reinterpret_cast<float*>(st + 2 * TILE)[wave * DKV_ROWS + lane] = stat;
     };
     const uint32_t v_at = lds_addr_of(tv) + (uint32_t)(wave * 32 * ROWB) + rows_lane<DP>(lane);
     const uint32_t rows_at = lds_addr_of(stage) + rows_lane<DP>(lane), cols_at = lds_addr_of(stage) + cols_lane<DP>(lane);
@@ -177,58 +196,69 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_dkv_kernel(const AttnArgs
         const float* st = reinterpret_cast<const float*>(stage + at + 2 * TILE);
         if (n + 1 < steps) load(n + 1);
         const int r0 = (row_first + row_tiles - 1 - n % row_tiles) * DKV_ROWS;
-        if (key0 < nk && (!P.causal || key0 <= min(r0 + DKV_ROWS, nq) - 1 + ahead)) {
+        auto work_on = [&]() {
+            // Four times N products: scores, dP, dV, dK.  Operands are asked for AHEAD products before, the order is held, and the weights
+            // lie beside dP's products, dS beside dV's.
+            constexpr int N = DP / 16, NV = DP / 32, AHEAD = 2, VAHEAD = 2;
+            auto operand = [&](int i) {
+                const int j = i % N;
+                switch (i / N) {
+                    case 0: return frag_rows<DP>(tq, 0, j);
+                    case 1: return frag_rows<DP>(tg, 0, j);
+                    case 2: return frag_cols<DP>(tgc, j / NV * 16, j % NV);
+                    default: return frag_cols<DP>(tqc, j / NV * 16, j % NV);
+                }
+            };
+            auto four = [&](int at4) { return *reinterpret_cast<const f32x4*>(st + at4 + 4 * h); };      // of rows 8 q + 4 h ..: at4 = 8 q
+            const int from = P.causal ? key - r0 - ahead - 4 * h : -1;   // the key is seen by the rows from it on
             f32x16 s = {}, dp = {};
+            bf16x8 f[AHEAD], vf[VAHEAD], p[2], ds = {};
+            f32x4 row4 = {};
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tq, 0, d), kf[d], s, 0, 0, 0);
+            for (int i = 0; i < AHEAD; ++i) f[i] = operand(i);
+            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const f32x4 lse = *reinterpret_cast<const f32x4*>(st + 8 * i + 4 * h);
+            for (int i = 0; i < 4 * N; ++i) {
+                const int j = i % N, phase = i / N;
+                __builtin_amdgcn_sched_barrier(0);
+                if (i == 2 * N) {
+                    p[0] = pack_frag(s, 0);
+                    p[1] = pack_frag(s, 1);
+                }
+                if (phase == 3 && j % NV == 0) ds = pack_frag(s, j / NV);
+                if (phase == 0) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], kf[j], s, 0, 0, 0);
+                else if (phase == 1) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], vf[j % VAHEAD], dp, 0, 0, 0);
+                else if (phase == 2) dv[j % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], p[j / NV], dv[j % NV], 0, 0, 0);
+                else dk[j % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], ds, dk[j % NV], 0, 0, 0);
+                if (i + AHEAD < 4 * N) f[i % AHEAD] = operand(i + AHEAD);
+                if (i >= N - VAHEAD && i < 2 * N - VAHEAD) vf[(i + VAHEAD) % VAHEAD] = frag_rows<DP>(v_at, 0, i + VAHEAD - N);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) s[4 * i + j] = __builtin_amdgcn_exp2f(fmaf(s[4 * i + j], c, -lse[j]));
+                for (int e = j * (16 / N); e < (j + 1) * (16 / N); ++e) {
+                    if (phase == 1) {
+                        if (e % 4 == 0) row4 = four(8 * (e / 4));
+                        s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -row4[e % 4]));
+                        if (8 * (e >> 2) + (e & 3) < from) s[e] = 0.0f;
+                    }
+                    if (phase == 2) {
+                        if (e % 4 == 0) row4 = four(DKV_ROWS + 8 * (e / 4));
+                        s[e] *= dp[e] - row4[e % 4];
+                    }
+                }
             }
-            const bool masked = P.causal && key0 + 31 > r0 + ahead;
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key > r0 + 8 * (i >> 2) + 4 * h + (i & 3) + ahead) s[i] = 0.0f;
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const bf16x8 p = pack_frag(s, k);
-#pragma unroll
-                for (int db = 0; db < DP / 32; ++db)
-                    dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tgc, k * 16, db), p, dv[db], 0, 0, 0);
-            }
-#pragma unroll
-            for (int d = 0; d < DP / 16; ++d)
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tg, 0, d), frag_rows<DP>(v_at, 0, d), dp, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const f32x4 delta = *reinterpret_cast<const f32x4*>(st + DKV_ROWS + 8 * i + 4 * h);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[4 * i + j] *= dp[4 * i + j] - delta[j];
-            }
-            if (masked) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (key > r0 + 8 * (i >> 2) + 4 * h + (i & 3) + ahead) s[i] = 0.0f;
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const bf16x8 ds = pack_frag(s, k);
-#pragma unroll
-                for (int db = 0; db < DP / 32; ++db)
-                    dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(tqc, k * 16, db), ds, dk[db], 0, 0, 0);
-            }
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_setprio(0);
+        };
+        if (key0 < nk && (!P.causal || key0 <= min(r0 + DKV_ROWS, nq) - 1 + ahead)) {
+            work_on();
         }
         if (n + 1 < steps) store(n + 1);
         __syncthreads();
     }
-    if (key < nk) {
-        store_cols<DP>(G.dk + kvh * G.dk_head + (int64_t)(k0 + key) * G.dk_tok, dk, P.scale, P.D, h);
-        store_cols<DP>(G.dv + kvh * G.dv_head + (int64_t)(k0 + key) * G.dv_tok, dv, 1.0f, P.D, h);
+    if (key0 < nk) {
+        char* rows = stage + wave * 32 * ROWB;           // every wavefront has read the last step's tiles
+        const int n = min(nk - key0, 32);
+        store_rows<DP>(G.dk + kvh * G.dk_head + (int64_t)(k0 + key0) * G.dk_tok, G.dk_tok, n, dk, P.scale, P.D, lane, rows);
+        store_rows<DP>(G.dv + kvh * G.dv_head + (int64_t)(k0 + key0) * G.dv_tok, G.dv_tok, n, dv, 1.0f, P.D, lane, rows);
     }
 }
 
