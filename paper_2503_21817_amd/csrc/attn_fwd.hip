@@ -2,22 +2,25 @@
 //
 // One pass over the keys with the running maximum and sum of the softmax.  A workgroup of four wavefronts works on four units - a
 // unit is 32 consecutive queries of a sequence in one head - of the same sequence and key/value head, the heads of a group first,
-// and takes tiles of 64 keys and values through LDS, two tiles deep: the next tile's loads are under way in registers while this
+// and takes tiles of 64 or 32 keys and values through LDS, two tiles deep: the next tile's loads are under way in registers while this
 // one is worked on.  With 8 heads a chip-wide row of 8 workgroups has one key/value head each, so that an XCD's L2 holds one
 // head's keys.  Units of a sequence are taken from its end: in a causal prompt the longest first.
 #include "attn.hpp"
 
 namespace skipffn {
 
-constexpr int FWD_KEYS = 64;
 
-// Workgroups that fit a compute unit at a time
-template <int DP> constexpr int fwd_per_cu() { return DP <= 64 ? 3 : 2; }
+// Workgroups a compute unit and keys a tile.  With pieces for all of them three workgroups (168 registers) do better than two, as some load
+// or store while others work; at 128 columns that leaves room for tiles of 32 keys.  64 keys and two workgroups / 32 and three, us:
+// 16 x 616 tokens 94 / 89, 32 x 200 45.8 / 40, 16 x up to 3080 729 / 711, 1 x 16384 2070 / 2110; but with fewer pieces than two a unit,
+// where a workgroup has its SIMDs to itself: 4 x 47 after 640 17.1 / 19.1.  64 columns, 64 keys and three / 32 and four: 8 x 577 25.4 / 26.6.
+template <int DP, int KEYS> constexpr int fwd_per_cu() { return DP <= 64 || KEYS == 32 ? 3 : 2; }
 
-template <int DP, bool PARTS>
-__global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel(const AttnArgs P, const int blocks) {
-    constexpr int TILE = FWD_KEYS * tile_row_bytes<DP>();
+template <int DP, int KEYS, bool PARTS>
+__global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fwd_kernel(const AttnArgs P, const int blocks) {
+    constexpr int KB = KEYS / 32, TILE = KEYS * tile_row_bytes<DP>(), ROWS = ATT_WAVES * 32 * tile_row_bytes<DP>();
     __shared__ __align__(256) char smem[4 * TILE];
+    static_assert(4 * TILE >= ROWS, "the rows of a piece leave by way of the tiles");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int g = P.Hq / P.Hkv;
     int kvh, turn = 0, part = 0;                         // part: of the keys
@@ -33,12 +36,12 @@ __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel
         }
         return locate_queries(P, unhoisted(lane), piece, g, to);
     };
-    const uint32_t k_off = TileLoad<DP, FWD_KEYS>::first(tid, P.k_tok, P.D), v_off = TileLoad<DP, FWD_KEYS>::first(tid, P.v_tok, P.D);
+    const uint32_t k_off = TileLoad<DP, KEYS>::first(tid, P.k_tok, P.D), v_off = TileLoad<DP, KEYS>::first(tid, P.v_tok, P.D);
     const uint32_t rows_at = lds_addr_of(smem) + rows_lane<DP>(lane), cols_at = lds_addr_of(smem) + TILE + cols_lane<DP>(lane);
-    TileLoad<DP, FWD_KEYS> lk, lv;
+    TileLoad<DP, KEYS> lk, lv;
     auto load_tile = [&](const SeqItem& s, int head, int t) {
-        lk.load(HeadRows{P.k + head * P.k_head + (int64_t)s.k0 * P.k_tok, P.k_tok}, t * FWD_KEYS, s.k1 - s.k0, P.D, k_off);
-        lv.load(HeadRows{P.v + head * P.v_head + (int64_t)s.k0 * P.v_tok, P.v_tok}, t * FWD_KEYS, s.k1 - s.k0, P.D, v_off);
+        lk.load(HeadRows{P.k + head * P.k_head + (int64_t)s.k0 * P.k_tok, P.k_tok}, t * KEYS, s.k1 - s.k0, P.D, k_off);
+        lv.load(HeadRows{P.v + head * P.v_head + (int64_t)s.k0 * P.v_tok, P.v_tok}, t * KEYS, s.k1 - s.k0, P.D, v_off);
     };
     bf16x8 qf[DP / 16];
     auto load_q = [&](const SeqItem& s, const QueryUnit& u) {
@@ -47,7 +50,7 @@ __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel
                       u.any && u.row0 + (ln & 31) < s.q1 - s.q0, P.D, ln, qf);
     };
     if (!locate(0, kvh, part, it)) return;
-    QueryUnit u = query_unit<FWD_KEYS>(P, it, kvh, wave, part, PARTS ? P.splits : 1);
+    QueryUnit u = query_unit<KEYS>(P, it, kvh, wave, part, PARTS ? P.splits : 1);
     load_q(it, u);
     if (u.t0 < u.t1) load_tile(it, kvh, u.t0);
     int stage = 0;                                       // which of the two tiles in LDS
@@ -55,7 +58,7 @@ __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel
         SeqItem next_it;
         int next_kvh = 0, next_part = 0;
         const bool more = locate(++turn, next_kvh, next_part, next_it);
-        const QueryUnit next = more ? query_unit<FWD_KEYS>(P, next_it, next_kvh, wave, next_part, PARTS ? P.splits : 1) : QueryUnit{};
+        const QueryUnit next = more ? query_unit<KEYS>(P, next_it, next_kvh, wave, next_part, PARTS ? P.splits : 1) : QueryUnit{};
         const int nq = it.q1 - it.q0, nk = it.k1 - it.k0, row = u.row0 + (lane & 31);
         const int row_keys = P.causal ? min(row + 1 + nk - nq, nk) : nk;
         f32x16 acc[DP / 32] = {};
@@ -69,37 +72,37 @@ __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel
             load_tile(next_it, next_kvh, next.t0);
         }
         auto work_on = [&](int t) {
-            if (t * FWD_KEYS >= u.wave_end) return;
+            if (t * KEYS >= u.wave_end) return;
             const uint32_t at = (uint32_t)stage * (2 * TILE), tk = rows_at + at, tv = cols_at + at;
             // Operands are asked for a few products ahead and the order is held (left to itself the compiler reads each right before its
             // product); products go before the other wavefront's exponentials.  1 x 16384 tokens 2127 -> 2030 us, 1 x 616 21.7 -> 17.8
-            f32x16 s[2];
-            constexpr int NK = DP / 16, AHEAD = 4;
+            f32x16 s[KB];
+            constexpr int NK = DP / 16, AHEAD = KB + 2;
             {
                 bf16x8 kf[AHEAD];
 #pragma unroll
                 for (int i = 0; i < AHEAD; ++i) kf[i] = frag_rows<DP>(tk, i / NK * 32, i % NK);
                 __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-                for (int i = 0; i < 2 * NK; ++i) {
+                for (int i = 0; i < KB * NK; ++i) {
                     __builtin_amdgcn_sched_barrier(0);
                     if (i % NK == 0) s[i / NK] = f32x16{};
                     s[i / NK] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i % AHEAD], qf[i % NK], s[i / NK], 0, 0, 0);
-                    if (i + AHEAD < 2 * NK) kf[i % AHEAD] = frag_rows<DP>(tk, (i + AHEAD) / NK * 32, (i + AHEAD) % NK);
+                    if (i + AHEAD < KB * NK) kf[i % AHEAD] = frag_rows<DP>(tk, (i + AHEAD) / NK * 32, (i + AHEAD) % NK);
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 __builtin_amdgcn_s_setprio(0);
             }
-            if ((t + 1) * FWD_KEYS > u.all_see) {
+            if ((t + 1) * KEYS > u.all_see) {
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
+                for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
-                        if (t * FWD_KEYS + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= row_keys) s[kb][i] = -INFINITY;
+                        if (t * KEYS + kb * 32 + 8 * (i >> 2) + 4 * h + (i & 3) >= row_keys) s[kb][i] = -INFINITY;
             }
             float top = s[0][0];
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+            for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
             top = halves_max(top);
@@ -119,7 +122,7 @@ __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel
                 s[kb][i] = __builtin_amdgcn_exp2f(fmaf(s[kb][i], c, -mc));
                 l += s[kb][i];
             };
-            constexpr int NV = DP / 32, VAHEAD = 3, STEPS = 4 * NV;
+            constexpr int NV = DP / 32, VAHEAD = KB + 1, STEPS = 2 * KB * NV;
             bf16x8 vf[VAHEAD], pf;
 #pragma unroll
             for (int i = 0; i < VAHEAD; ++i) vf[i] = frag_cols<DP>(tv, i / NV * 16, i % NV);
@@ -132,7 +135,7 @@ __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel
                 if (i % NV == 0) pf = pack_frag(s[i / NV >> 1], i / NV & 1);
                 acc[i % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % VAHEAD], pf, acc[i % NV], 0, 0, 0);
                 if (i + VAHEAD < STEPS) vf[i % VAHEAD] = frag_cols<DP>(tv, (i + VAHEAD) / NV * 16, (i + VAHEAD) % NV);
-                if (i < 3 * NV) {
+                if (i < (2 * KB - 1) * NV) {
 #pragma unroll
                     for (int j = 0; j < 8 / NV; ++j) { const int w = 8 + i * (8 / NV) + j; weight(w >> 4, w & 15); }
                 }
@@ -152,6 +155,7 @@ __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel
             if (next.t0 < next.t1) load_tile(next_it, next_kvh, next.t0);
             work_on(u.t1 - 1);
         }
+        if constexpr (2 * TILE < ROWS) __syncthreads();  // otherwise the rows fit the tile that no wavefront reads any more
         if (more) load_q(next_it, next);
         l = halves_sum(l);
         if (PARTS && u.any) {
@@ -170,9 +174,8 @@ __global__ __launch_bounds__(ATT_THREADS, fwd_per_cu<DP>()) void attn_fwd_kernel
             }
         } else if (u.any) {
             const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // a row that sees no key is zero
-            // by way of the tile that no wavefront reads any more
             store_rows<DP>(P.out + u.head * P.o_head + (int64_t)(it.q0 + u.row0) * P.o_tok, P.o_tok, min(nq - u.row0, ATT_ROWS), acc, inv, P.D,
-                           unhoisted(lane), smem + (stage ^ 1) * 2 * TILE + wave * 32 * tile_row_bytes<DP>());
+                           unhoisted(lane), smem + (2 * TILE < ROWS ? 0 : (stage ^ 1) * 2 * TILE) + wave * 32 * tile_row_bytes<DP>());
             if (P.lse != nullptr && h == 0 && row < nq)
                 P.lse[(int64_t)u.head * P.Tq + it.q0 + row] = l == 0.0f ? INFINITY : fmaf(m, c, __builtin_amdgcn_logf(l));
         }
@@ -192,7 +195,7 @@ int attn_forward_splits(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64
     AttnArgs a{};
     a.Tq = (int)Tq; a.n_seq = (int)n_seq; a.Hq = (int)Hq; a.Hkv = (int)Hkv;
     const int64_t blocks = attn_query_workgroups(a), fit = (int64_t)ncu * 2;
-    const double tiles = (double)Tk / (double)n_seq / FWD_KEYS, row_us = (double)Tq * (double)Hq * (attn_padded_columns((int)D) * 8) / 4e6;
+    const double tiles = (double)Tk / (double)n_seq / 64.0, row_us = (double)Tq * (double)Hq * (attn_padded_columns((int)D) * 8) / 4e6;
     int best = 1;
     double least = tiles * 1.2;
     for (int n = 2; n <= 16 && n <= tiles && blocks * n <= fit; ++n) {
@@ -202,14 +205,19 @@ int attn_forward_splits(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64
     return best;
 }
 
+template <int DP, int KEYS, bool PARTS>
+static void launch_fwd(const AttnArgs& a, int64_t blocks, int ncu, hipStream_t s) {
+    const int64_t fit = (int64_t)ncu * fwd_per_cu<DP, KEYS>() / 8 * 8;
+    attn_fwd_kernel<DP, KEYS, PARTS><<<dim3((uint32_t)(blocks < fit ? blocks : fit)), ATT_THREADS, 0, s>>>(a, (int)blocks);
+}
+
 hipError_t launch_attn_forward(const AttnArgs& a, int ncu, hipStream_t s) {
     const int64_t blocks = attn_query_workgroups(a) * a.splits;
-    const int64_t fit = (int64_t)ncu * (a.D <= 64 ? fwd_per_cu<64>() : fwd_per_cu<128>()) / 8 * 8;
-    const dim3 grid((uint32_t)(blocks < fit ? blocks : fit));
-    if (a.splits == 1 && a.D <= 64) attn_fwd_kernel<64, false><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
-    else if (a.splits == 1) attn_fwd_kernel<128, false><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
-    else if (a.D <= 64) attn_fwd_kernel<64, true><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
-    else attn_fwd_kernel<128, true><<<grid, ATT_THREADS, 0, s>>>(a, (int)blocks);
+    if (a.D <= 64 && a.splits > 1) launch_fwd<64, 64, true>(a, blocks, ncu, s);
+    else if (a.D <= 64) launch_fwd<64, 64, false>(a, blocks, ncu, s);
+    else if (a.splits > 1) launch_fwd<128, 64, true>(a, blocks, ncu, s);
+    else if (blocks <= 2 * ncu) launch_fwd<128, 64, false>(a, blocks, ncu, s);
+    else launch_fwd<128, 32, false>(a, blocks, ncu, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     AttnJoinArgs j{};
