@@ -145,31 +145,6 @@ __device__ __forceinline__ void store_rows(bf16_t* base, int stride, int rows, c
 }
 
 // ---- which sequence a workgroup works on ---------------------------------------------------------------
-// Set s has items(its length) workgroups; workgroup q of all -> s, its index among the set's, and the set's bounds, which
-// bounds(s, b, e) gives.  False past the last one.  A lane takes a set, a prefix sum over the lanes finds the workgroup's (whole
-// wavefronts).
-template <class Bounds, class Items>
-__device__ __forceinline__ bool locate_in(int S, int q, const Bounds& bounds, const Items& items, int& s, int& item, int& t0, int& t1) {
-    const int lane = threadIdx.x & 63;
-    int cc = 0;
-    for (int i0 = 0; i0 < S; i0 += 64) {
-        int b = 0, e = 0;
-        if (i0 + lane < S) bounds(i0 + lane, b, e);
-        const int nc = items(e - b);
-        const int incl = wave_inclusive_sum(nc);
-        const uint64_t past = __ballot(q < cc + incl);
-        if (past != 0) {
-            const int l = __builtin_ctzll(past);
-            t0 = __builtin_amdgcn_readlane(b, l);
-            t1 = __builtin_amdgcn_readlane(e, l);
-            s = i0 + l;
-            item = q - cc - __builtin_amdgcn_readlane(incl - nc, l);
-            return true;
-        }
-        cc += __builtin_amdgcn_readlane(incl, 63);
-    }
-    return false;
-}
 // The workgroups of a kernel over packed sequences, the longest first whatever sequence they belong to: the last ones to start are
 // the shortest, and the chip empties evenly.  Workgroup j of a sequence has the level top - j num / den (rounded down), in
 // 32s of rows that it goes over (num = 0: all the same), so that cnt(L) = ceil((top - L + 1) den / num) of a sequence's have at least L; a search over L finds

@@ -25,22 +25,41 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnD
     int b = (int)blockIdx.x;
     const int kvh = b % P.Hkv; b /= P.Hkv;
     const int hb = b % head_blocks; b /= head_blocks;
-    int group, item, s0, s1;
-    if (!locate_in(P.n_groups + 1, b,
-                   [&](int i, int& lo, int& hi) {
-                       if (i < P.n_groups) { seg_bounds(P.group_off, i, P.n_seq, lo, hi); return; }
-                       hi = P.n_seq;                                             // those of no group
-                       lo = P.n_groups > 0 ? min(max(P.group_off[P.n_groups], 0), P.n_seq) : 0;
-                   },
-                   [&](int n) { return (n + members - 1) / members; }, group, item, s0, s1))
-        return;
-    s0 += item * members;
-    const int ns = min(s1 - s0, members), heads = min(g - hb * 32, 32), rows = ns * heads;
-    int p0 = 0, p1 = 0;
-    if (group < P.n_groups && P.Tp > 0) seg_bounds(P.prefix_seg, group, P.Tp, p0, p1);
+    // Which sequences: a lane takes a group (the one past the last: the sequences of none), a prefix sum over the lanes finds the workgroup's.
+    // What depends on the group is loaded with its bounds, and so are the lengths if a wavefront holds them all: one latency, not three.
+    const bool few = P.n_seq <= 64;
+    const int all_own = few && lane < P.n_seq && P.cap > 0 ? P.suffix_len[lane] : 0;
+    int s0 = 0, ns = 0, p0 = 0, p1 = 0;
+    for (int i0 = 0, before = 0; i0 <= P.n_groups; i0 += 64) {
+        const int i = i0 + lane;
+        int lo = 0, hi = 0, pb = 0, pe = 0;
+        if (i < P.n_groups) {
+            seg_bounds(P.group_off, i, P.n_seq, lo, hi);
+            if (P.Tp > 0) seg_bounds(P.prefix_seg, i, P.Tp, pb, pe);
+        } else if (i == P.n_groups) {
+            lo = P.n_groups > 0 ? min(max(P.group_off[P.n_groups], 0), P.n_seq) : 0;
+            hi = P.n_seq;
+        }
+        const int n = (hi - lo + members - 1) / members, incl = wave_inclusive_sum(n);
+        const uint64_t past = __ballot(b < before + incl);
+        if (past != 0) {
+            const int l = __builtin_ctzll(past);
+            s0 = __builtin_amdgcn_readlane(lo, l) + (b - before - __builtin_amdgcn_readlane(incl - n, l)) * members;
+            ns = min(__builtin_amdgcn_readlane(hi, l) - s0, members);
+            p0 = __builtin_amdgcn_readlane(pb, l);
+            p1 = __builtin_amdgcn_readlane(pe, l);
+            break;
+        }
+        before += __builtin_amdgcn_readlane(incl, 63);
+    }
+    if (ns == 0) return;
+    const int heads = min(g - hb * 32, 32), rows = ns * heads;
     const int prefix_tiles = (p1 - p0 + DEC_KEYS - 1) / DEC_KEYS;
     // lane i: own keys of sequence s0 + i and the tiles up to it
-    const int own_keys = lane < ns && P.cap > 0 ? min(max(P.suffix_len[s0 + lane], 0), P.cap) : 0;
+    int own_keys = 0;
+    if (few) own_keys = __shfl(all_own, s0 + lane, 64);
+    else if (lane < ns && P.cap > 0) own_keys = P.suffix_len[s0 + lane];
+    own_keys = lane < ns ? min(max(own_keys, 0), P.cap) : 0;
     const int own_tiles = (own_keys + DEC_KEYS - 1) / DEC_KEYS, own_sum = wave_inclusive_sum(own_tiles);
     const int tiles = prefix_tiles + __builtin_amdgcn_readlane(own_sum, 63);
     const int z = (int)blockIdx.y;
