@@ -7,7 +7,8 @@
 //                               free, so V^T is read in the order of keys that the lane holds.
 // Row maxima and sums then stay inside a lane but for one exchange with the lane 32 further.
 //
-// A tile of rows [token][column] of one head lies in LDS with 256 (128) bytes a row for heads of up to 128 (64) columns, 16-byte
+// A kernel for 64, 96 or 128 columns serves heads of up to as many.  A tile of rows [token][column] of one head lies in LDS with 128 bytes a
+// row (64 columns) or 256, 16-byte
 // chunk c of row r at c ^ tile_swz(r).  The same placing serves both ways it is read, free of bank conflicts: 16 consecutive rows
 // at one chunk (ds_read_b128, the operand whose contraction runs along the columns) and 4 rows x 64 bytes (ds_read_b64_tr_b16, the
 // operand whose contraction runs along the tokens).

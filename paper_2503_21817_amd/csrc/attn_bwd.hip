@@ -34,6 +34,13 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dq_kernel(
     const bool row_ok = unit >= 0 && row < nq;
     const int row_keys = keys_of(row);
 
+    const HeadRows K{P.k + kvh * P.k_head + (int64_t)k0 * P.k_tok, P.k_tok}, V{P.v + kvh * P.v_head + (int64_t)k0 * P.v_tok, P.v_tok};
+    const uint32_t k_off = TileLoad<DP, DQ_KEYS>::first(tid, P.k_tok, P.D), v_off = TileLoad<DP, DQ_KEYS>::first(tid, P.v_tok, P.D);
+    TileLoad<DP, DQ_KEYS> lk, lv;
+    if (tiles > 0) {
+        lk.load(K, 0, nk, P.D, k_off);
+        lv.load(V, 0, nk, P.D, v_off);
+    }
     bf16x8 qf[DP / 16], gf[DP / 16];
     float delta = 0.0f, lse = INFINITY;
     {
@@ -54,15 +61,10 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dq_kernel(
         delta = halves_sum(delta);
         if (row_ok) lse = P.lse[(int64_t)head * P.Tq + q0 + row];
     }
-    const HeadRows K{P.k + kvh * P.k_head + (int64_t)k0 * P.k_tok, P.k_tok}, V{P.v + kvh * P.v_head + (int64_t)k0 * P.v_tok, P.v_tok};
-    const uint32_t k_off = TileLoad<DP, DQ_KEYS>::first(tid, P.k_tok, P.D), v_off = TileLoad<DP, DQ_KEYS>::first(tid, P.v_tok, P.D);
-    TileLoad<DP, DQ_KEYS> lk, lv;
     const uint32_t rows_at = lds_addr_of(smem) + rows_lane<DP>(lane), cols_at = lds_addr_of(smem) + cols_lane<DP>(lane);
     f32x16 acc[DP / 32] = {};
     const float c = P.scale_log2;
     if (tiles > 0) {
-        lk.load(K, 0, nk, P.D, k_off);
-        lv.load(V, 0, nk, P.D, v_off);
         lk.store(smem, tid);
         lv.store(smem + TILE, tid);
     }
@@ -100,14 +102,27 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dq_kernel(
             const int key0 = t * DQ_KEYS + kb * 32;
             if (key0 >= wave_end) continue;
             f32x16 s = {}, dp = {};
+            constexpr int AHEAD = 3;
+            bf16x8 f[AHEAD];
+            auto operand = [&](int i) { return frag_rows<DP>(i < N ? tk : tv, kb * 32, i % N); };
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) f[i] = operand(i);
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-            for (int d = 0; d < N; ++d) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tk, kb * 32, d), qf[d], s, 0, 0, 0);
+            for (int i = 0; i < 2 * N; ++i) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (i < N) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], qf[i], s, 0, 0, 0);
+                else dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], gf[i - N], dp, 0, 0, 0);
+                if (i + AHEAD < 2 * N) f[i % AHEAD] = operand(i + AHEAD);
+                if (i >= N) {
 #pragma unroll
-            for (int d = 0; d < N; ++d) dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(tv, kb * 32, d), gf[d], dp, 0, 0, 0);
+                    for (int e = (i - N) * 16 / N; e < (i - N + 1) * 16 / N; ++e) s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -lse));
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -lse)) * (dp[i] - delta);
+            for (int i = 0; i < 16; ++i) s[i] *= dp[i] - delta;
             if (key0 + 32 > all_see) {
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
@@ -168,13 +183,18 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dkv_kernel
     TileLoad<DP, DKV_ROWS> lq, lg;
     const float* row_stat = (wave & 1) != 0 ? G.delta : P.lse;       // the first wavefront loads the log-sum-exps, the second delta
     float stat = 0.0f;
-    auto load = [&](int n) {
-        const int head = kvh * g + n / row_tiles, r0 = (row_first + row_tiles - 1 - n % row_tiles) * DKV_ROWS;
+    // step by step through the tiles of rows, the last first, head by head: of the next load, and of the tile in work
+    const int r_last = (row_first + row_tiles - 1) * DKV_ROWS, r_first = row_first * DKV_ROWS;
+    int head = kvh * g, load_r0 = r_last, r0 = r_last;
+    auto load = [&]() {
+        const int r0 = load_r0;
         lq.load(HeadRows{P.q + head * P.q_head + (int64_t)q0 * P.q_tok, P.q_tok}, r0, nq, P.D, q_off);
         lg.load(HeadRows{G.go + head * G.go_head + (int64_t)q0 * G.go_tok, G.go_tok}, r0, nq, P.D, g_off);
         // rows past the sequence's read 0: with q and grad_out of 0 they give weights of 1 on gradients of 0
         const __amdgpu_buffer_rsrc_t rs = make_rsrc(row_stat + (int64_t)head * P.Tq + q0 + r0, (uint32_t)min(nq - r0, DKV_ROWS) * 4u);
         stat = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, lane * 4, 0, 0));
+        load_r0 -= DKV_ROWS;
+        if (load_r0 < r_first) { load_r0 = r_last; ++head; }
     };
     auto store = [&](int n) {
         char* st = stage + (n & 1) * STAGE;
@@ -187,15 +207,14 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dkv_kernel
     f32x16 dk[DP / 32] = {}, dv[DP / 32] = {};
     const float c = P.scale_log2;
     if (steps > 0) {
-        load(0);
+        load();
         store(0);
     }
     __syncthreads();
     for (int n = 0; n < steps; ++n) {
         const uint32_t at = (uint32_t)(n & 1) * STAGE, tq = rows_at + at, tg = tq + TILE, tqc = cols_at + at, tgc = tqc + TILE;
         const float* st = reinterpret_cast<const float*>(stage + at + 2 * TILE);
-        if (n + 1 < steps) load(n + 1);
-        const int r0 = (row_first + row_tiles - 1 - n % row_tiles) * DKV_ROWS;
+        if (n + 1 < steps) load();
         auto work_on = [&]() {
             // Four times N products: scores, dP, dV, dK.  Operands are asked for AHEAD products before, the order is held, and the weights
             // lie beside dP's products, dS beside dV's.
@@ -233,7 +252,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dkv_kernel
                 if (i + AHEAD < 4 * N) f[i % AHEAD] = operand(i + AHEAD);
                 if (i >= N - VAHEAD && i < 2 * N - VAHEAD) vf[(i + VAHEAD) % VAHEAD] = frag_rows<DP>(v_at, 0, i + VAHEAD - N);
 #pragma unroll
-                for (int e = j * (16 / N); e < (j + 1) * (16 / N); ++e) {
+                for (int e = j * 16 / N; e < (j + 1) * 16 / N; ++e) {
                     if (phase == 1) {
                         if (e % 4 == 0) row4 = four(8 * (e / 4));
                         s[e] = __builtin_amdgcn_exp2f(fmaf(s[e], c, -row4[e % 4]));
@@ -253,6 +272,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dkv_kernel
         }
         if (n + 1 < steps) store(n + 1);
         __syncthreads();
+        r0 = r0 == r_first ? r_last : r0 - DKV_ROWS;
     }
     if (key0 < nk) {
         char* rows = stage + wave * 32 * ROWB;           // every wavefront has read the last step's tiles
@@ -265,10 +285,12 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dkv_kernel
 hipError_t launch_attn_backward(const AttnArgs& a, const AttnGrads& gr, hipStream_t s) {
     const dim3 gq((uint32_t)attn_query_workgroups(a)), gk((uint32_t)(((int64_t)a.Tk / DKV_KEYS + a.n_seq) * a.Hkv));
     if (a.D <= 64) attn_dq_kernel<64><<<gq, ATT_THREADS, 0, s>>>(a, gr);
+    else if (a.D <= 96) attn_dq_kernel<96><<<gq, ATT_THREADS, 0, s>>>(a, gr);
     else attn_dq_kernel<128><<<gq, ATT_THREADS, 0, s>>>(a, gr);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (a.D <= 64) attn_dkv_kernel<64><<<gk, ATT_THREADS, 0, s>>>(a, gr);
+    else if (a.D <= 96) attn_dkv_kernel<96><<<gk, ATT_THREADS, 0, s>>>(a, gr);
     else attn_dkv_kernel<128><<<gk, ATT_THREADS, 0, s>>>(a, gr);
     return hipGetLastError();
 }

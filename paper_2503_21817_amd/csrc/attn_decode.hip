@@ -179,19 +179,16 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnD
             P.stat[2 * at + 1] = sum;
         }
 #pragma unroll
-        for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(P.part + at * DP + jd + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
+        for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(P.part + at * attn_padded_columns(DP) + jd + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
         return;
     }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;   // a row that sees no key is zero
     bf16_t* out = P.out + (int64_t)seq * P.o_tok + hq * P.o_head;
 #pragma unroll
-    for (int j = 0; j < PER; j += 8)
-        if (jd + j < P.D) {
-            u32x4 v;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = pack_bf16x2(o[j + 2 * i] * inv, o[j + 2 * i + 1] * inv);
-            *reinterpret_cast<u32x4*>(out + jd + j) = v;
-        }
+    for (int j = 0; j < PER; j += 4)
+        if (jd + j < P.D)
+            *reinterpret_cast<u32x2*>(out + jd + j) =
+                u32x2{pack_bf16x2(o[j] * inv, o[j + 1] * inv), pack_bf16x2(o[j + 2] * inv, o[j + 3] * inv)};
 }
 
 namespace {
@@ -217,6 +214,7 @@ int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv,
 hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s) {
     const dim3 grid((uint32_t)decode_blocks(a.n_seq, a.n_groups, a.Hq, a.Hkv), (uint32_t)a.splits);
     if (a.D <= 64) attn_decode_kernel<64><<<grid, ATT_THREADS, 0, s>>>(a);
+    else if (a.D <= 96) attn_decode_kernel<96><<<grid, ATT_THREADS, 0, s>>>(a);
     else attn_decode_kernel<128><<<grid, ATT_THREADS, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;

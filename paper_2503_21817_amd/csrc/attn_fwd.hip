@@ -137,7 +137,7 @@ __global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fw
                 if (i + VAHEAD < STEPS) vf[i % VAHEAD] = frag_cols<DP>(tv, (i + VAHEAD) / NV * 16, (i + VAHEAD) % NV);
                 if (i < (2 * KB - 1) * NV) {
 #pragma unroll
-                    for (int j = 0; j < 8 / NV; ++j) { const int w = 8 + i * (8 / NV) + j; weight(w >> 4, w & 15); }
+                    for (int w = 8 + i * 8 / NV; w < 8 + (i + 1) * 8 / NV; ++w) weight(w >> 4, w & 15);
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fw
                 for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<f32x4*>(P.part + at * DP + db * 32 + 8 * i + 4 * h) =
+                        *reinterpret_cast<f32x4*>(P.part + at * attn_padded_columns(DP) + db * 32 + 8 * i + 4 * h) =
                             f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]};
             }
         } else if (u.any) {
@@ -215,8 +215,11 @@ hipError_t launch_attn_forward(const AttnArgs& a, int ncu, hipStream_t s) {
     const int64_t blocks = attn_query_workgroups(a) * a.splits;
     if (a.D <= 64 && a.splits > 1) launch_fwd<64, 64, true>(a, blocks, ncu, s);
     else if (a.D <= 64) launch_fwd<64, 64, false>(a, blocks, ncu, s);
+    else if (a.splits > 1 && a.D <= 96) launch_fwd<96, 64, true>(a, blocks, ncu, s);
     else if (a.splits > 1) launch_fwd<128, 64, true>(a, blocks, ncu, s);
+    else if (blocks <= 2 * ncu && a.D <= 96) launch_fwd<96, 64, false>(a, blocks, ncu, s);
     else if (blocks <= 2 * ncu) launch_fwd<128, 64, false>(a, blocks, ncu, s);
+    else if (a.D <= 96) launch_fwd<96, 32, false>(a, blocks, ncu, s);
     else launch_fwd<128, 32, false>(a, blocks, ncu, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;

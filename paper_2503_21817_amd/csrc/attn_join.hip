@@ -60,8 +60,6 @@ __global__ __launch_bounds__(ATT_THREADS) void attn_join_kernel(const AttnJoinAr
     else *out = f32_to_bf16(o[0] * inv);
 }
 
-int attn_padded_columns(int D) { return D <= 64 ? 64 : 128; }
-
 hipError_t launch_attn_join(const AttnJoinArgs& a, hipStream_t s) {
     const uint32_t wgs = (uint32_t)(((int64_t)a.T * a.Hq + ATT_WAVES - 1) / ATT_WAVES);
     if (a.D <= 64) attn_join_kernel<64><<<wgs, ATT_THREADS, 0, s>>>(a);

@@ -192,7 +192,7 @@ struct AttnJoinArgs {
     float* lse;                                   // or null
     const int32_t* seg; int n_seq;                // null: every row; otherwise rows of the n_seq sequences, others are left as they were
 };
-int attn_padded_columns(int D);                   // columns of a row of part
+constexpr __host__ __device__ int attn_padded_columns(int D) { return D <= 64 ? 64 : 128; }   // of a row of part
 hipError_t launch_attn_join(const AttnJoinArgs& a, hipStream_t s);
 struct AttnGrads {
     const bf16_t* go; int go_tok; int64_t go_head;
