@@ -825,7 +825,7 @@ int check_attn(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, i
     if (Tq < 0 || Tk < 0 || n_seq < 0 || Hq <= 0 || Hkv <= 0 || D <= 0 || !(scale > 0.0f) || !std::isfinite(scale)) return SKIPFFN_EINVAL;
     if (Hq % Hkv != 0 || (D & 7) || D > ATTN_MAX_D || n_seq > 65535 || Hq > 65535 || Tq >= (1 << 30) || Tk >= (1 << 30)) return SKIPFFN_ESHAPE;
     // a grid of workgroups by queries, one by keys, as launch_attn_* form them
-    if ((Tq / 32 + 2 * n_seq) * Hq >= (1ll << 31) || (Tk / 32 + 2 * n_seq) * Hkv >= (1ll << 31)) return SKIPFFN_ESHAPE;
+    if ((Tq / 32 + 2 * n_seq) * Hq >= (1ll << 30) || (Tk / 32 + 2 * n_seq) * Hkv >= (1ll << 30)) return SKIPFFN_ESHAPE;
     return SKIPFFN_OK;
 }
 // bytes from the first element to past the last one
@@ -959,7 +959,7 @@ int check_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64
     if (n_groups < 0 || cap < 0) return SKIPFFN_EINVAL;
     const int st = check_attn(n_seq, Tp, n_groups, Hq, Hkv, D, scale);
     if (st != SKIPFFN_OK) return st;
-    if (n_groups > 65534 || cap >= (1 << 30) || (n_seq + n_groups + 1) * Hq >= (1ll << 31)) return SKIPFFN_ESHAPE;
+    if (n_groups > 65534 || cap >= (1 << 30) || (n_seq + n_groups + 1) * Hq >= (1ll << 30)) return SKIPFFN_ESHAPE;
     return SKIPFFN_OK;
 }
 }  // namespace

@@ -61,6 +61,25 @@ struct TileLoad {
         for (int i = 0; i < PER; ++i)
             v[i] = __builtin_amdgcn_raw_buffer_load_b128(r, (int)(off + (uint32_t)(i * (THREADS / CH) * h.stride) * 2u), 0, 0);
     }
+    // whether the thread holds an infinity or a NaN: an exponent of ones, the largest of all as unsigned 16-bit halves
+    __device__ __forceinline__ bool any_not_finite() const {
+        typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+        u16x2 top = {0, 0};
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, v[i][j] & 0x7fff7fffu));
+        return top[0] >= 0x7f80 || top[1] >= 0x7f80;
+    }
+    __device__ __forceinline__ void drop_not_finite() {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t x = v[i][j];
+                v[i][j] = ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u) | ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu);
+            }
+    }
     __device__ __forceinline__ void store(char* tile, int tid) const {
 #pragma unroll
         for (int i = 0; i < PER; ++i)

@@ -14,7 +14,7 @@ namespace skipffn {
 constexpr int DEC_KEYS = 32;
 
 template <int DP>
-__global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnDecodeArgs P) {
+__global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_kernel(const AttnDecodeArgs P) {
     constexpr int ROWB = tile_row_bytes<DP>(), TILE = DEC_KEYS * ROWB;
     static_assert(2 * TILE >= DP * 32 * 4, "a wavefront's sums fit where its tiles were");
     __shared__ __align__(256) char smem[ATT_WAVES * 2 * TILE];
@@ -78,6 +78,12 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnD
     const uint32_t sk_off = Load::first(lane, P.sk_tok, P.D), sv_off = Load::first(lane, P.sv_tok, P.D);
     Load lk, lv;
     int next_keys = 0, next_of = -1;                     // of the tile under way: its keys, and whose they are (-1: all rows')
+    bool dropped = false;
+    auto own_tile = [&](int u, int& i, int& k0, int& n) {    // member, first key, its keys
+        i = __builtin_ctzll(__ballot(u < own_sum));
+        k0 = (u - __builtin_amdgcn_readlane(own_sum - own_tiles, i)) * DEC_KEYS;
+        n = __builtin_amdgcn_readlane(own_keys, i);
+    };
     auto load = [&](int t) {
         if (t < prefix_tiles) {
             next_of = -1;
@@ -85,8 +91,8 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnD
             lk.load(HeadRows{P.pk + kvh * P.pk_head + (int64_t)p0 * P.pk_tok, P.pk_tok}, t * DEC_KEYS, p1 - p0, P.D, pk_off);
             lv.load(HeadRows{P.pv + kvh * P.pv_head + (int64_t)p0 * P.pv_tok, P.pv_tok}, t * DEC_KEYS, p1 - p0, P.D, pv_off);
         } else {
-            const int u = t - prefix_tiles, i = __builtin_ctzll(__ballot(u < own_sum));
-            const int k0 = (u - __builtin_amdgcn_readlane(own_sum - own_tiles, i)) * DEC_KEYS, n = __builtin_amdgcn_readlane(own_keys, i);
+            int i, k0, n;
+            own_tile(t - prefix_tiles, i, k0, n);
             next_of = i;
             next_keys = min(n - k0, DEC_KEYS);
             lk.load(HeadRows{P.sk + (s0 + i) * P.sk_seq + kvh * P.sk_head, P.sk_tok}, k0, n, P.D, sk_off);
@@ -99,16 +105,31 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnD
     if (t_first < t_end) load(t_first);
     for (int t = t_first; t < t_end; t += ATT_WAVES) {
         const int keys = next_keys;
-        const bool sees = next_of < 0 || member == next_of;
         // a wavefront's LDS operations are done in order: its last tile has been read
+        // Own rows of one sequence come to the others' with weight 0, which would make a NaN of an infinity or a NaN: these leave the tile,
+        // and are added to the rows that see them at the end
+        if (next_of >= 0 && ns > 1 && __ballot(lv.any_not_finite()) != 0) {
+            lv.drop_not_finite();
+            dropped = true;
+        }
+        const bool sees = next_of < 0 || member == next_of;
         lk.store(tk, lane);
         lv.store(tv, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         if (t + ATT_WAVES < t_end) load(t + ATT_WAVES);
+        // operands a few products ahead of them and the order held, as in the kernels over whole prompts
+        constexpr int N = DP / 16, NV = DP / 32, AHEAD = 3, VAHEAD = 2;
         f32x16 s = {};
+        bf16x8 f[AHEAD], vf[VAHEAD], p = {};
 #pragma unroll
-        for (int d = 0; d < DP / 16; ++d)
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_rows<DP>(rows_at, 0, d), qf[d], s, 0, 0, 0);
+        for (int i = 0; i < AHEAD; ++i) f[i] = frag_rows<DP>(rows_at, 0, i);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[i % AHEAD], qf[i], s, 0, 0, 0);
+            if (i + AHEAD < N) f[i % AHEAD] = frag_rows<DP>(rows_at, 0, i + AHEAD);
+        }
+        __builtin_amdgcn_sched_barrier(0);
         if (keys < DEC_KEYS) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -128,19 +149,48 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_decode_kernel(const AttnD
             m = now;
         }
         const float mc = m == -INFINITY ? 0.0f : m * c;
+        auto weights = [&](int i0) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s[i] = sees ? __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc)) : 0.0f;
-            l += s[i];
+            for (int i = i0; i < i0 + 8; ++i) {
+                s[i] = sees ? __builtin_amdgcn_exp2f(fmaf(s[i], c, -mc)) : 0.0f;
+                l += s[i];
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < VAHEAD; ++i) vf[i] = frag_cols<DP>(cols_at, i / NV * 16, i % NV);
+        weights(0);
+#pragma unroll
+        for (int i = 0; i < 2 * NV; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (i % NV == 0) p = pack_frag(s, i / NV);
+            acc[i % NV] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i % VAHEAD], p, acc[i % NV], 0, 0, 0);
+            if (i + VAHEAD < 2 * NV) vf[i % VAHEAD] = frag_cols<DP>(cols_at, (i + VAHEAD) / NV * 16, (i + VAHEAD) % NV);
+            if (i == 0) weights(8);
         }
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const bf16x8 p = pack_frag(s, k);
-#pragma unroll
-            for (int db = 0; db < DP / 32; ++db)
-                acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag_cols<DP>(cols_at, k * 16, db), p, acc[db], 0, 0, 0);
-        }
+        __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    if (dropped) {
+        for (int t = t_first; t < t_end; t += ATT_WAVES) {
+            const int u = t - prefix_tiles;
+            if (u < 0) continue;
+            int i, k0, n;
+            own_tile(u, i, k0, n);
+            const bf16_t* v = P.sv + (s0 + i) * P.sv_seq + kvh * P.sv_head + (int64_t)k0 * P.sv_tok;
+            for (int j = min(n - k0, DEC_KEYS); j > 0; --j, v += P.sv_tok)
+#pragma unroll
+                for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int d = db * 32 + 8 * q + 4 * h;
+                        const u32x2 x = d < P.D ? *reinterpret_cast<const u32x2*>(v + d) : u32x2{0, 0};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float f = (e & 1) != 0 ? bf16hi_to_f32(x[e >> 1]) : bf16lo_to_f32(x[e >> 1]);
+                            acc[db][4 * q + e] += member == i && !(fabsf(f) < INFINITY) ? f : 0.0f;
+                        }
+                    }
+        }
     }
     // join the wavefronts: [column][row] of each where its tiles were
     l = halves_sum(l);

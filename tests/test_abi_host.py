@@ -267,3 +267,139 @@ def test_buffer_sizes_grow_with_the_row_bound():
                lib.skipffn_backward_workspace_bytes(R, C, I), lib.skipffn_saved_bytes(R, C, I))
         assert all(c >= p for c, p in zip(cur, prev)), (R, cur, prev)
         prev = cur
+
+
+# ---- attention ---------------------------------------------------------------------------------------
+def heads(data=FAKE, token=None, head=64, H=4):
+    """skipffn_heads of a tensor [tokens, H, 64], as an array that ctypes passes by address"""
+    token = H * head if token is None else token
+    return ctypes.addressof(_keep((ctypes.c_int64 * 3)(data or 0, token, head)))
+
+
+_alive = []
+
+
+def _keep(a):
+    _alive.append(a)
+    return a
+
+
+FAR = [FAKE + (i << 32) for i in range(12)]           # memory ranges that do not meet
+
+
+def attn_fwd(Tq=64, Tk=64, n=1, Hq=4, Hkv=4, D=64, q=None, k=None, v=None, out=None, sq=FAKE, sk=None, scale=0.125, saved=None,
+             ws=None, ws_bytes=0):
+    t = [x if x is not None else heads(FAR[i]) for i, x in enumerate((q, k, v, out))]
+    return B.lib().skipffn_attn_forward(Tq, Tk, n, Hq, Hkv, D, *t, sq, sk, 1, scale, saved, ws, ws_bytes, None)
+
+
+def attn_bwd(Tq=64, Tk=64, n=1, Hq=4, Hkv=4, D=64, t=None, sq=FAKE, sk=None, scale=0.125, saved=FAKE, ws=FAKE, ws_bytes=1 << 40):
+    t = {**{i: heads(FAR[i]) for i in range(8)}, **(t or {})}
+    return B.lib().skipffn_attn_backward(Tq, Tk, n, Hq, Hkv, D, *(t[i] for i in range(5)), sq, sk, 1, scale, saved, t[5], t[6], t[7],
+                                         ws, ws_bytes, None)
+
+
+def attn_dec(n=4, G=1, Hq=4, Hkv=4, D=64, Tp=64, cap=64, t=None, seg=FAKE, off=FAKE, ks=1 << 14, vs=1 << 14, lens=FAKE, scale=0.125,
+             ws=FAKE, ws_bytes=1 << 40):
+    t = {**{i: heads(FAR[i]) for i in range(6)}, **(t or {})}      # q, prefix k, v, own k, v, out
+    return B.lib().skipffn_attn_decode(n, G, Hq, Hkv, D, Tp, cap, t[0], t[1], t[2], seg, off, t[3], t[4], ks, vs, lens, t[5], scale,
+                                       ws, ws_bytes, None)
+
+
+NO_SIZES = [dict(Hq=0), dict(Hkv=0), dict(D=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf"))]
+NO_SHAPES = [dict(Hq=6), dict(D=60), dict(D=136), dict(D=256)]
+
+
+def test_attention_rejects_bad_arguments_on_the_host():
+    for call in (attn_fwd, attn_bwd):
+        for bad in NO_SIZES + [dict(Tq=-1), dict(Tk=-1), dict(n=-1), dict(sq=None), dict(sq=ODD), dict(sk=ODD), dict(Tk=63)]:
+            assert call(**bad) == B.EINVAL, (call.__name__, bad)
+        for bad in NO_SHAPES + [dict(n=65536), dict(Tq=1 << 30, Tk=1 << 30)]:
+            assert call(**bad) == B.ESHAPE, (call.__name__, bad)
+    for name, i in zip("q k v out".split(), range(4)):
+        assert attn_fwd(**{name: heads(None)}) == B.EINVAL
+        assert attn_fwd(**{name: heads(FAR[i] + 8)}) == B.EINVAL            # not 16-byte aligned
+        assert attn_fwd(**{name: heads(FAR[i], token=-256)}) == B.EINVAL
+        assert attn_fwd(**{name: heads(FAR[i], token=260)}) == B.ESHAPE     # rows would not be 16-byte aligned
+        assert attn_fwd(**{name: heads(FAR[i], head=68)}) == B.ESHAPE
+        assert attn_fwd(**{name: heads(FAR[i], token=1 << 22)}) == B.ESHAPE
+    assert B.lib().skipffn_attn_forward(64, 64, 1, 4, 4, 64, None, heads(), heads(), heads(FAR[1]), FAKE, None, 1, 0.125, None, None, 0,
+                                        None) == B.EINVAL
+    # out: rows or heads over one another; memory of an input
+    assert attn_fwd(out=heads(FAR[3], token=128)) == B.EINVAL
+    assert attn_fwd(out=heads(FAR[3], head=0, token=64)) == B.EINVAL
+    for i in range(3):
+        assert attn_fwd(out=heads(FAR[i] + 1024)) == B.EINVAL
+    assert attn_fwd(saved=ODD) == B.EINVAL
+    # few queries over many keys: parts, and a workspace for them
+    need = B.skipffn_attn_forward_workspace_bytes(16, 1 << 16, 1, 4, 4, 64)
+    assert need > 0
+    assert attn_fwd(Tq=16, Tk=1 << 16, sk=FAKE) == B.EWORKSPACE
+    assert attn_fwd(Tq=16, Tk=1 << 16, sk=FAKE, ws=FAKE, ws_bytes=need - 1) == B.EWORKSPACE
+    # nothing to do
+    assert attn_fwd(n=0) == B.OK and attn_fwd(Tq=0, Tk=0, q=heads(None), k=heads(None), v=heads(None), out=heads(None)) == B.OK
+
+
+def test_attention_backward_rejects_bad_arguments_on_the_host():
+    for i in range(8):
+        assert attn_bwd(t={i: heads(None)}) == B.EINVAL
+        assert attn_bwd(t={i: heads(FAR[i], token=260)}) == B.ESHAPE
+    for o in (5, 6, 7):
+        assert attn_bwd(t={o: heads(FAR[o], token=128)}) == B.EINVAL
+        for i in range(5):
+            assert attn_bwd(t={o: heads(FAR[i])}) == B.EINVAL
+    assert attn_bwd(t={6: heads(FAR[5])}) == B.EINVAL
+    assert attn_bwd(saved=None) == B.EINVAL and attn_bwd(saved=ODD) == B.EINVAL
+    assert attn_bwd(ws=None) == B.EWORKSPACE and attn_bwd(ws_bytes=64 * 4 * 4 - 1) == B.EWORKSPACE
+    assert attn_bwd(n=0) == B.OK
+
+
+def test_attention_of_single_tokens_rejects_bad_arguments_on_the_host():
+    for bad in NO_SIZES + [dict(n=-1), dict(G=-1), dict(Tp=-1), dict(cap=-1), dict(seg=None), dict(off=ODD), dict(lens=None), dict(ks=-8)]:
+        assert attn_dec(**bad) == B.EINVAL, bad
+    for bad in NO_SHAPES + [dict(G=65535), dict(n=1 << 30), dict(ks=4), dict(vs=12)]:
+        assert attn_dec(**bad) == B.ESHAPE, bad
+    for i in range(6):
+        assert attn_dec(t={i: heads(None)}) == B.EINVAL
+        assert attn_dec(t={i: heads(FAR[i], token=260)}) == B.ESHAPE
+    assert attn_dec(t={0: heads(FAR[0], head=1 << 24)}) == B.ESHAPE
+    assert attn_dec(t={5: heads(FAR[5], token=128)}) == B.EINVAL
+    for i in range(5):
+        assert attn_dec(t={5: heads(FAR[i] + 512)}) == B.EINVAL
+    assert attn_dec(t={5: heads(FAR[3] + 3 * (1 << 15) + 512)}) == B.EINVAL          # the last sequence's own keys
+    big = dict(n=1, Tp=1 << 16)
+    need = B.skipffn_attn_decode_workspace_bytes(1, 1, 4, 4, 64, 1 << 16, 64)
+    assert need > 0 and attn_dec(**big, ws=None) == B.EWORKSPACE and attn_dec(**big, ws_bytes=need - 1) == B.EWORKSPACE
+    assert attn_dec(n=0) == B.OK
+
+
+def test_attention_size_queries():
+    assert B.skipffn_attn_saved_bytes(1000, 32) >= 1000 * 32 * 4
+    assert B.skipffn_attn_backward_workspace_bytes(1000, 1000, 3, 32, 8, 128) >= 1000 * 32 * 4
+    assert B.skipffn_attn_forward_workspace_bytes(100_000, 100_000, 4, 32, 8, 128) == 0          # enough queries: no parts
+    for bad in ((-1, 1, 1, 1, 1, 8), (1, 1, 1, 3, 2, 8), (1, 1, 1, 1, 1, 9)):
+        assert B.skipffn_attn_forward_workspace_bytes(*bad) == 0 == B.skipffn_attn_backward_workspace_bytes(*bad)
+
+
+def test_attention_binding_refuses_what_the_library_cannot_see():
+    import torch
+    bf = dict(dtype=torch.bfloat16)
+    q, k = torch.zeros(8, 4, 64, **bf), torch.zeros(8, 2, 64, **bf)
+    seg = torch.tensor([0, 8], dtype=torch.int32)
+    with pytest.raises(ValueError, match="current GPU"):
+        B.skipffn_attn_forward(q, k, k, torch.zeros_like(q), seg)
+    with pytest.raises(ValueError, match="current GPU"):
+        B.skipffn_attn_decode(q, k, k, seg, seg, None, None, None, torch.zeros_like(q))
+    # shapes, types, strides and devices of what comes with it
+    for t in (torch.zeros(8, 2, 32, **bf), torch.zeros(8, 2, 64), torch.zeros(8, 2, 128, **bf)[:, :, ::2], torch.zeros(7, 2, 64, **bf)):
+        with pytest.raises(ValueError, match="bfloat16 tensor"):
+            B._heads("call", -1, (t, k.shape))
+    with pytest.raises(ValueError, match="device"):
+        B._heads("call", 0, (k, k.shape))
+    for t in (seg.long(), torch.zeros(3, dtype=torch.int32), torch.zeros(4, dtype=torch.int32)[::2]):
+        with pytest.raises(ValueError, match="int32"):
+            B._ints(t, 2, "call", -1)
+    with pytest.raises(ValueError, match="at least"):
+        B._buffer(torch.zeros(15, dtype=torch.uint8), 16, "call", -1)
+    # a dimension of one has whatever stride it was cut with
+    assert list(B._heads("call", -1, (torch.zeros(1, 7, 64, **bf)[:, 3:4], (1, 1, 64)))[0])[1:] == [0, 0]

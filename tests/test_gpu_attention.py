@@ -136,3 +136,132 @@ def test_peaked_softmax_and_large_scores():
         # a score is off by up to 64 products of 2^-24 |q| |k| scale log2(e): |q| . |k| is about 64 x 30 x 0.64, so 0.0014 in the exponent
         extra = 0.001 * 2 * np.stack([P[h] @ np.abs(f["v"][r][:, h]) for h in range(2)], axis=1)
         assert_within(got[r], out, out_bound(P, f["v"][r], out) + extra, "out")
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 2, 64), (2, 1, 128)])
+def test_more_sequences_than_lanes(Hq, Hkv, D):
+    rng = np.random.default_rng(D)
+    lens = tuple(int(n) for n in rng.integers(0, 70, 150))
+    print(f"attention {len(lens)} sequences heads {Hq}/{Hkv} D={D}", flush=True)
+    p = Prompt(lens, lens, Hq, Hkv, D)
+    p.forward(True, D ** -0.5)
+    p.backward(True, D ** -0.5)
+    p.check(True, D ** -0.5, True)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,D,causal", [((257, 130, 64, 1, 190, 33, 250, 97) * 4, 32, 8, 128, True),
+                                                  ((200,) * 24, 24, 24, 64, False), ((150, 31, 260) * 9, 12, 4, 96, True)])
+def test_more_pieces_than_fit_the_chip(lens, Hq, Hkv, D, causal):
+    """Workgroups go on to further pieces, of other sequences, heads and lengths; twice the same bits."""
+    print(f"attention {len(lens)} sequences heads {Hq}/{Hkv} D={D}", flush=True)
+    p = Prompt(lens, lens, Hq, Hkv, D)
+    p.forward(causal, D ** -0.5)
+    p.backward(causal, D ** -0.5)
+    p.check(causal, D ** -0.5, True)
+    first = [bits_of(t) for t in (p.out, p.dq, p.dk, p.dv)]
+    for t in (p.out, p.dq, p.dk, p.dv):
+        t.fill_(7.0)
+    p.forward(causal, D ** -0.5)
+    p.backward(causal, D ** -0.5)
+    torch.cuda.synchronize()
+    assert all(np.array_equal(bits_of(t), f) for t, f in zip((p.out, p.dq, p.dk, p.dv), first))
+
+
+@pytest.mark.parametrize("nq,nk", [((3,), (4000,)), ((40, 1, 0, 17), (3000, 2100, 0, 5000)), ((9, 20), (5, 2500))], ids=str)
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (4, 4, 64), (6, 1, 80)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+def test_few_queries_whose_keys_are_cut_into_parts(nq, nk, Hq, Hkv, D, causal):
+    print(f"attention {nq} over {nk} heads {Hq}/{Hkv} D={D} causal={causal}", flush=True)
+    p = Prompt(nq, nk, Hq, Hkv, D, "cache")
+    assert p.fws.numel() > 16                             # the forward call wants room for parts
+    p.forward(causal, D ** -0.5)
+    p.backward(causal, D ** -0.5)
+    p.check(causal, D ** -0.5, True)
+
+
+def test_inputs_that_repeat_and_odd_strides():
+    """Keys and values of stride 0 by head (one head seen as several) and by token, rows with a gap between them: the same bits as
+    from tensors that hold the repeats."""
+    T, H, D = 75, 4, 64
+    rng = np.random.default_rng(9)
+    seg = offsets((50, 25))
+    wide = to_dev_bf16(O.f64_to_bf16_bits(rng.standard_normal((T, H + 3, D + 8))))
+    q, g = wide[:, 1:H + 1, :D], wide[:, 2:H + 2, :D]
+    one = to_dev_bf16(O.f64_to_bf16_bits(rng.standard_normal((2, T, 1, D))))
+    row = to_dev_bf16(O.f64_to_bf16_bits(rng.standard_normal((1, H, D))))
+    for k, v in ((one[0].expand(T, H, D), one[1].expand(T, H, D)), (row.expand(T, H, D), one[1].expand(T, H, D))):
+        got = []
+        for a, b, c, d in ((q, k, v, g), tuple(t.contiguous() for t in (q, k, v, g))):
+            out, dq, dk, dv = (torch.empty(T, H, D, dtype=torch.bfloat16, device="cuda") for _ in range(4))
+            saved, ws = nbytes(B.skipffn_attn_saved_bytes(T, H)), nbytes(B.skipffn_attn_backward_workspace_bytes(T, T, 2, H, H, D))
+            B.skipffn_attn_forward(a, b, c, out, seg, saved=saved)
+            B.skipffn_attn_backward(a, b, c, out, d, seg, None, saved, dq, dk, dv, workspace=ws)
+            got.append([bits_of(t) for t in (out, dq, dk, dv)])
+        assert all(np.array_equal(x, y) for x, y in zip(*got))
+
+
+def test_a_sequence_that_is_not_finite_leaves_the_others_as_they_are():
+    """NaN and infinities in one sequence reach nothing of its neighbours, in either direction and pass."""
+    lens, Hq, Hkv, D = (45, 70, 33), 4, 2, 128
+    p = Prompt(lens, lens, Hq, Hkv, D)
+    p.forward(True, 0.1)
+    p.backward(True, 0.1)
+    torch.cuda.synchronize()
+    clean = [bits_of(t) for t in (p.out, p.dq, p.dk, p.dv)]
+    p.v[45:115] = float("nan")
+    p.k[60] = float("inf")
+    p.q[70, 1] = float("-inf")
+    p.g[80] = float("nan")
+    p.forward(True, 0.1)
+    p.backward(True, 0.1)
+    torch.cuda.synchronize()
+    for t, c in zip((p.out, p.dq, p.dk, p.dv), clean):
+        b = bits_of(t)
+        assert np.array_equal(b[:45], c[:45]) and np.array_equal(b[115:], c[115:])
+    assert np.all(np.isnan(f64_of(p.out)[45:115]))
+
+
+def test_keys_past_32_bits():
+    """Queries after a cache whose rows lie past 2^31 elements."""
+    Hq, Hkv, D, Tk, n = 4, 8, 128, 2_200_000, 200
+    rng = np.random.default_rng(4)
+    Hq = 8
+    bits = O.f64_to_bf16_bits(rng.standard_normal((2, n, Hkv, D)))
+    kv = [torch.zeros(Tk, Hkv, D, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for t, b in zip(kv, bits):
+        t[Tk - n:] = to_dev_bf16(b)
+    q = to_dev_bf16(O.f64_to_bf16_bits(rng.standard_normal((50, Hq, D))))
+    out = torch.empty_like(q)
+    seg_q, seg_k = offsets((50,)), torch.tensor([Tk - n, Tk], dtype=torch.int32, device="cuda")
+    B.skipffn_attn_forward(q, *kv, out, seg_q, seg_k, workspace=nbytes(B.skipffn_attn_forward_workspace_bytes(50, Tk, 1, Hq, Hkv, D)))
+    torch.cuda.synchronize()
+    f = O.bf16_bits_to_f64(bits)
+    want, P = O.attn_forward_real(f64_of(q), f[0], f[1], True, D ** -0.5)
+    assert_within(f64_of(out), want, out_bound(P, f[1], want), "out")
+
+
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+def test_gradients_against_differences(causal):
+    """Along random directions of q, k and v the outputs' change, in fp64 by the oracle, is what the gradients say."""
+    Hq, Hkv, D, lens = 4, 2, 64, (37, 64)
+    p = Prompt(lens, lens, Hq, Hkv, D, "plain")
+    p.forward(causal, 0.125)
+    p.backward(causal, 0.125)
+    torch.cuda.synchronize()
+    f = {n: f64_of(getattr(p, n)) for n in ("q", "k", "v", "g", "dq", "dk", "dv")}
+    rng, eps, a = np.random.default_rng(5), 1e-5, 0
+    for n in lens:
+        r = slice(a, a + n)
+        a += n
+        x = {m: f[m][r] for m in ("q", "k", "v")}
+        b = O.attn_backward_real(x["q"], x["k"], x["v"], f["g"][r], causal, 0.125)
+        e = grad_bounds(x["q"], x["k"], x["v"], f["g"][r], 0.125, b)
+        for m in x:
+            d = rng.standard_normal(x[m].shape)
+            def loss(t):
+                y = dict(x, **{m: x[m] + t * d})
+                return (O.attn_forward_real(y["q"], y["k"], y["v"], causal, 0.125)[0] * f["g"][r]).sum()
+            by_difference = (loss(eps) - loss(-eps)) / (2 * eps)
+            # every element's bound in the worst direction, and the differences' own error (eps^2, 1e-16 / eps)
+            allowed = (e["d" + m] * np.abs(d)).sum() + 1e-4 * np.abs(by_difference) + 1e-4
+            assert abs((f["d" + m][r] * d).sum() - by_difference) <= allowed

@@ -100,3 +100,69 @@ def test_lengths_outside_the_capacity_are_clamped():
     d.run(0.125)
     d.own = [0, 3]
     d.check(0.125)
+
+
+def test_a_sequence_that_is_not_finite_leaves_the_others_as_they_are():
+    """Infinities and NaN among one sequence's own rows, and in the prefix of one group, reach the rows that see them and no others."""
+    Hq, Hkv, D = 8, 2, 128
+    d = Decode((5, 3, 0), (100, 70), (40, 33, 0, 70, 5, 1, 64, 9), Hq, Hkv, D)
+    d.run(D ** -0.5)
+    torch.cuda.synchronize()
+    clean = bits_of(d.out)
+    d.sv[1, 32, 0, 5] = float("inf")
+    d.sv[3, 10, 1, 7] = float("nan")
+    d.sk[4, 2, 0, 3] = float("nan")
+    d.sv[6, 3] = float("-inf")
+    d.run(D ** -0.5)
+    torch.cuda.synchronize()
+    got, f = bits_of(d.out), f64_of(d.out)
+    g = Hq // Hkv
+    for i in range(d.n):
+        for kh in range(Hkv):
+            heads = slice(kh * g, (kh + 1) * g)
+            hit = {(1, 0): [5], (3, 1): [7], (4, 0): range(D), (6, 0): range(D), (6, 1): range(D)}.get((i, kh), [])
+            keep = [c for c in range(D) if c not in hit]
+            assert np.array_equal(got[i, heads][:, keep], clean[i, heads][:, keep]), (i, kh)
+            assert not np.isfinite(f[i, heads][:, list(hit)]).any()
+    assert np.all(f[1, :g, 5] == np.inf) and np.all(f[6] == -np.inf) and np.all(np.isnan(f[3, g:, 7]))
+    # the prefix of the second group: the first group's rows keep their bits
+    d.pv[150, 1, 9] = float("nan")
+    d.run(D ** -0.5)
+    torch.cuda.synchronize()
+    assert np.array_equal(bits_of(d.out)[:5], got[:5])
+    assert np.all(np.isnan(f64_of(d.out)[5:, g:, 9]))
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 64), (4, 4, 128)])
+def test_more_sequences_and_groups_than_lanes(Hq, Hkv, D):
+    rng = np.random.default_rng(D)
+    members = [int(m) for m in rng.integers(0, 4, 130)] + [7]
+    prefix = [int(p) for p in rng.integers(0, 70, 130)]
+    own = [int(n) for n in rng.integers(0, 50, sum(members))]
+    print(f"decode {sum(members)} sequences, 130 groups, heads {Hq}/{Hkv} D={D}", flush=True)
+    d = Decode(members, prefix, own, Hq, Hkv, D)
+    d.run(D ** -0.5)
+    d.check(D ** -0.5)
+
+
+def test_offsets_past_32_bits():
+    """A cache of 2.2 million rows of 8 heads: elements past 2^31, bytes past 2^32, by token and by head."""
+    Hkv, D, Tp = 8, 128, 2_200_000
+    rng = np.random.default_rng(3)
+    rows = rng.standard_normal((2, 300, Hkv, D))
+    bits = O.f64_to_bf16_bits(rows)
+    for by_head in (False, True):
+        kv = [torch.zeros((Hkv, Tp, D) if by_head else (Tp, Hkv, D), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        kv = [t.transpose(0, 1) if by_head else t for t in kv]
+        for t, b in zip(kv, bits):
+            t[Tp - 300:] = to_dev_bf16(b)
+        q = to_dev_bf16(O.f64_to_bf16_bits(rng.standard_normal((2, 16, D))))
+        out = torch.empty(2, 16, D, dtype=torch.bfloat16, device="cuda")
+        ws = torch.empty(max(16, B.skipffn_attn_decode_workspace_bytes(2, 1, 16, Hkv, D, Tp, 0)), dtype=torch.uint8, device="cuda")
+        B.skipffn_attn_decode(q, kv[0], kv[1], ints([Tp - 300, Tp]), ints([0, 2]), None, None, None, out, workspace=ws)
+        torch.cuda.synchronize()
+        f = f64_of(q), O.bf16_bits_to_f64(bits)
+        for i in range(2):
+            want, P = O.attn_forward_real(f[0][i:i + 1], f[1][0], f[1][1], False, D ** -0.5)
+            assert_within(f64_of(out)[i:i + 1], want, out_bound(P, f[1][1], want), f"sequence {i}, by_head={by_head}")
+        del kv

@@ -184,3 +184,49 @@ def test_row_gathers_stay_inside_their_buffers(slabs, T, R, D, dt):
     torch.cuda.synchronize()
     gk.check(); gr.check()
     assert torch.equal(dst, src[:, idx.long()]) and torch.equal(rows, src[0][idx.long()])
+
+
+@pytest.mark.parametrize("nq,nk,Hq,Hkv,D", [((300, 41, 0, 129), None, 8, 2, 128), ((33, 64), None, 3, 3, 72), ((20, 1), (2500, 900), 8, 2, 128),
+                                            ((5, 40), (3000, 7), 4, 4, 64)])
+def test_attention_stays_inside_its_buffers(nq, nk, Hq, Hkv, D):
+    print(f"guard bytes attention {nq} over {nk} heads {Hq}/{Hkv} D={D}", flush=True)
+    nk = nq if nk is None else nk
+    T, Tk, n = sum(nq), sum(nk), len(nq)
+    seg_q, seg_k = (torch.tensor(np.concatenate([[0], np.cumsum(x)]).astype(np.int32)).cuda() for x in (nq, nk))
+    q, go = (torch.randn(T, Hq, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+    k, v = (torch.randn(Tk, Hkv, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+    sizes = (T, Tk, n, Hq, Hkv, D)
+    g = {
+        "out": Guarded(2 * T * Hq * D, "attention out"),
+        "saved": Guarded(B.skipffn_attn_saved_bytes(T, Hq), "attention saved"),
+        "fws": Guarded(max(16, B.skipffn_attn_forward_workspace_bytes(*sizes)), "attention forward workspace"),
+        "bws": Guarded(B.skipffn_attn_backward_workspace_bytes(*sizes), "attention backward workspace"),
+        "dq": Guarded(2 * T * Hq * D, "grad_q"), "dk": Guarded(2 * Tk * Hkv * D, "grad_k"), "dv": Guarded(2 * Tk * Hkv * D, "grad_v"),
+    }
+    out, dq = (g[x].typed(torch.bfloat16, (T, Hq, D)) for x in ("out", "dq"))
+    dk, dv = (g[x].typed(torch.bfloat16, (Tk, Hkv, D)) for x in ("dk", "dv"))
+    B.skipffn_attn_forward(q, k, v, out, seg_q, seg_k, saved=g["saved"].view, workspace=g["fws"].view)
+    B.skipffn_attn_backward(q, k, v, out, go, seg_q, seg_k, g["saved"].view, dq, dk, dv, workspace=g["bws"].view)
+    torch.cuda.synchronize()
+    for x in g.values():
+        x.check()
+    assert all(torch.isfinite(t.float()).all() for t in (out, dq, dk, dv))
+
+
+@pytest.mark.parametrize("members,prefix,own,Hq,Hkv,D", [((3, 0, 9), (700, 50, 4000), 40, 8, 2, 128), ((1, 1), (30, 7), 300, 5, 1, 40)])
+def test_single_token_attention_stays_inside_its_buffers(members, prefix, own, Hq, Hkv, D):
+    print(f"guard bytes single tokens {members} {prefix} {own} heads {Hq}/{Hkv} D={D}", flush=True)
+    n, Tp = sum(members), sum(prefix)
+    off, seg = (torch.tensor(np.concatenate([[0], np.cumsum(x)]).astype(np.int32)).cuda() for x in (members, prefix))
+    lens = torch.arange(n, dtype=torch.int32, device="cuda") % (own + 1)
+    pk, pv = (torch.randn(Tp, Hkv, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+    sk, sv = (torch.randn(n, own, Hkv, D, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(n, Hq, D, device="cuda").to(torch.bfloat16)
+    g = {"out": Guarded(2 * n * Hq * D, "out"),
+         "ws": Guarded(max(16, B.skipffn_attn_decode_workspace_bytes(n, len(members), Hq, Hkv, D, Tp, own)), "workspace")}
+    out = g["out"].typed(torch.bfloat16, (n, Hq, D))
+    B.skipffn_attn_decode(q, pk, pv, seg, off, sk, sv, lens, out, workspace=g["ws"].view)
+    torch.cuda.synchronize()
+    for x in g.values():
+        x.check()
+    assert torch.isfinite(out.float()).all()
