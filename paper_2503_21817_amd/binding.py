@@ -123,9 +123,9 @@ def _ptr(t):
     return None if t is None else c_void_p(t.data_ptr())
 
 
-def _stream():
+def _stream(device=None):
     # the handle that torch.cuda.current_stream().cuda_stream wraps, without the objects around it: 0.3 us for 2
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
 
 
 def _rargs(R, num_retained):
@@ -309,19 +309,22 @@ def _device(t, where):
     return d
 
 
+_HEADS = [c_int64 * (3 * n) for n in range(9)]
+
+
 def _heads(where, device, *tensors):
     """What the library takes as skipffn_heads of tensors [tokens, heads, columns] whose columns lie together: the array that
     holds them, and the address of each."""
     v = []
     for t, shape in tensors:
-        s, n = t.stride(), t.shape
-        if n != shape or t.dtype != torch.bfloat16 or t.get_device() != device or (s[2] != 1 and n[2] > 1):
+        s = t.stride()
+        if t.shape != shape or t.dtype is not torch.bfloat16 or t.get_device() != device or (s[2] != 1 and shape[2] > 1):
             raise ValueError(f"{where}: a bfloat16 tensor {tuple(shape)} on the device of the call, with contiguous columns, is wanted")
         # a stride that nothing is apart by is whatever the tensor was cut from
-        v += (t.data_ptr(), s[0] if n[0] > 1 else 0, s[1] if n[1] > 1 else 0)
-    a = (c_int64 * len(v))(*v)
+        v += (t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0)
+    a = _HEADS[len(tensors)](*v)
     at = addressof(a)
-    return a, [at + 24 * i for i in range(len(tensors))]
+    return a, range(at, at + 24 * len(tensors), 24)
 
 
 def _ints(t, n, where, device):
@@ -366,7 +369,7 @@ def skipffn_attn_forward(q, k, v, out, seg_q, seg_k=None, *, causal=True, scale=
     sv = None if saved is None else _buffer(saved, Tq * Hq * 4, where, dev)[0]
     _check(lib().skipffn_attn_forward(Tq, Tk, n1 - 1, Hq, Hkv, D, hq, hk, hv, ho, _ints(seg_q, n1, where, dev),
                                       None if seg_k is None else _ints(seg_k, n1, where, dev), 1 if causal else 0,
-                                      D ** -0.5 if scale is None else scale, sv, ws, ws_bytes, _stream()), where)
+                                      D ** -0.5 if scale is None else scale, sv, ws, ws_bytes, _stream(dev)), where)
 
 
 def skipffn_attn_backward(q, k, v, out, grad_out, seg_q, seg_k, saved, grad_q, grad_k, grad_v, *, causal=True, scale=None,
@@ -384,7 +387,7 @@ def skipffn_attn_backward(q, k, v, out, grad_out, seg_q, seg_k, saved, grad_q, g
     _check(lib().skipffn_attn_backward(Tq, Tk, n1 - 1, Hq, Hkv, D, hq, hk, hv, ho, hg, _ints(seg_q, n1, where, dev),
                                        None if seg_k is None else _ints(seg_k, n1, where, dev), 1 if causal else 0,
                                        D ** -0.5 if scale is None else scale, _buffer(saved, Tq * Hq * 4, where, dev)[0], gq, gk, gv,
-                                       ws, ws_bytes, _stream()), where)
+                                       ws, ws_bytes, _stream(dev)), where)
 
 
 def skipffn_attn_decode_workspace_bytes(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity) -> int:
@@ -416,13 +419,13 @@ def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, 
         lens = _ints(suffix_len, n_seq, where, dev)
         if n_seq > 1:
             seq_k, seq_v = suffix_k.stride(0), suffix_v.stride(0)
-        given += [(suffix_k[0], (cap, Hkv, D)), (suffix_v[0], (cap, Hkv, D))]
+        given += [(suffix_k.select(0, 0), (cap, Hkv, D)), (suffix_v.select(0, 0), (cap, Hkv, D))]
     hold, at = _heads(where, dev, *given)
     pk, pv = at[2:4] if prefix_k is not None else (None, None)
     sk, sv = at[-2:] if suffix_k is not None and n_seq > 0 else (None, None)
     ws, ws_bytes = _buffer(workspace, 0, where, dev)
     _check(lib().skipffn_attn_decode(n_seq, n_groups, Hq, Hkv, D, Tp, cap, at[0], pk, pv, seg, off, sk, sv, seq_k, seq_v, lens, at[1],
-                                     D ** -0.5 if scale is None else scale, ws, ws_bytes, _stream()), where)
+                                     D ** -0.5 if scale is None else scale, ws, ws_bytes, _stream(dev)), where)
 
 
 def skipffn_probe_mfma(blocks, iters, random_operands, out, clocks):

@@ -129,6 +129,24 @@ __device__ __forceinline__ void load_rows(const __amdgpu_buffer_rsrc_t& r, uint3
     }
 }
 
+// What was dropped of a row of values before the products (an infinity or a NaN would make a NaN of a weight of 0), added to the sums of
+// those that see it
+template <int DP>
+__device__ __forceinline__ void add_not_finite(f32x16 (&acc)[DP / 32], const bf16_t* v, int D, int h, bool sees) {
+#pragma unroll
+    for (int db = 0; db < DP / 32; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int d = db * 32 + 8 * q + 4 * h;
+            const u32x2 x = d < D ? *reinterpret_cast<const u32x2*>(v + d) : u32x2{0, 0};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float f = (e & 1) != 0 ? bf16hi_to_f32(x[e >> 1]) : bf16lo_to_f32(x[e >> 1]);
+                acc[db][4 * q + e] += sees && !(fabsf(f) < INFINITY) ? f : 0.0f;
+            }
+        }
+}
+
 // the two halves of a wavefront joined, lane l with lane l + 32
 __device__ __forceinline__ float halves_max(float v) {
     const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -252,6 +270,7 @@ __device__ __forceinline__ int piece_of(int k) {
 // What a wavefront works on in a kernel by queries: 32 rows of a head
 struct QueryUnit {
     int head, row0, wave_end, all_see;                   // keys that the last row, the first row see
+    int wg_sees;                                         // keys that every row of the workgroup sees
     int t0, t1;                                          // the workgroup's tiles of keys
     bool any;
 };
@@ -270,6 +289,7 @@ __device__ __forceinline__ QueryUnit query_unit(const AttnArgs& P, const SeqItem
     u.t1 = parts == 1 ? tiles : tiles * (part + 1) / parts;
     u.wave_end = u.any ? keys_of(min(u.row0 + ATT_ROWS, nq) - 1) : 0;
     u.all_see = keys_of(u.row0);
+    u.wg_sees = keys_of(max(first - (ATT_WAVES - 1), 0) / g * ATT_ROWS);
     return u;
 }
 

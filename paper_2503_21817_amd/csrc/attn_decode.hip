@@ -177,19 +177,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
             int i, k0, n;
             own_tile(u, i, k0, n);
             const bf16_t* v = P.sv + (s0 + i) * P.sv_seq + kvh * P.sv_head + (int64_t)k0 * P.sv_tok;
-            for (int j = min(n - k0, DEC_KEYS); j > 0; --j, v += P.sv_tok)
-#pragma unroll
-                for (int db = 0; db < DP / 32; ++db)
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int d = db * 32 + 8 * q + 4 * h;
-                        const u32x2 x = d < P.D ? *reinterpret_cast<const u32x2*>(v + d) : u32x2{0, 0};
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float f = (e & 1) != 0 ? bf16hi_to_f32(x[e >> 1]) : bf16lo_to_f32(x[e >> 1]);
-                            acc[db][4 * q + e] += member == i && !(fabsf(f) < INFINITY) ? f : 0.0f;
-                        }
-                    }
+            for (int j = min(n - k0, DEC_KEYS); j > 0; --j, v += P.sv_tok) add_not_finite<DP>(acc, v, P.D, h, member == i);
         }
     }
     // join the wavefronts: [column][row] of each where its tiles were

@@ -20,6 +20,7 @@ template <int DP, int KEYS, bool PARTS>
 __global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fwd_kernel(const AttnArgs P, const int blocks) {
     constexpr int KB = KEYS / 32, TILE = KEYS * tile_row_bytes<DP>(), ROWS = ATT_WAVES * 32 * tile_row_bytes<DP>();
     __shared__ __align__(256) char smem[4 * TILE];
+    __shared__ int dropped_in[ATT_WAVES];                // by wavefront: the last piece in whose tiles it dropped a value
     static_assert(4 * TILE >= ROWS, "the rows of a piece leave by way of the tiles");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
     const int g = P.Hq / P.Hkv;
@@ -50,6 +51,7 @@ __global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fw
                       u.any && u.row0 + (ln & 31) < s.q1 - s.q0, P.D, ln, qf);
     };
     if (!locate(0, kvh, part, it)) return;
+    if (lane == 0) dropped_in[wave] = 0;
     QueryUnit u = query_unit<KEYS>(P, it, kvh, wave, part, PARTS ? P.splits : 1);
     load_q(it, u);
     if (u.t0 < u.t1) load_tile(it, kvh, u.t0);
@@ -64,10 +66,18 @@ __global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fw
         f32x16 acc[DP / 32] = {};
         float m = -INFINITY, l = 0.0f;
         const float c = P.scale_log2;
-        if (u.t0 < u.t1) {
+        // a tile of which a row does not see every key: values that are not finite leave it, and are added at the end
+        auto store_tile = [&](int t) {
+            if (P.causal && (t + 1) * KEYS > u.wg_sees && lv.any_not_finite()) {
+                lv.drop_not_finite();
+                dropped_in[wave] = turn;
+            }
             lk.store(smem + stage * 2 * TILE, tid);
             lv.store(smem + stage * 2 * TILE + TILE, tid);
             __syncthreads();
+        };
+        if (u.t0 < u.t1) {
+            store_tile(u.t0);
         } else if (next.t0 < next.t1) {
             load_tile(next_it, next_kvh, next.t0);
         }
@@ -147,13 +157,19 @@ __global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fw
             load_tile(it, kvh, t + 1);
             work_on(t);
             stage ^= 1;
-            lk.store(smem + stage * 2 * TILE, tid);
-            lv.store(smem + stage * 2 * TILE + TILE, tid);
-            __syncthreads();
+            store_tile(t + 1);
         }
         if (u.t0 < u.t1) {
             if (next.t0 < next.t1) load_tile(next_it, next_kvh, next.t0);
             work_on(u.t1 - 1);
+        }
+        bool dropped = false;
+#pragma unroll
+        for (int i = 0; i < ATT_WAVES; ++i) dropped |= dropped_in[i] == turn;
+        if (P.causal && __ballot(dropped) != 0) {
+            const int end = min(u.t1 * KEYS, u.wave_end);
+            for (int j = max(u.t0, max(u.wg_sees, 0) / KEYS) * KEYS; j < end; ++j)
+                add_not_finite<DP>(acc, P.v + kvh * P.v_head + (int64_t)(it.k0 + j) * P.v_tok, P.D, h, j < row_keys);
         }
         if constexpr (2 * TILE < ROWS) __syncthreads();  // otherwise the rows fit the tile that no wavefront reads any more
         if (more) load_q(next_it, next);

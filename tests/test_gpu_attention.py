@@ -265,3 +265,33 @@ def test_gradients_against_differences(causal):
             # every element's bound in the worst direction, and the differences' own error (eps^2, 1e-16 / eps)
             allowed = (e["d" + m] * np.abs(d)).sum() + 1e-4 * np.abs(by_difference) + 1e-4
             assert abs((f["d" + m][r] * d).sum() - by_difference) <= allowed
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,nq,nk", [(4, 2, 128, (200, 40), (200, 40)), (32, 8, 128, (150,) * 9, (150,) * 9), (4, 4, 64, (130,), (130,)),
+                                            (8, 2, 80, (5, 60), (3000, 60)), (6, 3, 96, (150,) * 20, (150,) * 20)], ids=str)
+def test_values_that_are_not_finite_reach_the_rows_that_see_them_alone(Hq, Hkv, D, nq, nk):
+    """In a causal prompt a NaN or an infinity among the values of token j shows in the rows from j on, in its column; the rows before it
+    keep their bits, and so do the other columns."""
+    print(f"not finite, heads {Hq}/{Hkv} D={D} {nq} over {nk}", flush=True)
+    p = Prompt(nq, nk, Hq, Hkv, D, "fused" if nq == nk else "plain")
+    p.forward(True, D ** -0.5)
+    torch.cuda.synchronize()
+    clean, lse = bits_of(p.out), p.saved.clone()
+    ko, qo = np.concatenate([[0], np.cumsum(nk)]), np.concatenate([[0], np.cumsum(nq)])
+    planted = []                                         # (sequence, key, key/value head, column, value)
+    for s, (a, b) in enumerate(zip(nq, nk)):
+        for back, value in ((a // 2, np.inf), (1, np.nan), (a - 1, -np.inf)):
+            key, kh, col = b - 1 - back, s % Hkv, (7 * s + 3 * back) % D
+            planted.append((s, key, kh, col, value))
+            p.v[int(ko[s]) + key, kh, col] = value
+    p.forward(True, D ** -0.5)
+    torch.cuda.synchronize()
+    got, f = bits_of(p.out), f64_of(p.out)
+    hit = np.zeros(got.shape, bool)
+    for s, key, kh, col, value in planted:
+        first = max(key - (nk[s] - nq[s]), 0)            # the first query that sees the key
+        heads = slice(kh * (Hq // Hkv), (kh + 1) * (Hq // Hkv))
+        hit[qo[s] + first:qo[s + 1], heads, col] = True
+    assert np.array_equal(got[~hit], clean[~hit])
+    assert not np.isfinite(f[hit]).any()
+    assert torch.equal(p.saved[:4 * p.T * Hq], lse[:4 * p.T * Hq])
