@@ -237,15 +237,16 @@ int64_t decode_blocks(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv) 
 }
 }  // namespace
 
-// As many parts as give every compute unit two workgroups, but none of fewer than 4 tiles a wavefront of the longest list that
-// the bounds allow on average
+// As many parts as give every compute unit two workgroups (one / two / three, us: 64 sequences on 2 prefixes of up to 5795 rows 25.5 / 23.3 / 29.3,
+// 128 on 2 of 1000 29.2 / 24.5 / 32.5, 4 caches of up to 32768 rows 64 / 65 / 66), but none of fewer than 192 keys of the longest list that the
+// bounds allow on average (128 / 256, us: 1 sequence of 600 + 100 rows 9.0 / 10.2, 8 of 184 + 64 9.9 / 8.3)
 int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t Tp, int64_t cap, int ncu) {
     if (n_seq <= 0) return 1;
     const int64_t g = Hq / Hkv, members = g >= 32 ? 1 : 32 / g;
     const int64_t blocks = std::max<int64_t>(std::max(n_groups, (n_seq + members - 1) / members), 1) * Hkv * ((g + 31) / 32);
     const int64_t shared = std::max<int64_t>(1, std::min(members, n_groups > 0 ? n_seq / n_groups : members));
     const int64_t keys = (n_groups > 0 ? Tp / n_groups : 0) + shared * cap;
-    const int64_t want = (2 * (int64_t)ncu + blocks - 1) / blocks, most = keys / (DEC_KEYS * ATT_WAVES * 2);
+    const int64_t want = (2 * (int64_t)ncu + blocks - 1) / blocks, most = keys * 2 / (DEC_KEYS * ATT_WAVES * 3);
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), ATTN_MAX_SPLITS));
 }
 
