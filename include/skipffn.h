@@ -1,7 +1,8 @@
 /*
  * skipffn.h - C ABI of the MI355X (gfx950) Skip-FFN block.
  *
- * The block is the feed-forward half of one decoder layer under Skip-Vision
+ * The block is the feed-forward half of one decoder layer under Skip-Vision (its first half,
+ * attention, is here too: skipffn_attn_*)
  * (Section 4.2 of the paper):
  *
  *     retained token :  h_out = h_attn + FFN(h_attn)
@@ -301,9 +302,14 @@ int skipffn_token_merge_backward(const void* grad_out, const int32_t* seg_host, 
  *   scale          > 0, finite (1 / sqrt(D))
  *   saved          NULL (inference) or skipffn_attn_saved_bytes(Tq, Hq) bytes OUT (log-sum-exp, f32)
  *   workspace      at least skipffn_attn_forward_workspace_bytes(...) bytes (NULL where that is 0)
- * D % 8 == 0, 8 <= D <= 128, Hq a multiple of Hkv, n_seq <= 65535.  Scores, softmax sums and products are
- * accumulated in fp32; the weights P are rounded to bf16 before they meet v (the matrix cores' operand
- * type).  Deterministic: every sum has a fixed order. */
+ * D % 8 == 0, 8 <= D <= 128, Hq a multiple of Hkv, n_seq <= 65535, (max(Tq, Tk) / 32 + 2 n_seq) Hq < 2^25.
+ * Scores, softmax sums and products are accumulated in fp32; the weights P are rounded to bf16 before they
+ * meet v (the matrix cores' operand type).  Deterministic: every sum has a fixed order.
+ * A k_j or v_j that is not finite reaches the queries that see key j, and no others; rows that belong to no
+ * sequence may hold anything.
+ * The workspace is for the keys of few queries, which are cut into parts: ask for the sizes of the call (more
+ * queries may need less), or for the largest answer of the calls to come.  As everywhere, calls that may
+ * overlap in time need workspaces of their own. */
 typedef struct skipffn_heads {
     void* data;
     int64_t token_stride, head_stride;
@@ -322,10 +328,10 @@ int skipffn_attn_forward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int6
  * the last two summed over the query heads of a key/value head too (in fp32, rounded once).
  *   out, saved     what the forward call wrote for the same inputs
  *   grad_q [Tq, Hq, D], grad_k and grad_v [Tk, Hkv, D] OUT, overwritten; rows that belong to no sequence
- *                  are left as they were.  They may be column ranges of one tensor; what they span
- *                  meets none of the inputs.
+ *                  are left as they were.  They may be column ranges of one tensor (no element
+ *                  is shared); what they span meets none of the inputs.
  *   workspace      at least skipffn_attn_backward_workspace_bytes(...)
- * Deterministic. */
+ * Deterministic.  What is not finite in one sequence may reach any gradient of that sequence, and none of another. */
 size_t skipffn_attn_backward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D);
 int skipffn_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D,
                           const skipffn_heads* q, const skipffn_heads* k, const skipffn_heads* v,
@@ -348,8 +354,9 @@ int skipffn_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int
  *   suffix_k, suffix_v        [n_seq][suffix_capacity, Hkv, D], sequence s suffix_k_seq (suffix_v_seq) elements
  *                             after the one before it.  Not read where suffix_capacity == 0
  *   suffix_len  i32 [n_seq] device: own rows of every sequence (clamped to 0 .. suffix_capacity)
- * A sequence with no rows at all gives a zero row.  Types, scale and shapes as above; out may not meet q or
- * the caches.  workspace: at least skipffn_attn_decode_workspace_bytes(...), which holds fp32 rows of the parts
+ * A sequence with no rows at all gives a zero row.  What is not finite among a sequence's own rows reaches that
+ * sequence alone.  Types, scale and shapes as above, (n_seq + n_groups + 1) Hq < 2^24, strides by sequence < 2^36;
+ * out may not meet q or the caches.  workspace: at least skipffn_attn_decode_workspace_bytes(...), which holds fp32 rows of the parts
  * that long caches are cut into.  The parts depend on the bounds of the call (Tp, suffix_capacity, n_groups),
  * not on the lengths on the device.  Deterministic. */
 size_t skipffn_attn_decode_workspace_bytes(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp,

@@ -139,7 +139,8 @@ const char* skipffn_status_string(int status) {
     switch (status) {
         case SKIPFFN_OK: return "ok";
         case SKIPFFN_EINVAL: return "invalid argument (null or misaligned pointer, negative size, R > T)";
-        case SKIPFFN_ESHAPE: return "unsupported shape (C, I must be multiples of 8; tensors below 2 GiB; skipffn_compact_static: T above skipffn_compact_static_max_tokens())";
+        case SKIPFFN_ESHAPE: return "unsupported shape (C, I must be multiples of 8; tensors below 2 GiB; skipffn_compact_static: T above skipffn_compact_static_max_tokens(); "
+                                      "attention: columns a head, strides, heads or tokens outside their limits)";
         case SKIPFFN_EWORKSPACE: return "workspace too small";
         case SKIPFFN_EHIP: return "HIP runtime error";
         case SKIPFFN_EUNSUPPORTED: return "unsupported flag";
@@ -149,7 +150,7 @@ const char* skipffn_status_string(int status) {
 }
 
 int skipffn_last_hip_error(void) { return g_last_hip; }
-int skipffn_version(void) { return 20100; }   // 2.1.0: leading dimension of the transposed saved copies
+int skipffn_version(void) { return 20200; }   // 2.2.0: attention
 
 int skipffn_profile_begin(void) {
     std::lock_guard<std::mutex> lk(g_prof_mu);
@@ -824,8 +825,8 @@ namespace {
 int check_attn(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, float scale) {
     if (Tq < 0 || Tk < 0 || n_seq < 0 || Hq <= 0 || Hkv <= 0 || D <= 0 || !(scale > 0.0f) || !std::isfinite(scale)) return SKIPFFN_EINVAL;
     if (Hq % Hkv != 0 || (D & 7) || D > ATTN_MAX_D || n_seq > 65535 || Hq > 65535 || Tq >= (1 << 30) || Tk >= (1 << 30)) return SKIPFFN_ESHAPE;
-    // a grid of workgroups by queries, one by keys, as launch_attn_* form them
-    if ((Tq / 32 + 2 * n_seq) * Hq >= (1ll << 30) || (Tk / 32 + 2 * n_seq) * Hkv >= (1ll << 30)) return SKIPFFN_ESHAPE;
+    // grids of workgroups by queries and by keys (a launch has fewer than 2^32 threads), and the kernels' 32-bit products of blocks and heads
+    if ((std::max(Tq, Tk) / 32 + 2 * n_seq) * Hq >= ((int64_t)1 << 25)) return SKIPFFN_ESHAPE;
     return SKIPFFN_OK;
 }
 // bytes from the first element to past the last one
@@ -959,7 +960,7 @@ int check_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64
     if (n_groups < 0 || cap < 0) return SKIPFFN_EINVAL;
     const int st = check_attn(n_seq, Tp, n_groups, Hq, Hkv, D, scale);
     if (st != SKIPFFN_OK) return st;
-    if (n_groups > 65534 || cap >= (1 << 30) || (n_seq + n_groups + 1) * Hq >= (1ll << 30)) return SKIPFFN_ESHAPE;
+    if (n_groups > 65534 || cap >= (1 << 30) || (n_seq + n_groups + 1) * Hq >= ((int64_t)1 << 24)) return SKIPFFN_ESHAPE;
     return SKIPFFN_OK;
 }
 }  // namespace
@@ -985,7 +986,7 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
     if (cap > 0) {
         if ((st = check_heads(suffix_k, cap, Hkv, D, false)) || (st = check_heads(suffix_v, cap, Hkv, D, false))) return st;
         if (suffix_k_seq < 0 || suffix_v_seq < 0 || bad_seg(suffix_len)) return SKIPFFN_EINVAL;
-        if ((suffix_k_seq & 7) || (suffix_v_seq & 7) || suffix_k_seq >= ((int64_t)1 << 44) || suffix_v_seq >= ((int64_t)1 << 44)) return SKIPFFN_ESHAPE;
+        if ((suffix_k_seq & 7) || (suffix_v_seq & 7) || suffix_k_seq >= ((int64_t)1 << 36) || suffix_v_seq >= ((int64_t)1 << 36)) return SKIPFFN_ESHAPE;
     }
     if (n_seq == 0) return SKIPFFN_OK;
     const uintptr_t o0 = reinterpret_cast<uintptr_t>(out->data), o1 = o0 + (uintptr_t)heads_span(out, n_seq, Hq, D);

@@ -4,7 +4,12 @@
 // key/value head, so that a prefix is read once for all of them.  Their keys are one list of tiles of 32: the prefix's, seen by
 // every row, then each sequence's own, seen by its rows alone.  The list is cut into `splits` even parts, one a workgroup, and
 // a part is dealt out to the four wavefronts, each with tiles of its own in LDS (nothing is waited for but a wavefront's own loads);
-// the wavefronts' maxima, sums and rows are joined in LDS, those of the parts by a second kernel.  Bound by the reads of the cache.
+// the wavefronts' maxima, sums and rows are joined in LDS, those of the parts by a second kernel.  Few rows of a product are in use
+// where little is shared (4 of 32 with 32 / 8 heads and no sharing): the matrix cores have the time, the reads of the cache bound it.
+//
+// Measured, 32 / 8 heads of 128: 4 caches of up to 32768 rows (300 MB) 50 us, 6.0 TB/s, and 4.3 for the second kernel (a large copy: 5.0 TB/s); 64
+// sequences on two prefixes of up to 5795 rows (54 MB) 18.4 + 3.9 us: four tiles a wavefront one after the other, a latency each; 8 sequences of
+// 184 + 64 rows 8.1 us, all latency.
 #include <algorithm>
 
 #include "attn.hpp"

@@ -5,14 +5,17 @@
 // and takes tiles of 64 or 32 keys and values through LDS, two tiles deep: the next tile's loads are under way in registers while this
 // one is worked on.  With 8 heads a chip-wide row of 8 workgroups has one key/value head each, so that an XCD's L2 holds one
 // head's keys.  Units of a sequence are taken from its end: in a causal prompt the longest first.
+//
+// Long prompts are bound by the power limit (the chip falls to 1.75-1.85 GHz with the matrix cores busy half of the time): 1 x 16384 tokens, 32 / 8
+// heads of 128, 2030-2280 us by the box, 966-1083 TFLOP/s of what the mask leaves, a library product of 8192^3 reaching 1175-1190.  Short ones
+// by the bytes of q and out, which a workgroup's products do not hide: 8 x 616 tokens 48 us, 520 TFLOP/s and 2.1 TB/s.
 #include "attn.hpp"
 
 namespace skipffn {
 
-
 // Workgroups a compute unit and keys a tile.  With pieces for all of them three workgroups (168 registers) do better than two, as some load
 // or store while others work; at 128 columns that leaves room for tiles of 32 keys.  64 keys and two workgroups / 32 and three, us:
-// 16 x 616 tokens 94 / 89, 32 x 200 45.8 / 40, 16 x up to 3080 729 / 711, 1 x 16384 2070 / 2110; but with fewer pieces than two a unit,
+// 16 x 616 tokens 94 / 89, 32 x 200 45.8 / 40, 16 x up to 3080 729 / 711, 4 x 4096 605 / 608, 1 x 16384 2271 / 2275 (the power limit); but with fewer pieces than two a unit,
 // where a workgroup has its SIMDs to itself: 4 x 47 after 640 17.1 / 19.1.  64 columns, 64 keys and three / 32 and four: 8 x 577 25.4 / 26.6.
 template <int DP, int KEYS> constexpr int fwd_per_cu() { return DP <= 64 || KEYS == 32 ? 3 : 2; }
 
