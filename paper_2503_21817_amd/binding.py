@@ -404,6 +404,8 @@ def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, 
     n_seq, Hq, D = q.shape
     if prefix_k is None and suffix_k is None:
         raise ValueError(f"{where}: a prefix or own rows are wanted")
+    if len({t is None for t in (prefix_k, prefix_v, prefix_seg, group_off)}) > 1 or len({t is None for t in (suffix_k, suffix_v, suffix_len)}) > 1:
+        raise ValueError(f"{where}: a prefix, or own rows, come with all that belongs to them")
     Hkv = (suffix_k if prefix_k is None else prefix_k).shape[-2]
     Tp = n_groups = cap = seq_k = seq_v = 0
     seg = off = lens = None

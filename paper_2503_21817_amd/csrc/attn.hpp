@@ -7,11 +7,10 @@
 //                               free, so V^T is read in the order of keys that the lane holds.
 // Row maxima and sums then stay inside a lane but for one exchange with the lane 32 further.
 //
-// A kernel for 64, 96 or 128 columns serves heads of up to as many.  A tile of rows [token][column] of one head lies in LDS with 128 bytes a
-// row (64 columns) or 256, 16-byte
-// chunk c of row r at c ^ tile_swz(r).  The same placing serves both ways it is read, free of bank conflicts: 16 consecutive rows
-// at one chunk (ds_read_b128, the operand whose contraction runs along the columns) and 4 rows x 64 bytes (ds_read_b64_tr_b16, the
-// operand whose contraction runs along the tokens).
+// A kernel for 64, 96 or 128 columns serves heads of up to as many.  A tile of rows [token][column] of one head lies in LDS with
+// 128 bytes a row (64 columns) or 256, 16-byte chunk c of row r at c ^ tile_swz(r).  The same placing serves both ways it is read,
+// free of bank conflicts: 16 consecutive rows at one chunk (ds_read_b128, the operand whose contraction runs along the columns) and
+// 4 rows x 64 bytes (ds_read_b64_tr_b16, the operand whose contraction runs along the tokens).
 #pragma once
 
 #include "kernels.hpp"
@@ -22,7 +21,6 @@ namespace skipffn {
 constexpr int ATT_ROWS = 32;               // queries of a wavefront
 constexpr int ATT_WAVES = 4;
 constexpr int ATT_THREADS = ATT_WAVES * 64;
-constexpr float kLog2e = 1.4426950408889634f;
 
 typedef __attribute__((address_space(3))) bf16x4* lds_bf16x4_ptr;
 
@@ -87,8 +85,8 @@ struct TileLoad {
     }
 };
 
-// Operands from a tile at LDS address `tile` (a multiple of a row's bytes), in 32-bit LDS addresses: the lane's part of an address is
-// added once a tile, the chunk then an exclusive or and the rows an immediate offset, so that no register holds an address a chunk.
+// Operands from a tile that begins at a multiple of 256 bytes of LDS, by 32-bit LDS addresses: `at` is the tile's with the lane's part
+// (rows_lane, cols_lane) added once, the chunk then an exclusive or and the rows an immediate offset, so that no register holds an address a chunk.
 //
 // With the contraction along the columns: lane l holds row row0 + l % 32 and columns 16 c + 8 (l / 32) .. + 7; row0 % 32 == 0
 typedef __attribute__((address_space(3))) const bf16x8* lds_bf16x8_ptr;
@@ -128,6 +126,24 @@ __device__ __forceinline__ void load_rows(const __amdgpu_buffer_rsrc_t& r, uint3
         f[c] = __builtin_bit_cast(bf16x8, buf_load16(r, ok && d < D ? row_off + (uint32_t)d * 2u : kOobOffset));
     }
 }
+
+// The same by way of LDS: 32 rows of a wavefront loaded in whole rows (a load of the operand itself touches 32 bytes of each of 32 rows),
+// stored to 32 rows of a tile that nobody else uses, and read as operands
+template <int DP>
+struct RowsIn {
+    TileLoad<DP, 32, 64> t;
+    __device__ __forceinline__ void load(const bf16_t* base, int stride, int rows, int D, int lane) {
+        t.load(HeadRows{base, stride}, 0, rows, D, TileLoad<DP, 32, 64>::first(lane, stride, D));
+    }
+    __device__ __forceinline__ void operands(char* lds, int lane, bf16x8 (&f)[DP / 16]) const {
+        t.store(lds, lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        const uint32_t at = lds_addr_of(lds) + rows_lane<DP>(lane);
+#pragma unroll
+        for (int c = 0; c < DP / 16; ++c) f[c] = frag_rows<DP>(at, 0, c);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+};
 
 // What was dropped of a row of values before the products (an infinity or a NaN would make a NaN of a weight of 0), added to the sums of
 // those that see it
@@ -188,7 +204,7 @@ __device__ __forceinline__ void store_rows(bf16_t* base, int stride, int rows, c
 // 32s of rows that it goes over (num = 0: all the same), so that cnt(L) = ceil((top - L + 1) den / num) of a sequence's have at least L; a search over L finds
 // the level of workgroup q, a prefix sum its sequence.  For up to 64 sequences, a lane each; with more of them (each then a small
 // part of the whole) workgroups go sequence by sequence.  rows(lengths of a sequence) gives its workgroups and top.
-struct SeqItem { int seq, item, q0, q1, k0, k1; };
+struct SeqItem { int item, q0, q1, k0, k1; };
 template <class Rows>
 __device__ __forceinline__ bool locate_longest(const AttnArgs& P, int lane, int q, int num, int den, const Rows& rows, SeqItem& it) {
     if (P.n_seq > 64) {
@@ -204,7 +220,7 @@ __device__ __forceinline__ bool locate_longest(const AttnArgs& P, int lane, int 
             const uint64_t past = __ballot(q < cc + incl);
             if (past != 0) {
                 const int l = __builtin_ctzll(past);
-                it = {i0 + l, q - cc - __builtin_amdgcn_readlane(incl - n, l), __builtin_amdgcn_readlane(qb, l), __builtin_amdgcn_readlane(qe, l),
+                it = {q - cc - __builtin_amdgcn_readlane(incl - n, l), __builtin_amdgcn_readlane(qb, l), __builtin_amdgcn_readlane(qe, l),
                       __builtin_amdgcn_readlane(kb, l), __builtin_amdgcn_readlane(ke, l)};
                 return true;
             }
@@ -242,7 +258,7 @@ __device__ __forceinline__ bool locate_longest(const AttnArgs& P, int lane, int 
         l = __builtin_ctzll(__ballot(r < incl));
         item = r - __builtin_amdgcn_readlane(incl - here, l) + __builtin_amdgcn_readlane(before, l);
     }
-    it = {l, item, __builtin_amdgcn_readlane(qb, l), __builtin_amdgcn_readlane(qe, l), __builtin_amdgcn_readlane(kb, l), __builtin_amdgcn_readlane(ke, l)};
+    it = {item, __builtin_amdgcn_readlane(qb, l), __builtin_amdgcn_readlane(qe, l), __builtin_amdgcn_readlane(kb, l), __builtin_amdgcn_readlane(ke, l)};
     return true;
 }
 // workgroup of a kernel by queries: four units of 32 rows of a head, g heads a block of rows, from a sequence's end

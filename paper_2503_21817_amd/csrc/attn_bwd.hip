@@ -8,7 +8,7 @@
 // and everything summed is fp32.
 //
 // Bound by power in long prompts and by the bytes of q, out and their gradients in short ones.  32 / 8 heads of 128, us (TFLOP/s of each kernel's own
-// products): 4 x 2944 tokens dQ 430 (990), dK and dV 655 (867); 16 x 616 dQ 135-146 (510-550), dK and dV 148-170 (590-670).
+// products): 4 x 2944 tokens dQ 410-416 (1025-1040), dK and dV 637-645 (880-890); 16 x 616 dQ 125-136 (550-600), dK and dV 156-168 (590-640).
 #include "attn.hpp"
 
 namespace skipffn {
@@ -16,7 +16,8 @@ namespace skipffn {
 constexpr int DQ_KEYS = 64;
 
 // ---- dQ, delta: a wavefront has a unit of 32 queries of one head, as in the forward kernel ------------------------------------
-// Two workgroups a compute unit: the queries and their gradients stay in registers (64 of them) beside the sums of dQ.
+// Two workgroups a compute unit: the queries and their gradients stay in registers (64 of them) beside the sums of dQ.  The rows come in by way
+// of LDS: loaded as operands, 32 bytes of each of 32 rows at a time, a training step of 16 x 616 tokens takes 380 us for 372.
 template <int DP>
 __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dq_kernel(const AttnArgs P, const AttnGrads G) {
     constexpr int TILE = DQ_KEYS * tile_row_bytes<DP>();
@@ -49,12 +50,18 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dq_kernel(
     bf16x8 qf[DP / 16], gf[DP / 16];
     float delta = 0.0f, lse = INFINITY;
     {
-        const uint32_t r = (uint32_t)(lane & 31) * 2u;
         const int64_t t = q0 + row0;
-        load_rows<DP>(make_rsrc(P.q + head * P.q_head + t * P.q_tok, 0x7fffffffu), r * (uint32_t)P.q_tok, row_ok, P.D, lane, qf);
-        load_rows<DP>(make_rsrc(G.go + head * G.go_head + t * G.go_tok, 0x7fffffffu), r * (uint32_t)G.go_tok, row_ok, P.D, lane, gf);
+        const int rows = unit >= 0 ? min(nq - row0, ATT_ROWS) : 0;
+        char* lds = smem + 2 * TILE + wave * 32 * tile_row_bytes<DP>();      // of the stage that is filled later
+        RowsIn<DP> iq, ig, io;
+        iq.load(P.q + head * P.q_head + t * P.q_tok, P.q_tok, rows, P.D, lane);
+        ig.load(G.go + head * G.go_head + t * G.go_tok, G.go_tok, rows, P.D, lane);
+        io.load(P.out + head * P.o_head + t * P.o_tok, P.o_tok, rows, P.D, lane);
+        if (row_ok) lse = P.lse[(int64_t)head * P.Tq + q0 + row];
         bf16x8 of[DP / 16];
-        load_rows<DP>(make_rsrc(P.out + head * P.o_head + t * P.o_tok, 0x7fffffffu), r * (uint32_t)P.o_tok, row_ok, P.D, lane, of);
+        iq.operands(lds, lane, qf);
+        ig.operands(lds, lane, gf);
+        io.operands(lds, lane, of);
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d) {
             float a[8], b[8];
@@ -64,7 +71,6 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dq_kernel(
             for (int j = 0; j < 8; ++j) delta = fmaf(a[j], b[j], delta);
         }
         delta = halves_sum(delta);
-        if (row_ok) lse = P.lse[(int64_t)head * P.Tq + q0 + row];
     }
     const uint32_t rows_at = lds_addr_of(smem) + rows_lane<DP>(lane), cols_at = lds_addr_of(smem) + cols_lane<DP>(lane);
     f32x16 acc[DP / 32] = {};

@@ -390,6 +390,8 @@ def test_attention_binding_refuses_what_the_library_cannot_see():
         B.skipffn_attn_forward(q, k, k, torch.zeros_like(q), seg)
     with pytest.raises(ValueError, match="current GPU"):
         B.skipffn_attn_decode(q, k, k, seg, seg, None, None, None, torch.zeros_like(q))
+    with pytest.raises(ValueError, match="current GPU"):
+        B.skipffn_attn_backward(q, k, k, q, q, seg, None, None, q, k, k)
     # shapes, types, strides and devices of what comes with it
     for t in (torch.zeros(8, 2, 32, **bf), torch.zeros(8, 2, 64), torch.zeros(8, 2, 128, **bf)[:, :, ::2], torch.zeros(7, 2, 64, **bf)):
         with pytest.raises(ValueError, match="bfloat16 tensor"):

@@ -166,3 +166,15 @@ def test_offsets_past_32_bits():
             want, P = O.attn_forward_real(f[0][i:i + 1], f[1][0], f[1][1], False, D ** -0.5)
             assert_within(f64_of(out)[i:i + 1], want, out_bound(P, f[1][1], want), f"sequence {i}, by_head={by_head}")
         del kv
+
+
+def test_what_belongs_together_comes_together():
+    d = Decode((2, 0), (50,), (7, 3), 2, 2, 64)
+    given = [d.q, d.pk, d.pv, d.d_seg, d.d_off, d.sk, d.sv, d.d_own, d.out]
+    for missing in (2, 3, 4, 6, 7):
+        with pytest.raises(ValueError, match="belongs"):
+            B.skipffn_attn_decode(*(None if i == missing else t for i, t in enumerate(given)), workspace=d.ws)
+    with pytest.raises(ValueError, match="prefix or own rows"):
+        B.skipffn_attn_decode(d.q, *[None] * 7, d.out, workspace=d.ws)
+    with pytest.raises(B.SkipFFNError):
+        B.skipffn_attn_decode(d.q, *given[1:8], d.q, workspace=d.ws)
