@@ -313,15 +313,15 @@ _HEADS = [c_int64 * (3 * n) for n in range(9)]
 
 
 def _heads(where, device, *tensors):
-    """What the library takes as skipffn_heads of tensors [tokens, heads, columns] whose columns lie together: the array that
+    """What the library takes as skipffn_heads of tensors [..., tokens, heads, columns] whose columns lie together: the array that
     holds them, and the address of each."""
     v = []
     for t, shape in tensors:
-        s = t.stride()
-        if t.shape != shape or t.dtype is not torch.bfloat16 or t.get_device() != device or (s[2] != 1 and shape[2] > 1):
+        *_, st, sh, sc = t.stride()
+        if t.shape != shape or t.dtype is not torch.bfloat16 or t.get_device() != device or (sc != 1 and shape[-1] > 1):
             raise ValueError(f"{where}: a bfloat16 tensor {tuple(shape)} on the device of the call, with contiguous columns, is wanted")
         # a stride that nothing is apart by is whatever the tensor was cut from
-        v += (t.data_ptr(), s[0] if shape[0] > 1 else 0, s[1] if shape[1] > 1 else 0)
+        v += (t.data_ptr(), st if shape[-3] > 1 else 0, sh if shape[-2] > 1 else 0)
     a = _HEADS[len(tensors)](*v)
     at = addressof(a)
     return a, range(at, at + 24 * len(tensors), 24)
@@ -404,7 +404,9 @@ def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, 
     n_seq, Hq, D = q.shape
     if prefix_k is None and suffix_k is None:
         raise ValueError(f"{where}: a prefix or own rows are wanted")
-    if len({t is None for t in (prefix_k, prefix_v, prefix_seg, group_off)}) > 1 or len({t is None for t in (suffix_k, suffix_v, suffix_len)}) > 1:
+    bare, alone = prefix_k is None, suffix_k is None
+    if bare != (prefix_v is None) or bare != (prefix_seg is None) or bare != (group_off is None) or \
+            alone != (suffix_v is None) or alone != (suffix_len is None):
         raise ValueError(f"{where}: a prefix, or own rows, come with all that belongs to them")
     Hkv = (suffix_k if prefix_k is None else prefix_k).shape[-2]
     Tp = n_groups = cap = seq_k = seq_v = 0
@@ -416,12 +418,11 @@ def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, 
         given += [(prefix_k, (Tp, Hkv, D)), (prefix_v, (Tp, Hkv, D))]
     if suffix_k is not None and n_seq > 0:
         cap = suffix_k.shape[1]
-        if suffix_k.shape != (n_seq, cap, Hkv, D) or suffix_v.shape != suffix_k.shape:
-            raise ValueError(f"{where}: own rows are tensors [{n_seq}, capacity, {Hkv}, {D}]")
         lens = _ints(suffix_len, n_seq, where, dev)
         if n_seq > 1:
             seq_k, seq_v = suffix_k.stride(0), suffix_v.stride(0)
-        given += [(suffix_k.select(0, 0), (cap, Hkv, D)), (suffix_v.select(0, 0), (cap, Hkv, D))]
+        own = (n_seq, cap, Hkv, D)
+        given += [(suffix_k, own), (suffix_v, own)]
     hold, at = _heads(where, dev, *given)
     pk, pv = at[2:4] if prefix_k is not None else (None, None)
     sk, sv = at[-2:] if suffix_k is not None and n_seq > 0 else (None, None)
