@@ -63,6 +63,8 @@ CASES = {
     "empty group and prefix": ((0, 2, 1, 0), (50, 0, 33), (0, 4, 2)),
     "many": ((19, 41, 3), (257, 900), tuple(range(63))),
     "long": ((1, 2, 0), (5000, 3001), (70, 0, 900)),
+    "large groups, short": ((40, 37, 5), (300, 250), tuple(i % 9 for i in range(82))),
+    "large groups, one without a prefix": ((33, 70, 0, 2), (0, 3000, 777), tuple(i * 7 % 130 for i in range(105))),
 }
 
 
@@ -125,6 +127,18 @@ def test_a_sequence_that_is_not_finite_leaves_the_others_as_they_are():
             assert np.array_equal(got[i, heads][:, keep], clean[i, heads][:, keep]), (i, kh)
             assert not np.isfinite(f[i, heads][:, list(hit)]).any()
     assert np.all(f[1, :g, 5] == np.inf) and np.all(f[6] == -np.inf) and np.all(np.isnan(f[3, g:, 7]))
+    # a large group of many products
+    w = Decode((50, 0), (700,), tuple(3 + i % 40 for i in range(50)), Hq, Hkv, D, seed=1)
+    w.run(D ** -0.5)
+    torch.cuda.synchronize()
+    before = bits_of(w.out)
+    w.sv[13, 2, 1, 4] = float("nan")
+    w.sv[40, 0, 0, 100] = float("inf")
+    w.run(D ** -0.5)
+    torch.cuda.synchronize()
+    after, hit = bits_of(w.out), np.zeros((50, Hq, D), bool)
+    hit[13, g:, 4] = hit[40, :g, 100] = True
+    assert np.array_equal(after[~hit], before[~hit]) and not np.isfinite(f64_of(w.out)[hit]).any()
     # the prefix of the second group: the first group's rows keep their bits
     d.pv[150, 1, 9] = float("nan")
     d.run(D ** -0.5)
