@@ -295,3 +295,58 @@ def test_values_that_are_not_finite_reach_the_rows_that_see_them_alone(Hq, Hkv, 
     assert np.array_equal(got[~hit], clean[~hit])
     assert not np.isfinite(f[hit]).any()
     assert torch.equal(p.saved[:4 * p.T * Hq], lse[:4 * p.T * Hq])
+
+
+def torch_check(p, causal, scale, heads, gradients):
+    """The same bounds as Prompt.check, in fp64 on the device, of the key/value heads listed."""
+    from attn_bounds import F, P16, SLACK, U
+    rep = p.Hq // p.Hkv
+    aq = ak = 0
+    for s, (nq, nk) in enumerate(zip(p.nq, p.nk)):
+        rq, rk = slice(aq, aq + nq), slice(ak, ak + nk)
+        aq, ak = aq + nq, ak + nk
+        hide = torch.ones(nq, nk, dtype=torch.bool, device="cuda").triu(nk - nq + 1) if causal else None
+        for kh in heads:
+            k, v = p.k[rk, kh].double(), p.v[rk, kh].double()
+            dk, dv, ek, ev = (torch.zeros_like(k) for _ in range(4))
+            for h in range(kh * rep, (kh + 1) * rep):
+                q, g = p.q[rq, h].double(), p.g[rq, h].double()
+                S = scale * (q @ k.T)
+                P = torch.softmax(S if hide is None else S.masked_fill(hide, -float("inf")), -1)
+                del S
+                out = P @ v
+                e_out = SLACK * ((U + F) * (P @ v.abs()) + U * out.abs())
+                assert bool(((p.out[rq, h].double() - out).abs() <= e_out).all()), ("out", s, h)
+                if not gradients:
+                    continue
+                e_delta = (g.abs() * (e_out + P16 * out.abs())).sum(1, keepdim=True)
+                dS = P * (g @ v.T - (g * out).sum(1, keepdim=True))
+                E = P * (e_delta + P16 * (g.abs() @ v.abs().T)) + (U + F) * dS.abs()
+                dq = scale * (dS @ k)
+                bound = SLACK * (scale * (E @ k.abs()) + U * dq.abs())
+                assert bool(((p.dq[rq, h].double() - dq).abs() <= bound).all()), ("dq", s, h)
+                dk += scale * (dS.T @ q)
+                dv += P.T @ g
+                ek += scale * (E.T @ q.abs())
+                ev += (U + F) * (P.T @ g.abs())
+            if gradients:
+                assert bool(((p.dk[rk, kh].double() - dk).abs() <= SLACK * (ek + U * dk.abs())).all()), ("dk", s, kh)
+                assert bool(((p.dv[rk, kh].double() - dv).abs() <= SLACK * (ev + U * dv.abs())).all()), ("dv", s, kh)
+
+
+@pytest.mark.parametrize("lens,Hq,Hkv,D,causal,heads", [((2944, 616, 1), 32, 8, 128, True, (0, 7)), ((577,) * 4, 16, 16, 64, False, (3, 15)),
+                                                        ((3500, 40), 28, 4, 96, True, (2,))], ids=str)
+def test_full_size_forward_and_backward(lens, Hq, Hkv, D, causal, heads):
+    print(f"attention {lens} heads {Hq}/{Hkv} D={D} causal={causal}", flush=True)
+    p = Prompt(lens, lens, Hq, Hkv, D)
+    p.forward(causal, D ** -0.5)
+    p.backward(causal, D ** -0.5)
+    torch.cuda.synchronize()
+    torch_check(p, causal, D ** -0.5, heads, True)
+
+
+def test_full_size_long_prompt():
+    p = Prompt((16384,), (16384,), 8, 2, 128)
+    p.forward(True, 128 ** -0.5)
+    torch.cuda.synchronize()
+    torch_check(p, True, 128 ** -0.5, (0, 1), False)
