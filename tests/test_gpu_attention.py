@@ -350,3 +350,43 @@ def test_full_size_long_prompt():
     p.forward(True, 128 ** -0.5)
     torch.cuda.synchronize()
     torch_check(p, True, 128 ** -0.5, (0, 1), False)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(40, 1, 64), (33, 1, 128), (64, 2, 24)])
+def test_many_query_heads_a_key_value_head(Hq, Hkv, D):
+    lens = (65, 33, 4)
+    p = Prompt(lens, lens, Hq, Hkv, D)
+    p.forward(True, D ** -0.5)
+    p.backward(True, D ** -0.5)
+    p.check(True, D ** -0.5, True)
+
+
+def test_results_in_column_ranges_and_by_head():
+    """out and the gradients as column ranges of wider rows, and as [head][token][column]: the same bits, and nothing between them."""
+    T, Hq, Hkv, D, lens = 133, 4, 2, 72, (100, 30)
+    p = Prompt(lens, lens, Hq, Hkv, D, "plain")
+    p.forward(True, 0.1)
+    p.backward(True, 0.1)
+    torch.cuda.synchronize()
+    want = [bits_of(t) for t in (p.out, p.dq, p.dk, p.dv)]
+    wide = torch.full((T, 20, 80), 7.0, dtype=torch.bfloat16, device="cuda")
+    other = torch.full((T, 6, 80), 7.0, dtype=torch.bfloat16, device="cuda")
+    ranges = [other[:, 1:1 + Hq, 8:], wide[:, 6:6 + Hq, 8:], wide[:, 11:11 + Hkv, 8:], wide[:, 15:15 + Hkv, 8:]]
+    byhead = [torch.full((h, T + 3, D), 7.0, dtype=torch.bfloat16, device="cuda")[:, :T].transpose(0, 1) for h in (Hq, Hq, Hkv, Hkv)]
+    for places in (ranges, byhead):
+        p.out, p.dq, p.dk, p.dv = places
+        p.forward(True, 0.1)
+        p.backward(True, 0.1)
+        torch.cuda.synchronize()
+        assert all(np.array_equal(bits_of(t), w) for t, w in zip(places, want))
+    used = torch.zeros(T, 20, 80, dtype=torch.bool, device="cuda")
+    for a, h in ((6, Hq), (11, Hkv), (15, Hkv)):
+        used[:sum(lens), a:a + h, 8:] = True
+    assert bool((wide[~used] == 7.0).all())
+    other[:sum(lens), 1:1 + Hq, 8:] = 7.0
+    assert bool((other == 7.0).all())
+    # gradients among the columns of an input are refused: what they span meets it
+    p.dq = wide[:, :Hq, :D]
+    p.q = wide[:, Hq:2 * Hq, :D]
+    with pytest.raises(B.SkipFFNError):
+        p.backward(True, 0.1)

@@ -192,3 +192,23 @@ def test_what_belongs_together_comes_together():
         B.skipffn_attn_decode(d.q, *[None] * 7, d.out, workspace=d.ws)
     with pytest.raises(B.SkipFFNError):
         B.skipffn_attn_decode(d.q, *given[1:8], d.q, workspace=d.ws)
+
+
+def test_queries_and_results_in_column_ranges_and_by_head():
+    Hq, Hkv, D = 6, 2, 40
+    d = Decode((3, 2, 1), (100, 300), (5, 0, 33, 64, 1, 7), Hq, Hkv, D)
+    d.run(0.2)
+    torch.cuda.synchronize()
+    want = bits_of(d.out)
+    fused = torch.full((d.n, Hq + 2 * Hkv, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    fused[:, :Hq] = d.q
+    wide = torch.full((d.n, Hq + 3, D + 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    byhead = torch.full((Hq, d.n, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    byhead.copy_(d.q.transpose(0, 1))
+    for q, out in ((fused[:, :Hq], wide[:, 2:2 + Hq, 8:]), (byhead.transpose(0, 1), torch.full_like(byhead, 7.0).transpose(0, 1))):
+        d.q, d.out = q, out
+        d.run(0.2)
+        torch.cuda.synchronize()
+        assert np.array_equal(bits_of(out), want)
+    wide[:, 2:2 + Hq, 8:] = 7.0
+    assert bool((wide == 7.0).all())
