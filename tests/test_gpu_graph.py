@@ -133,3 +133,33 @@ def test_attention_on_another_stream_than_the_default():
     side.synchronize()
     torch.cuda.synchronize()
     assert torch.equal(a, b)
+
+
+def test_attention_calls_at_once_on_two_streams():
+    """Two calls whose kernels may overlap, each with its own workspace, give what they give one after the other."""
+    Hq, Hkv, D, Tk = 8, 2, 128, 3000
+    def room(n):
+        return torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+    seg_q, seg_k = torch.tensor([0, 7, 30], dtype=torch.int32, device="cuda"), torch.tensor([0, 1200, Tk], dtype=torch.int32, device="cuda")
+    jobs = []
+    for _ in range(2):
+        q, k, v = (torch.randn(t, h, D, device="cuda").to(torch.bfloat16) for t, h in ((30, Hq), (Tk, Hkv), (Tk, Hkv)))
+        jobs.append((q, k, v, torch.zeros_like(q), room(B.skipffn_attn_forward_workspace_bytes(30, Tk, 2, Hq, Hkv, D))))
+    assert jobs[0][4].numel() > 16
+    for q, k, v, out, ws in jobs:
+        B.skipffn_attn_forward(q, k, v, out, seg_q, seg_k, workspace=ws)
+    torch.cuda.synchronize()
+    want = [job[3].clone() for job in jobs]
+    streams = [torch.cuda.Stream() for _ in jobs]
+    for _ in range(20):
+        for job in jobs:
+            job[3].zero_()
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        for s, (q, k, v, out, ws) in zip(streams, jobs):
+            with torch.cuda.stream(s):
+                B.skipffn_attn_forward(q, k, v, out, seg_q, seg_k, workspace=ws)
+        for s in streams:
+            torch.cuda.current_stream().wait_stream(s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(job[3], w) for job, w in zip(jobs, want))
