@@ -38,8 +38,9 @@ __device__ __forceinline__ uint32_t tile_off(int r, int chunk) {
 // The rows of one head of one sequence: row r at base + r * stride elements
 struct HeadRows { const bf16_t* base; int stride; };
 
-// A tile of N rows on its way through registers: issued as buffer loads, stored to LDS a tile later.  Rows at and past `rows`
-// and columns at and past the head's read zeros (so a masked weight of 0 never meets what lies there).
+// A tile of N rows on its way through registers: issued as buffer loads, stored to LDS a tile later.  Columns at and past the head's read
+// zeros, and so do rows at and past `rows` where rows are apart.  With a stride of less than a row's columns (0: every row is the same one) the last
+// row lies where they do and they read of it: never what is not the head's in this sequence, but they have to be masked by who uses them.
 template <int DP, int N, int THREADS = ATT_THREADS>
 struct TileLoad {
     static constexpr int CH = tile_row_bytes<DP>() / 16;        // 16-byte chunks of a row in LDS

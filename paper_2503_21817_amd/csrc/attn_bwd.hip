@@ -197,6 +197,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dkv_kernel
     TileLoad<DP, DKV_ROWS> lq, lg;
     const float* row_stat = (wave & 1) != 0 ? G.delta : P.lse;       // the first wavefront loads the log-sum-exps, the second delta
     float stat = 0.0f;
+    int tile_rows = 0;                                   // of the tile under way: the sequence's rows
     // step by step through the tiles of rows, the last first, head by head: of the next load, and of the tile in work
     const int r_last = (row_first + row_tiles - 1) * DKV_ROWS, r_first = row_first * DKV_ROWS;
     int head = kvh * g, load_r0 = r_last, r0 = r_last;
@@ -204,8 +205,8 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dkv_kernel
         const int r0 = load_r0;
         lq.load(HeadRows{P.q + head * P.q_head + (int64_t)q0 * P.q_tok, P.q_tok}, r0, nq, P.D, q_off);
         lg.load(HeadRows{G.go + head * G.go_head + (int64_t)q0 * G.go_tok, G.go_tok}, r0, nq, P.D, g_off);
-        // rows past the sequence's read 0: with q and grad_out of 0 they give weights of 1 on gradients of 0
-        const __amdgpu_buffer_rsrc_t rs = make_rsrc(row_stat + (int64_t)head * P.Tq + q0 + r0, (uint32_t)min(nq - r0, DKV_ROWS) * 4u);
+        tile_rows = min(nq - r0, DKV_ROWS);
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(row_stat + (int64_t)head * P.Tq + q0 + r0, (uint32_t)tile_rows * 4u);
         stat = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, lane * 4, 0, 0));
         load_r0 -= DKV_ROWS;
         if (load_r0 < r_first) { load_r0 = r_last; ++head; }
@@ -214,7 +215,11 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dkv_kernel
         char* st = stage + (n & 1) * STAGE;
         lq.store(st, tid);
         lg.store(st + TILE, tid);
-        if (wave < 2 && lane < DKV_ROWS) reinterpret_cast<float*>(st + 2 * TILE)[wave * DKV_ROWS + lane] = stat;
+        // Rows past the sequence's: their log-sum-exp is infinity, so that their weights are 0 whatever q and grad_out read for them (0, or the last
+        // row again where rows repeat or lie over one another); their delta is the 0 that it reads.  Here, not where it is loaded: there it would
+        // wait for the tiles
+        if (wave < 2 && lane < DKV_ROWS)
+            reinterpret_cast<float*>(st + 2 * TILE)[wave * DKV_ROWS + lane] = wave == 0 && lane >= tile_rows ? INFINITY : stat;
     };
     const uint32_t v_at = lds_addr_of(tv) + (uint32_t)(wave * 32 * ROWB) + rows_lane<DP>(lane);
     const uint32_t rows_at = lds_addr_of(stage) + rows_lane<DP>(lane), cols_at = lds_addr_of(stage) + cols_lane<DP>(lane);

@@ -1,0 +1,101 @@
+"""Attention at the edges of what its tensors may be: inputs that repeat a row for every token, rows that lie over one another, single
+tokens."""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_attention as A
+from attn_bounds import assert_within, grad_bounds, out_bound
+from oracle import skipffn_oracle as O
+from paper_2503_21817_amd import binding as B
+from helpers import bits_of, f64_of, to_dev_bf16
+
+pytestmark = pytest.mark.gpu
+
+
+def normal(rng, *shape):
+    return to_dev_bf16(O.f64_to_bf16_bits(rng.standard_normal(shape)))
+
+
+def step(q, k, v, g, nq, nk, causal, scale):
+    """out, dq, dk, dv of a packed batch whose tensors end with its last row."""
+    (T, Hq, D), (Tk, Hkv, _) = q.shape, k.shape
+    seg_q, seg_k = A.offsets(nq), A.offsets(nk)
+    out, dq = (torch.full((T, Hq, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    dk, dv = (torch.full((Tk, Hkv, D), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    sizes = (T, Tk, len(nq), Hq, Hkv, D)
+    saved = A.nbytes(B.skipffn_attn_saved_bytes(T, Hq))
+    B.skipffn_attn_forward(q, k, v, out, seg_q, seg_k, causal=causal, scale=scale, saved=saved,
+                           workspace=A.nbytes(B.skipffn_attn_forward_workspace_bytes(*sizes)))
+    B.skipffn_attn_backward(q, k, v, out, g, seg_q, seg_k, saved, dq, dk, dv, causal=causal, scale=scale,
+                            workspace=A.nbytes(B.skipffn_attn_backward_workspace_bytes(*sizes)))
+    torch.cuda.synchronize()
+    return out, dq, dk, dv
+
+
+def check(q, k, v, g, got, nq, nk, causal, scale):
+    q, k, v, g, out, dq, dk, dv = (f64_of(t.contiguous()) for t in (q, k, v, g, *got))
+    aq = ak = 0
+    for s, (n, m) in enumerate(zip(nq, nk)):
+        rq, rk = slice(aq, aq + n), slice(ak, ak + m)
+        aq, ak = aq + n, ak + m
+        b = O.attn_backward_real(q[rq], k[rk], v[rk], g[rq], causal, scale)
+        e = grad_bounds(q[rq], k[rk], v[rk], g[rq], scale, b)
+        assert_within(out[rq], b["out"], out_bound(b["P"], v[rk], b["out"]), f"out, sequence {s}")
+        for name, t, r in (("dq", dq, rq), ("dk", dk, rk), ("dv", dv, rk)):
+            assert_within(t[r], b[name], e[name], f"{name}, sequence {s}")
+
+
+# ---- rows past a sequence's end have no part in the gradients of its keys, whatever the strides make them read -----------------
+@pytest.mark.parametrize("repeated", ["g", "q", "qg", "qkvg"])
+@pytest.mark.parametrize("lens", [(50,), (33, 1, 95, 0, 64), (7, 130)], ids=str)
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 2, 64), (2, 1, 128), (3, 3, 72)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+def test_inputs_that_repeat_a_row_for_every_token(repeated, lens, Hq, Hkv, D, causal):
+    """The gradient of a sum over tokens is one row expanded over them."""
+    print(f"repeated {repeated} {lens} heads {Hq}/{Hkv} D={D} causal={causal}", flush=True)
+    rng, T = np.random.default_rng(D + len(lens)), sum(lens)
+    t = [normal(rng, 1 if x in repeated else T, h, D).expand(T, h, D) for x, h in (("q", Hq), ("k", Hkv), ("v", Hkv), ("g", Hq))]
+    got = step(*t, lens, lens, causal, 0.2)
+    check(*t, got, lens, lens, causal, 0.2)
+    same = step(*(x.contiguous() for x in t), lens, lens, causal, 0.2)
+    assert all(np.array_equal(bits_of(a), bits_of(b)) for a, b in zip(got, same))
+
+
+@pytest.mark.parametrize("stride", [8, 40, 64])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+def test_rows_that_lie_over_one_another(stride, causal):
+    """Token strides between 0 and the columns, heads apart."""
+    H, D, lens = 2, 72, (50, 37, 3)
+    print(f"rows {stride} apart, causal={causal}", flush=True)
+    rng, T = np.random.default_rng(stride), sum(lens)
+    t = []
+    for _ in range(4):
+        room = (T - 1) * stride + 128
+        t.append(normal(rng, H * room).as_strided((T, H, D), (stride, room, 1)))
+    got = step(*t, lens, lens, causal, 0.2)
+    check(*t, got, lens, lens, causal, 0.2)
+    same = step(*(x.contiguous() for x in t), lens, lens, causal, 0.2)
+    assert all(np.array_equal(bits_of(a), bits_of(b)) for a, b in zip(got, same))
+
+
+@pytest.mark.parametrize("nq,nk", [((1,), (1,)), ((1,), (40,)), ((1,), (3000,)), ((1, 0), (0, 5)), ((5,), (1,)), ((40,), (1,))], ids=str)
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 2, 64), (5, 1, 128), (1, 1, 8)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+def test_tensors_of_one_token(nq, nk, Hq, Hkv, D, causal):
+    print(f"one token {nq} over {nk} heads {Hq}/{Hkv} D={D} causal={causal}", flush=True)
+    rng = np.random.default_rng(D + sum(nk))
+    t = [normal(rng, n, h, D) for n, h in ((sum(nq), Hq), (sum(nk), Hkv), (sum(nk), Hkv), (sum(nq), Hq))]
+    check(*t, step(*t, nq, nk, causal, 0.2), nq, nk, causal, 0.2)
+
+
+def test_repeated_queries_of_large_scores():
+    """Rows past the end that repeat a query have scores of some hundred and no log-sum-exp of their own."""
+    lens, H, D = (41,), 2, 64
+    rng = np.random.default_rng(1)
+    q = (20.0 * normal(rng, 1, H, D)).expand(41, H, D)
+    k, v, g = (normal(rng, 41, H, D) for _ in range(3))
+    got = step(q, k, v, g, lens, lens, True, 1.0)
+    same = step(q.contiguous(), k, v, g, lens, lens, True, 1.0)
+    assert all(np.array_equal(bits_of(a), bits_of(b)) for a, b in zip(got, same))
+    assert all(torch.isfinite(t.float()).all() for t in got)
