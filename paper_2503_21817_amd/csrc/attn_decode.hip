@@ -144,8 +144,10 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
         top = sees ? halves_max(top) : -INFINITY;
-        if (__ballot((top - m) * c > 8.0f || (m == -INFINITY && top != -INFINITY)) != 0) {
-            const float now = fmaxf(m, top), scale = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - now) * c);
+        // the maximum may lag, as in the kernels over whole prompts, and each row by its own scores
+        const bool grow = (top - m) * c > 8.0f || (m == -INFINITY && top != -INFINITY);
+        if (__ballot(grow) != 0) {
+            const float now = grow ? fmaxf(m, top) : m, scale = grow ? __builtin_amdgcn_exp2f((m - now) * c) : 1.0f;
             l *= scale;
 #pragma unroll
             for (int db = 0; db < DP / 32; ++db)

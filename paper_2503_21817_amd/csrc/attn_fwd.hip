@@ -120,9 +120,10 @@ __global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fw
                 for (int i = 0; i < 16; ++i) top = fmaxf(top, s[kb][i]);
             top = halves_max(top);
             // The maximum may lag by up to a factor 2^8 of the weights, which bf16 and the fp32 sums hold as exactly: the sums are
-            // seldom scaled again
-            if (__ballot((top - m) * c > 8.0f || (m == -INFINITY && top != -INFINITY)) != 0) {
-                const float now = fmaxf(m, top), scale = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - now) * c);
+            // seldom scaled again.  Each row by its own scores: what its neighbours in the product see does not change how its weights are rounded
+            const bool grow = (top - m) * c > 8.0f || (m == -INFINITY && top != -INFINITY);
+            if (__ballot(grow) != 0) {
+                const float now = grow ? fmaxf(m, top) : m, scale = grow ? __builtin_amdgcn_exp2f((m - now) * c) : 1.0f;
                 l *= scale;
 #pragma unroll
                 for (int db = 0; db < DP / 32; ++db)

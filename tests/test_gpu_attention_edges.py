@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import test_gpu_attention as A
+from test_gpu_attn_decode import Decode
 from attn_bounds import assert_within, grad_bounds, out_bound
 from oracle import skipffn_oracle as O
 from paper_2503_21817_amd import binding as B
@@ -99,3 +100,51 @@ def test_repeated_queries_of_large_scores():
     same = step(q.contiguous(), k, v, g, lens, lens, True, 1.0)
     assert all(np.array_equal(bits_of(a), bits_of(b)) for a, b in zip(got, same))
     assert all(torch.isfinite(t.float()).all() for t in got)
+
+
+# ---- a row's bits are its own: neither a neighbour's queries nor keys that it does not see change its rounding --------------------
+@pytest.mark.parametrize("Hq,Hkv,D,nq,nk", [(4, 2, 128, (200, 70), (200, 70)), (4, 4, 64, (200, 130), (200, 130)), (32, 8, 128, (150,) * 9, (150,) * 9),
+                                            (8, 2, 80, (40,), (3000,))], ids=str)
+def test_a_query_or_an_unseen_key_leaves_the_other_rows_bits(Hq, Hkv, D, nq, nk):
+    print(f"neighbours, heads {Hq}/{Hkv} D={D} {nq} over {nk}", flush=True)
+    p = A.Prompt(nq, nk, Hq, Hkv, D, "fused" if nq == nk else "plain")
+    p.q[..., 0] = 1.0
+    p.forward(True, 0.2)
+    torch.cuda.synchronize()
+    clean, stat = bits_of(p.out), p.saved[:4 * p.T * Hq].view(torch.float32).view(Hq, p.T).clone()
+    q, k = p.q.clone(), p.k.clone()
+    hit = np.zeros(clean.shape[:2], bool)
+    row = nq[0] - 20                                     # a query of large scores among ordinary ones
+    p.q[row] *= 64.0
+    hit[row] = True
+    key = nk[0] - 15                                     # a key of infinite scores, seen by the last rows of the first sequence
+    p.k[key, 0, 0] = float("inf")
+    hit[nq[0] - 15:nq[0], :Hq // Hkv] = True
+    p.forward(True, 0.2)
+    torch.cuda.synchronize()
+    after = p.saved[:4 * p.T * Hq].view(torch.float32).view(Hq, p.T)
+    rows = ~hit[:sum(nq)]
+    assert np.array_equal(bits_of(p.out)[:sum(nq)][rows], clean[:sum(nq)][rows])
+    assert torch.equal(after[:, :sum(nq)].T[torch.from_numpy(rows).cuda()], stat[:, :sum(nq)].T[torch.from_numpy(rows).cuda()])
+    assert np.isnan(f64_of(p.out)[nq[0] - 15:nq[0], :Hq // Hkv]).all()
+    p.q.copy_(q)
+    p.k.copy_(k)
+    p.forward(True, 0.2)
+    torch.cuda.synchronize()
+    assert np.array_equal(bits_of(p.out), clean)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (4, 1, 64)])
+def test_a_sequence_leaves_the_bits_of_those_that_share_its_prefix(Hq, Hkv, D):
+    d = Decode((6, 0), (900,), (40, 33, 0, 70, 5, 1), Hq, Hkv, D)
+    d.q[..., 0] = 1.0
+    d.run(0.2)
+    torch.cuda.synchronize()
+    clean = bits_of(d.out)
+    d.q[2] *= 64.0
+    d.sk[3, 60, :, 0] = float("inf")
+    d.run(0.2)
+    torch.cuda.synchronize()
+    got = bits_of(d.out)
+    assert np.array_equal(got[[0, 1, 4, 5]], clean[[0, 1, 4, 5]])
+    assert np.isnan(f64_of(d.out)[3]).all() and np.isfinite(f64_of(d.out)[2]).all()
