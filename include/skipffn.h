@@ -305,8 +305,8 @@ int skipffn_token_merge_backward(const void* grad_out, const int32_t* seg_host, 
  * D % 8 == 0, 8 <= D <= 128, Hq a multiple of Hkv, n_seq <= 65535, (max(Tq, Tk) / 32 + 2 n_seq) Hq < 2^25.
  * Scores, softmax sums and products are accumulated in fp32; the weights P are rounded to bf16 before they
  * meet v (the matrix cores' operand type).  Deterministic: every sum has a fixed order.
- * A k_j or v_j that is not finite reaches the queries that see key j, and no others; rows that belong to no
- * sequence may hold anything.
+ * A k_j or v_j that is not finite reaches the queries that see key j, and no others: a score of minus infinity is a
+ * weight of 0, and a query that sees keys, but such scores alone, is NaN.  Rows that belong to no sequence may hold anything.
  * The workspace is for the keys of few queries, which are cut into parts: ask for the sizes of the call (more
  * queries may need less), or for the largest answer of the calls to come.  As everywhere, calls that may
  * overlap in time need workspaces of their own. */
@@ -354,8 +354,8 @@ int skipffn_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int
  *   suffix_k, suffix_v        [n_seq][suffix_capacity, Hkv, D], sequence s suffix_k_seq (suffix_v_seq) elements
  *                             after the one before it.  Not read where suffix_capacity == 0
  *   suffix_len  i32 [n_seq] device: own rows of every sequence (clamped to 0 .. suffix_capacity)
- * A sequence with no rows at all gives a zero row.  What is not finite among a sequence's own rows reaches that
- * sequence alone.  Types, scale and shapes as above, (n_seq + n_groups + 1) Hq < 2^24, strides by sequence < 2^36;
+ * A sequence with no rows at all gives a zero row, one of nothing but scores of minus infinity NaN.  What is not finite
+ * among a sequence's own rows reaches that sequence alone.  Types, scale and shapes as above, (n_seq + n_groups + 1) Hq < 2^24, strides by sequence < 2^36;
  * out may not meet q or the caches.  workspace: at least skipffn_attn_decode_workspace_bytes(...), which holds fp32 rows of the parts
  * that long caches are cut into.  The parts depend on the bounds of the call (Tp, suffix_capacity, n_groups),
  * not on the lengths on the device.  Deterministic. */

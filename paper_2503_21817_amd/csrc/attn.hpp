@@ -13,6 +13,8 @@
 // 4 rows x 64 bytes (ds_read_b64_tr_b16, the operand whose contraction runs along the tokens).
 #pragma once
 
+#include <cfloat>
+
 #include "kernels.hpp"
 #include "segments.hpp"
 

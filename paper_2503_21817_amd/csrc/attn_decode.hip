@@ -83,7 +83,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
     const uint32_t sk_off = Load::first(lane, P.sk_tok, P.D), sv_off = Load::first(lane, P.sv_tok, P.D);
     Load lk, lv;
     int next_keys = 0, next_of = -1;                     // of the tile under way: its keys, and whose they are (-1: all rows')
-    bool dropped = false;
+    bool dropped = false, seen = false;                  // seen: the row sees a key of the wavefront's
     auto own_tile = [&](int u, int& i, int& k0, int& n) {    // member, first key, its keys
         i = __builtin_ctzll(__ballot(u < own_sum));
         k0 = (u - __builtin_amdgcn_readlane(own_sum - own_tiles, i)) * DEC_KEYS;
@@ -118,6 +118,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
             dropped = true;
         }
         const bool sees = next_of < 0 || member == next_of;
+        seen |= sees;
         lk.store(tk, lane);
         lv.store(tv, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -189,6 +190,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
     }
     // join the wavefronts: [column][row] of each where its tiles were
     l = halves_sum(l);
+    if (seen) m = fmaxf(m, -FLT_MAX);                    // minus infinity: no key, as in attn_join.hip
     float* mine = reinterpret_cast<float*>(tk);
 #pragma unroll
     for (int db = 0; db < DP / 32; ++db)
@@ -227,7 +229,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
         for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(P.part + at * attn_padded_columns(DP) + jd + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
         return;
     }
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;   // a row that sees no key is zero
+    const float inv = top == -INFINITY ? 0.0f : 1.0f / sum;   // a row that sees no key is zero
     bf16_t* out = P.out + (int64_t)seq * P.o_tok + hq * P.o_head;
 #pragma unroll
     for (int j = 0; j < PER; j += 4)

@@ -179,6 +179,8 @@ __global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fw
         if (more) load_q(next_it, next);
         l = halves_sum(l);
         if (PARTS && u.any) {
+            // keys seen, all with scores of minus infinity: not the infinity of a part without any (see attn_join.hip)
+            if (u.t0 < u.t1 && row_keys > u.t0 * KEYS) m = fmaxf(m, -FLT_MAX);
             if (row < nq) {
                 const int64_t at = ((int64_t)(it.q0 + row) * P.Hq + u.head) * P.splits + part;
                 if (h == 0) {
@@ -193,11 +195,13 @@ __global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fw
                             f32x4{acc[db][4 * i], acc[db][4 * i + 1], acc[db][4 * i + 2], acc[db][4 * i + 3]};
             }
         } else if (u.any) {
-            const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // a row that sees no key is zero
+            // A row that sees no key is zero.  One that does has a weight of 1 at its maximum; if all its scores are minus infinity it is 0 / 0
+            const bool none = row_keys <= 0;
+            const float inv = none ? 0.0f : 1.0f / l;
             store_rows<DP>(P.out + u.head * P.o_head + (int64_t)(it.q0 + u.row0) * P.o_tok, P.o_tok, min(nq - u.row0, ATT_ROWS), acc, inv, P.D,
                            unhoisted(lane), smem + (2 * TILE < ROWS ? 0 : (stage ^ 1) * 2 * TILE) + wave * 32 * tile_row_bytes<DP>());
             if (P.lse != nullptr && h == 0 && row < nq)
-                P.lse[(int64_t)u.head * P.Tq + it.q0 + row] = l == 0.0f ? INFINITY : fmaf(m, c, __builtin_amdgcn_logf(l));
+                P.lse[(int64_t)u.head * P.Tq + it.q0 + row] = none ? INFINITY : fmaf(m, c, __builtin_amdgcn_logf(l));
         }
         if (!more) return;
         __syncthreads();                                 // both tiles have been read

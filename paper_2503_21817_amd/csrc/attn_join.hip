@@ -40,7 +40,10 @@ __global__ __launch_bounds__(ATT_THREADS) void attn_join_kernel(const AttnJoinAr
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
     const float w = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f((m - top) * P.scale_log2);
     const float sum = wave_sum(w * l);
-    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;   // a row that sees no key is zero
+    // A row that sees no key, and it alone, has no maximum in any part: it is zero.  Where keys are seen and all scores are minus infinity the part's
+    // maximum is the lowest number and its sum 0: no weight beside other parts, and 0 / 0 if there are no others
+    const bool none = top == -INFINITY;
+    const float inv = none ? 0.0f : 1.0f / sum;
     float o[V] = {};
     for (int i0 = 0;;) {
 #pragma unroll
@@ -53,7 +56,7 @@ __global__ __launch_bounds__(ATT_THREADS) void attn_join_kernel(const AttnJoinAr
         if ((i0 += 8) >= P.splits) break;
         fetch(i0);
     }
-    if (P.lse != nullptr && lane == 0) P.lse[(int64_t)head * P.T + t] = sum == 0.0f ? INFINITY : fmaf(top, P.scale_log2, __builtin_amdgcn_logf(sum));
+    if (P.lse != nullptr && lane == 0) P.lse[(int64_t)head * P.T + t] = none ? INFINITY : fmaf(top, P.scale_log2, __builtin_amdgcn_logf(sum));
     if (lane * V >= P.D) return;
     bf16_t* out = P.out + (int64_t)t * P.o_tok + head * P.o_head + lane * V;
     if constexpr (V == 2) *reinterpret_cast<uint32_t*>(out) = pack_bf16x2(o[0] * inv, o[1] * inv);

@@ -181,7 +181,8 @@ struct AttnArgs {
     float* lse;                                   // [Hq][Tq], base 2, or null; infinity: the row sees no key
     int splits; float* part; float* stat;         // forward, splits > 1: as in AttnJoinArgs
 };
-// Rows whose keys are cut into parts: row (t, h), part z: statistics (largest score, sum of weights) at stat[2 * ((t * Hq + h) * splits + z)],
+// Rows whose keys are cut into parts: row (t, h), part z: statistics (largest score, -infinity where the row sees no key of the part and there alone; sum
+// of weights) at stat[2 * ((t * Hq + h) * splits + z)],
 // unnormalised columns at part[((t * Hq + h) * splits + z) * attn_padded_columns(D)]
 constexpr int ATTN_MAX_SPLITS = 64;
 struct AttnJoinArgs {

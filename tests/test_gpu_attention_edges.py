@@ -148,3 +148,95 @@ def test_a_sequence_leaves_the_bits_of_those_that_share_its_prefix(Hq, Hkv, D):
     got = bits_of(d.out)
     assert np.array_equal(got[[0, 1, 4, 5]], clean[[0, 1, 4, 5]])
     assert np.isnan(f64_of(d.out)[3]).all() and np.isfinite(f64_of(d.out)[2]).all()
+
+
+# ---- a row that sees keys, all with scores of minus infinity: 0 / 0, not the zeros of a row that sees none ------------------------
+def against_all_but(keys, q, k):
+    """Every query's product with the keys listed is minus infinity."""
+    q[..., 0] = -1.0
+    k[keys, :, 0] = float("inf")
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,lens", [(4, 2, 128, (70, 45)), (4, 4, 64, (33, 130)), (32, 8, 128, (150,) * 9), (6, 2, 96, (40, 40))], ids=str)
+def test_a_row_whose_every_score_is_minus_infinity(Hq, Hkv, D, lens):
+    print(f"minus infinity, heads {Hq}/{Hkv} D={D} {lens}", flush=True)
+    p = A.Prompt(lens, lens, Hq, Hkv, D)
+    p.forward(True, 0.2)
+    p.backward(True, 0.2)
+    torch.cuda.synchronize()
+    clean = [bits_of(t) for t in (p.out, p.dq, p.dk, p.dv)]
+    n = lens[0]
+    against_all_but([0], p.q[:n], p.k[:n])               # the first row sees the first key alone
+    p.forward(True, 0.2)
+    p.backward(True, 0.2)
+    torch.cuda.synchronize()
+    out = f64_of(p.out)
+    assert np.isnan(out[0]).all() and np.isnan(f64_of(p.dq)[0]).all() and np.isnan(f64_of(p.dv)[0]).all()
+    # the others as if the key were not there
+    q, k, v = (f64_of(t)[1:n] for t in (p.q, p.k, p.v))
+    want, P = O.attn_forward_real(q, k, v, True, 0.2)
+    assert_within(out[1:n], want, out_bound(P, v, want), "out")
+    for t, c in zip((p.out, p.dq, p.dk, p.dv), clean):   # and nothing of it in the next sequences
+        assert np.array_equal(bits_of(t)[n:], c[n:])
+    against_all_but(slice(0, n), p.q[:n], p.k[:n])
+    for causal in (True, False):
+        p.forward(causal, 0.2)
+        torch.cuda.synchronize()
+        assert np.isnan(f64_of(p.out)[:n]).all() and np.isfinite(f64_of(p.out)[n:sum(lens)]).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (4, 4, 64)])
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+def test_parts_whose_every_score_is_minus_infinity(Hq, Hkv, D, causal):
+    """Keys cut into parts: some parts of nothing but such scores have weight 0; if all are, the row is not a number."""
+    nq, nk = (9, 20), (5, 4500)
+    print(f"minus infinity in parts, heads {Hq}/{Hkv} D={D} causal={causal}", flush=True)
+    for hidden in (slice(0, 3000), slice(1000, 4400), slice(0, 4500)):
+        p = A.Prompt(nq, nk, Hq, Hkv, D, "cache")
+        assert p.fws.numel() > 16
+        q, k, v = p.q[9:29], p.k[5:4505], p.v[5:4505]
+        against_all_but(hidden, q, k)
+        p.forward(causal, 0.2)
+        torch.cuda.synchronize()
+        out = f64_of(p.out)
+        if causal:
+            assert np.all(out[:4] == 0)                  # these see no key
+        assert np.isfinite(out[:9]).all()
+        if hidden == slice(0, 4500):
+            assert np.isnan(out[9:29]).all()
+            continue
+        keep = np.ones(4500, bool)
+        keep[hidden] = False
+        f = [f64_of(t) for t in (q, k, v)]
+        want, weights = np.zeros(f[0].shape), np.zeros((Hq, 20, 4500))
+        for i in range(20):                              # row i sees the first nk - nq + 1 + i keys
+            sees = keep & (np.arange(4500) <= 4480 + i if causal else True)
+            want[i:i + 1], P = O.attn_forward_real(f[0][i:i + 1], f[1][sees], f[2][sees], False, 0.2)
+            weights[:, i, sees] = P[:, 0]
+        assert_within(out[9:29], want, out_bound(weights, f[2], want), f"out without {hidden}")
+
+
+@pytest.mark.parametrize("prefix", [0, 70, 3000])
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 2, 128), (4, 1, 64)])
+def test_single_tokens_whose_every_score_is_minus_infinity(prefix, Hq, Hkv, D):
+    print(f"minus infinity, single tokens, prefix {prefix}, heads {Hq}/{Hkv} D={D}", flush=True)
+    d = Decode((4, 0), (prefix,), (40, 0, 300, 7), Hq, Hkv, D)
+    d.q[..., 0] = -1.0
+    d.sk[0, :, :, 0] = float("inf")
+    d.sk[2, 30:, :, 0] = float("inf")
+    d.run(0.2)
+    torch.cuda.synchronize()
+    out = f64_of(d.out)
+    if prefix == 0:
+        assert np.isnan(out[0]).all() and np.all(out[1] == 0)
+    f = {n: f64_of(getattr(d, n)) for n in ("q", "pk", "pv", "sk", "sv")}
+    want, seen = O.attn_decode_real(f["q"], f["pk"], f["pv"], d.seg, d.off, f["sk"], f["sv"], [0, 0, 30, 7], 0.2)
+    for i, (k, v, P) in enumerate(seen):                 # the rows of such scores as if they were not there
+        if i > 0 or prefix > 0:
+            assert_within(out[i:i + 1], want[i:i + 1], out_bound(P[:, None], v, want[i:i + 1]), f"sequence {i}")
+    d.pk[..., 0] = float("inf")
+    d.run(0.2)
+    torch.cuda.synchronize()
+    out = f64_of(d.out)
+    assert np.isnan(out[0]).all() and np.isfinite(out[2:]).all()
+    assert np.isnan(out[1]).all() if prefix > 0 else np.all(out[1] == 0)
