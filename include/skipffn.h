@@ -331,6 +331,7 @@ int skipffn_attn_forward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int6
  *                  are left as they were.  They may be column ranges of one tensor (no element
  *                  is shared); what they span meets none of the inputs.
  *   workspace      at least skipffn_attn_backward_workspace_bytes(...)
+ * Shapes as above, and ((Tq / 32 + n_seq) (Hq / Hkv) / 4 + n_seq) Hkv < 2^24, (Tk / 128 + n_seq) Hkv < 2^24.
  * Deterministic.  What is not finite in one sequence may reach any gradient of that sequence, and none of another. */
 size_t skipffn_attn_backward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D);
 int skipffn_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D,

@@ -825,9 +825,14 @@ namespace {
 int check_attn(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, float scale) {
     if (Tq < 0 || Tk < 0 || n_seq < 0 || Hq <= 0 || Hkv <= 0 || D <= 0 || !(scale > 0.0f) || !std::isfinite(scale)) return SKIPFFN_EINVAL;
     if (Hq % Hkv != 0 || (D & 7) || D > ATTN_MAX_D || n_seq > 65535 || Hq > 65535 || Tq >= (1 << 30) || Tk >= (1 << 30)) return SKIPFFN_ESHAPE;
-    // grids of workgroups by queries and by keys (a launch has fewer than 2^32 threads), and the kernels' 32-bit products of blocks and heads
+    // the kernels' 32-bit products of blocks and heads
     if ((std::max(Tq, Tk) / 32 + 2 * n_seq) * Hq >= ((int64_t)1 << 25)) return SKIPFFN_ESHAPE;
     return SKIPFFN_OK;
+}
+int check_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, float scale) {
+    const int st = check_attn(Tq, Tk, n_seq, Hq, Hkv, D, scale);
+    // a launch has fewer than 2^32 threads (the forward's workgroups go on to further pieces: as many as fit the chip)
+    return st == SKIPFFN_OK && attn_backward_workgroups(Tq, Tk, n_seq, Hq, Hkv) >= ((int64_t)1 << 24) ? SKIPFFN_ESHAPE : st;
 }
 // bytes from the first element to past the last one
 int64_t heads_span(const skipffn_heads* t, int64_t T, int64_t H, int64_t D) {
@@ -886,7 +891,7 @@ size_t skipffn_attn_forward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_se
     return parts_ws(Tq * Hq, D, attn_forward_splits(Tq, Tk, n_seq, Hq, Hkv, D, num_cus())).total;
 }
 size_t skipffn_attn_backward_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D) {
-    if (check_attn(Tq, Tk, n_seq, Hq, Hkv, D, 1.0f) != SKIPFFN_OK) return 0;
+    if (check_attn_backward(Tq, Tk, n_seq, Hq, Hkv, D, 1.0f) != SKIPFFN_OK) return 0;
     return align_up((size_t)Tq * Hq * 4) + 256;
 }
 
@@ -922,7 +927,7 @@ int skipffn_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int
                           const skipffn_heads* grad_out, const int32_t* seg_q, const int32_t* seg_k, int causal, float scale,
                           const void* saved, const skipffn_heads* grad_q, const skipffn_heads* grad_k, const skipffn_heads* grad_v,
                           void* workspace, size_t workspace_bytes, void* stream) {
-    int st = check_attn(Tq, Tk, n_seq, Hq, Hkv, D, scale);
+    int st = check_attn_backward(Tq, Tk, n_seq, Hq, Hkv, D, scale);
     if (st != SKIPFFN_OK) return st;
     if ((st = check_heads(q, Tq, Hq, D, false)) || (st = check_heads(k, Tk, Hkv, D, false)) || (st = check_heads(v, Tk, Hkv, D, false)) ||
         (st = check_heads(out, Tq, Hq, D, false)) || (st = check_heads(grad_out, Tq, Hq, D, false)) || (st = check_heads(grad_q, Tq, Hq, D, true)) ||

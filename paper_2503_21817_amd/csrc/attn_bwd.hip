@@ -9,6 +9,8 @@
 //
 // Bound by power in long prompts and by the bytes of q, out and their gradients in short ones.  32 / 8 heads of 128, us (TFLOP/s of each kernel's own
 // products): 4 x 2944 tokens dQ 410-416 (1025-1040), dK and dV 637-645 (880-890); 16 x 616 dQ 125-136 (550-600), dK and dV 156-168 (590-640).
+#include <algorithm>
+
 #include "attn.hpp"
 
 namespace skipffn {
@@ -301,8 +303,16 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_dkv_kernel
     }
 }
 
+static int64_t key_workgroups(const AttnArgs& a) { return ((int64_t)a.Tk / DKV_KEYS + a.n_seq) * a.Hkv; }
+
+int64_t attn_backward_workgroups(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv) {
+    AttnArgs a{};
+    a.Tq = (int)Tq; a.Tk = (int)Tk; a.n_seq = (int)n_seq; a.Hq = (int)Hq; a.Hkv = (int)Hkv;
+    return std::max(attn_query_workgroups(a), key_workgroups(a));
+}
+
 hipError_t launch_attn_backward(const AttnArgs& a, const AttnGrads& gr, hipStream_t s) {
-    const dim3 gq((uint32_t)attn_query_workgroups(a)), gk((uint32_t)(((int64_t)a.Tk / DKV_KEYS + a.n_seq) * a.Hkv));
+    const dim3 gq((uint32_t)attn_query_workgroups(a)), gk((uint32_t)key_workgroups(a));
     if (a.D <= 64) attn_dq_kernel<64><<<gq, ATT_THREADS, 0, s>>>(a, gr);
     else if (a.D <= 96) attn_dq_kernel<96><<<gq, ATT_THREADS, 0, s>>>(a, gr);
     else attn_dq_kernel<128><<<gq, ATT_THREADS, 0, s>>>(a, gr);

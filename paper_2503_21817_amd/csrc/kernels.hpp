@@ -219,6 +219,7 @@ hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s);
 // parts that the keys of a query are cut into
 int attn_forward_splits(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int ncu);
 hipError_t launch_attn_forward(const AttnArgs& a, int ncu, hipStream_t s);
+int64_t attn_backward_workgroups(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv);   // of the larger of its launches
 hipError_t launch_attn_backward(const AttnArgs& a, const AttnGrads& g, hipStream_t s);
 
 // ---- GEMMs -----------------------------------------------------------------------

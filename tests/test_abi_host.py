@@ -405,3 +405,16 @@ def test_attention_binding_refuses_what_the_library_cannot_see():
         B._buffer(torch.zeros(15, dtype=torch.uint8), 16, "call", -1)
     # a dimension of one has whatever stride it was cut with
     assert list(B._heads("call", -1, (torch.zeros(1, 7, 64, **bf)[:, 3:4], (1, 1, 64)))[0])[1:] == [0, 0]
+
+
+def test_attention_backward_refuses_grids_past_a_launch():
+    """A launch has fewer than 2^32 threads.  ((Tq / 32 + n) g / 4 + n) Hkv workgroups of 256 are the kernel's by queries."""
+    def call(n, H, T=63):
+        return attn_bwd(Tq=T, Tk=T, n=n, Hq=H, Hkv=H, D=64, t={i: heads(FAR[i], head=64, H=H) for i in range(8)}, ws=None)
+    # ((1 + 65535) / 4 + 65535) * 256 = 20,971,264 workgroups
+    assert call(65535, 256) == B.ESHAPE
+    assert B.skipffn_attn_backward_workspace_bytes(63, 63, 65535, 256, 256, 64) == 0
+    # ((1 + 52428) / 4 + 52428) * 256 = 16,776,960 are the last to fit 2^24; one sequence more makes 16,777,216
+    assert call(52428, 256) == B.EWORKSPACE and call(52429, 256) == B.ESHAPE
+    # the forward's workgroups stay and go on, however many pieces there are
+    assert attn_fwd(Tq=63, Tk=63, n=65535, Hq=256, Hkv=256, out=heads(FAR[0], H=256), **{x: heads(FAR[0], H=256) for x in "qkv"}) == B.EINVAL
