@@ -849,6 +849,7 @@ int check_heads(const skipffn_heads* t, int64_t T, int64_t H, int64_t D, bool wr
     return SKIPFFN_OK;
 }
 bool heads_meet(const skipffn_heads* a, int64_t Ta, int64_t Ha, const skipffn_heads* b, int64_t Tb, int64_t Hb, int64_t D) {
+    if (Ta <= 0 || Tb <= 0) return false;                // no memory: wherever it points to
     const uintptr_t x = reinterpret_cast<uintptr_t>(a->data), y = reinterpret_cast<uintptr_t>(b->data);
     return x < y + (uintptr_t)heads_span(b, Tb, Hb, D) && y < x + (uintptr_t)heads_span(a, Ta, Ha, D);
 }
@@ -939,10 +940,10 @@ int skipffn_attn_backward(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int
     const skipffn_heads* ins[5] = {q, out, grad_out, k, v};
     const skipffn_heads* outs[3] = {grad_q, grad_k, grad_v};
     for (int o = 0; o < 3; ++o) {
-        const int64_t To = o == 0 ? Tq : Tk, Ho = o == 0 ? Hq : Hkv;
+        const int64_t To = o == 0 ? Tq : Tk, Ho = o == 0 ? Hq : Hkv, Tnext = o == 2 ? Tq : Tk;
         for (int i = 0; i < 5; ++i)
             if (heads_meet(outs[o], To, Ho, ins[i], i < 3 ? Tq : Tk, i < 3 ? Hq : Hkv, D)) return SKIPFFN_EINVAL;
-        if (To > 0 && outs[o]->data == outs[(o + 1) % 3]->data) return SKIPFFN_EINVAL;
+        if (To > 0 && Tnext > 0 && outs[o]->data == outs[(o + 1) % 3]->data) return SKIPFFN_EINVAL;
     }
     if (Tq > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < align_up((size_t)Tq * Hq * 4))) return SKIPFFN_EWORKSPACE;
     hipStream_t s = (hipStream_t)stream;

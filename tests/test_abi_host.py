@@ -418,3 +418,14 @@ def test_attention_backward_refuses_grids_past_a_launch():
     assert call(52428, 256) == B.EWORKSPACE and call(52429, 256) == B.ESHAPE
     # the forward's workgroups stay and go on, however many pieces there are
     assert attn_fwd(Tq=63, Tk=63, n=65535, Hq=256, Hkv=256, out=heads(FAR[0], H=256), **{x: heads(FAR[0], H=256) for x in "qkv"}) == B.EINVAL
+
+
+def test_tensors_without_tokens_meet_nothing():
+    """Where there are no queries, or no keys, what their tensors point to is nobody's memory."""
+    span = lambda i, at: heads(FAR[i] + at)              # 64 tokens of 4 heads of 64: 32 KiB
+    # no keys: k, v and their gradients anywhere inside the others
+    assert attn_bwd(Tk=0, sk=FAKE, t={1: span(5, 1024), 2: span(5, 2048)}, ws=None) == B.EWORKSPACE
+    assert attn_bwd(Tk=0, sk=FAKE, t={6: span(0, 1024), 7: span(5, 0)}, ws=None) == B.EWORKSPACE
+    assert attn_bwd(Tk=0, sk=FAKE, t={6: span(5, 0), 7: span(5, 0)}, ws=None) == B.EWORKSPACE
+    # tokens that are there still meet
+    assert attn_bwd(t={1: span(5, 1024)}) == B.EINVAL and attn_bwd(t={6: span(5, 0)}) == B.EINVAL
