@@ -1,5 +1,5 @@
-"""Attention at the edges of what its tensors may be: inputs that repeat a row for every token, rows that lie over one another, single
-tokens."""
+"""Attention at the edges of what its tensors may be: inputs that repeat a row for every token, rows that lie over one another, one
+token, scores without bounds."""
 import numpy as np
 import pytest
 import torch
@@ -240,3 +240,32 @@ def test_single_tokens_whose_every_score_is_minus_infinity(prefix, Hq, Hkv, D):
     out = f64_of(d.out)
     assert np.isnan(out[0]).all() and np.isfinite(out[2:]).all()
     assert np.isnan(out[1]).all() if prefix > 0 else np.all(out[1] == 0)
+
+
+# ---- gradients of peaked rows ------------------------------------------------------------------------------------------------
+def test_gradients_of_peaked_rows():
+    """Queries of 30 times the usual size, as in the forward's test: weights are formed again from scores and log-sum-exps of some hundred,
+    and those of keys that a row does not see overflow before they are masked."""
+    lens, H, D, scale = (257, 90, 33), 2, 64, 0.125
+    p = A.Prompt(lens, lens, H, H, D, "plain", q_std=30.0)
+    p.forward(True, scale)
+    p.backward(True, scale)
+    torch.cuda.synchronize()
+    f, a = {n: f64_of(getattr(p, n)) for n in ("q", "k", "v", "g", "dq", "dk", "dv")}, 0
+    for s, n in enumerate(lens):
+        r = slice(a, a + n)
+        a += n
+        q, k, v, g = (f[x][r] for x in "qkvg")
+        b = O.attn_backward_real(q, k, v, g, True, scale)
+        e = grad_bounds(q, k, v, g, scale, b)
+        # a score, and the log-sum-exp, is off by up to 0.0014 in the exponent: a weight by eta of itself.  out is then off by eta A with A = P |v|
+        # more, so delta by |g| . eta A, dS by eta |dS| + P (that), and what is summed from them accordingly
+        eta = 0.002
+        for h in range(H):
+            A_ = b["P"][h] @ np.abs(v[:, h])
+            E = eta * (np.abs(b["dS"][h]) + b["P"][h] * (np.abs(g[:, h]) * A_).sum(axis=1, keepdims=True))
+            e["dq"][:, h] += 1.1 * scale * (E @ np.abs(k[:, h]))
+            e["dk"][:, h] += 1.1 * scale * (E.T @ np.abs(q[:, h]))
+            e["dv"][:, h] += 1.1 * eta * (b["P"][h].T @ np.abs(g[:, h]))
+        for name in ("dq", "dk", "dv"):
+            assert_within(f[name][r], b[name], e[name], f"{name}, sequence {s}")
