@@ -7,8 +7,9 @@
 // no fp32 traffic for partial dQ.  The weights and dS are rounded to bf16 for the products they enter, as the matrix cores want them; delta
 // and everything summed is fp32.
 //
-// Bound by power in long prompts and by the bytes of q, out and their gradients in short ones.  32 / 8 heads of 128, us (TFLOP/s of each kernel's own
-// products): 4 x 2944 tokens dQ 410-416 (1025-1040), dK and dV 637-645 (880-890); 16 x 616 dQ 125-136 (550-600), dK and dV 156-168 (590-640).
+// dQ is bound by power in long prompts, dK and dV less so (matrix cores busy 49 % of the time at the clock at which dQ has 56 %: their causal pieces are up to
+// a third longer than an even share); both by the bytes of q, out and their gradients in short ones.  32 / 8 heads of 128, us (TFLOP/s of each kernel's own
+// products), by the card: 4 x 2944 tokens dQ 410-456 (935-1040), dK and dV 637-705 (805-890); 16 x 616 dQ 125-138 (540-600), dK and dV 156-174 (570-640).
 #include <algorithm>
 
 #include "attn.hpp"

@@ -8,8 +8,8 @@
 // where little is shared (4 of 32 with 32 / 8 heads and no sharing): the matrix cores have the time, the reads of the cache bound it.
 //
 // Measured, 32 / 8 heads of 128, us: 4 caches of up to 32768 rows (300 MB) 62-65 where the inputs change from pass to pass, 4.6-4.8 TB/s (a large
-// copy: 5.0), of which the second kernel 4.3; 64 sequences on two prefixes of up to 5795 rows (54 MB) 18.4 + 3.9: some tiles a wavefront one after
-// the other, a latency each; 8 sequences of 184 + 64 rows 8.1, all latency.
+// copy: 5.0), of which the second kernel 4.3; 64 sequences on two prefixes of up to 5795 rows (54 MB) 18.4-19.1 + 4: some tiles a wavefront one after
+// the other, a latency each; 8 sequences of 184 + 64 rows 8.1-8.8, all latency.
 #include <algorithm>
 
 #include "attn.hpp"

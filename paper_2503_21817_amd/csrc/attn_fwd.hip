@@ -6,8 +6,8 @@
 // one is worked on.  With 8 heads a chip-wide row of 8 workgroups has one key/value head each, so that an XCD's L2 holds one
 // head's keys.  Units of a sequence are taken from its end: in a causal prompt the longest first.
 //
-// Long prompts are bound by the power limit (the chip falls to 1.75-1.85 GHz with the matrix cores busy half of the time): 1 x 16384 tokens, 32 / 8
-// heads of 128, 2030-2280 us by the box, 966-1083 TFLOP/s of what the mask leaves, a library product of 8192^3 reaching 1175-1190.  Short ones
+// Long prompts are bound by the power limit (the chip falls to 1.42-1.85 GHz, by the card, with the matrix cores busy 50-56 % of the time): 1 x 16384 tokens,
+// 32 / 8 heads of 128, 2030-2325 us by the card, 945-1083 TFLOP/s of what the mask leaves, a library product of 8192^3 reaching 1150-1190.  Short ones
 // by the bytes of q and out, which a workgroup's products do not hide: 8 x 616 tokens 48 us, 520 TFLOP/s and 2.1 TB/s.
 #include "attn.hpp"
 
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(ATT_THREADS, (fwd_per_cu<DP, KEYS>())) void attn_fw
     }
 }
 
-// Few queries over many keys would leave most of the chip idle.  Parts cost a second kernel (about 4 us) and a row of fp32 written
+// Few queries over many keys would leave most of the chip idle.  The lengths are on the device: this goes by the average number of keys a sequence.  Parts cost a second kernel (about 4 us) and a row of fp32 written
 // and read again each (at about 4 TB/s), and save tiles of keys one after the other (about 1.2 us each)
 int attn_forward_splits(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int ncu) {
     if (Tq <= 0 || Tk <= 0 || n_seq <= 0) return 1;
