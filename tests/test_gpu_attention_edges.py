@@ -90,6 +90,18 @@ def test_tensors_of_one_token(nq, nk, Hq, Hkv, D, causal):
     check(*t, step(*t, nq, nk, causal, 0.2), nq, nk, causal, 0.2)
 
 
+@pytest.mark.parametrize("nq,nk", [((45, 20), (45, 20)), ((3, 40), (2500, 33)), ((70,), (31,))], ids=str)
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+def test_one_row_for_every_token_and_head(nq, nk, causal):
+    """Token and head strides of 0 in the queries and in the outputs' gradient, more keys or fewer than queries."""
+    Hq, Hkv, D = 6, 2, 80
+    print(f"one row {nq} over {nk} causal={causal}", flush=True)
+    rng = np.random.default_rng(sum(nk))
+    q, g = (normal(rng, 1, 1, D).expand(sum(nq), Hq, D) for _ in range(2))
+    k, v = (normal(rng, sum(nk), Hkv, D) for _ in range(2))
+    check(q, k, v, g, step(q, k, v, g, nq, nk, causal, 0.2), nq, nk, causal, 0.2)
+
+
 def test_repeated_queries_of_large_scores():
     """Rows past the end that repeat a query have scores of some hundred and no log-sum-exp of their own."""
     lens, H, D = (41,), 2, 64
