@@ -69,7 +69,9 @@ typedef enum skipffn_status {
                                              enqueued, when it is not.  The ONE case in which a call waits for the
                                              stream (it reads the verdict back), so not for use under graph capture.
                                              Without the flag idx is trusted: a wrong entry is an out-of-bounds write. */
-#define SKIPFFN_FLAG_ALL            0x1Fu
+#define SKIPFFN_FLAG_ALL            0x1Fu  /* what forward / backward take */
+#define SKIPFFN_FLAG_QK_NORM         0x20u /* qk_rope: an RMS norm of every head of q and k before the rotation */
+#define SKIPFFN_FLAG_ROPE_PAIRS      0x40u /* qk_rope: columns 2 j and 2 j + 1 are rotated together, not j and j + rot / 2 */
 
 /* ---- step 1: mask -> ascending retained indices -------------------------
  * Section 4.1 decides which visual tokens are retained; the block consumes
@@ -368,6 +370,45 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
                         const skipffn_heads* suffix_k, const skipffn_heads* suffix_v, int64_t suffix_k_seq, int64_t suffix_v_seq,
                         const int32_t* suffix_len, const skipffn_heads* out, float scale,
                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- norm and rotation of queries and keys (between the projection and the attention) ------
+ * For every token t and every head x of q and k, with n = x, or with SKIPFFN_FLAG_QK_NORM
+ *     n = x * rsqrt(mean(x^2) + eps) * gain          (mean over the head's D columns; gain_q, gain_k bf16 [D] or NULL = ones),
+ * the first `rot` columns are rotated in pairs by the angle A_j = pos[axis_j][t] * inv_freq[j], j < rot / 2,
+ *     y_a = n_a cos A_j - n_b sin A_j,   y_b = n_a sin A_j + n_b cos A_j
+ * with (a, b) = (j, j + rot / 2), or (2 j, 2 j + 1) with SKIPFFN_FLAG_ROPE_PAIRS; columns from rot on leave as n.  One axis of positions
+ * is the place in the text; images have several (time, height, width), each with frequencies of its own.  The angle is the exact
+ * product of the two numbers (taken in 64 bits), all else is fp32, rounded once to bf16.
+ *   q [T, Hq, D], k, v [T, Hkv, D]      as skipffn_heads, e.g. column ranges of the projections' output; v and v_out: both or none
+ *   pos       i32 [n_axes, T] device, any sign; inv_freq f32 [rot / 2] device (neither is read where rot == 0)
+ *   axis      u8 [rot / 2] HOST, every one below n_axes, or NULL: axis 0 for all
+ *   q_out [T, Hq, D]; k_out, v_out OUT: [T, Hkv, D], or with row != NULL the rows of a cache [rows_out, Hkv, D]:
+ *   row       i32 [T] device: token t's key and value go to row row[t] of k_out and v_out, and nowhere if that is outside
+ *             [0, rows_out) (a padded batch); rows that no token has are left as they were.  Two tokens with the same row: each 16 bytes
+ *             of it come from one of them.  NULL: row t (rows_out is not read)
+ * An output may be its own input (same memory and strides, row == NULL); training with a norm needs the inputs again, so not then.
+ * Otherwise it shares no element with an input or another output: what they span does not meet, or they are column ranges of
+ * rows of one stride.  v is copied bit for bit.
+ * D % 8 == 0, 8 <= D <= 128, rot % 8 == 0, 0 <= rot <= D, n_axes <= 4, T < 2^30.  eps >= 0, finite. */
+int skipffn_qk_rope_forward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, int64_t n_axes, const skipffn_heads* q,
+                            const skipffn_heads* k, const skipffn_heads* v, const int32_t* pos, const float* inv_freq, const uint8_t* axis,
+                            const void* gain_q, const void* gain_k, float eps, const int32_t* row, int64_t rows_out,
+                            const skipffn_heads* q_out, const skipffn_heads* k_out, const skipffn_heads* v_out, uint32_t flags, void* stream);
+
+/* Gradients of the above (without `row`; the values' gradient passes by) for L with dL/dq_out = grad_q_out, dL/dk_out = grad_k_out: with
+ * g the gradient rotated back and r = rsqrt(mean(x^2) + eps),
+ *     d_gain = sum over tokens and heads of g x r,   grad_x = r (g gain - x r^2 mean(g gain x)),   or grad_x = g without the norm.
+ *   q, k             what the forward call read; NULL (not read) without SKIPFFN_FLAG_QK_NORM
+ *   grad_q, grad_k   OUT, as q and k; may be grad_q_out, grad_k_out themselves, else as the outputs above
+ *   d_gain_q, d_gain_k  NULL, or f32 [D] OUT (with the norm; also where the gain is NULL), overwritten, or += with
+ *                    SKIPFFN_FLAG_DW_ACCUMULATE.  Summed in a fixed order that depends on the sizes of the call.
+ *   workspace        for gain gradients alone: at least skipffn_qk_rope_backward_workspace_bytes(...) */
+size_t skipffn_qk_rope_backward_workspace_bytes(int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
+int skipffn_qk_rope_backward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, int64_t n_axes, const skipffn_heads* q,
+                             const skipffn_heads* k, const skipffn_heads* grad_q_out, const skipffn_heads* grad_k_out, const int32_t* pos,
+                             const float* inv_freq, const uint8_t* axis, const void* gain_q, const void* gain_k, float eps,
+                             const skipffn_heads* grad_q, const skipffn_heads* grad_k, float* d_gain_q, float* d_gain_k,
+                             void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
 
 /* ---- layout of `saved`, for tests that compare stage by stage -------------
  * Byte offsets of the sections inside a saved buffer for (R_max, C, I):

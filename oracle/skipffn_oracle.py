@@ -674,3 +674,69 @@ def attn_decode_real(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suf
         out[i] = o[0]
         seen.append((k, v, P[:, 0]))
     return out, seen
+
+
+# ---- norm and rotation of queries and keys ----------------------------------------------------------------
+def rope_pairs(rot, neighbours):
+    """Columns (a, b) of every rotated pair."""
+    j = np.arange(rot // 2)
+    return (2 * j, 2 * j + 1) if neighbours else (j, j + rot // 2)
+
+
+def rope_rotate(x, angle, neighbours):
+    """x [T, H, D], angle [T, rot / 2]: the first rot columns rotated in pairs."""
+    y = np.array(x, dtype=np.float64)
+    a, b = rope_pairs(2 * angle.shape[1], neighbours)
+    cos, sin = np.cos(angle)[:, None], np.sin(angle)[:, None]
+    y[..., a], y[..., b] = x[..., a] * cos - x[..., b] * sin, x[..., a] * sin + x[..., b] * cos
+    return y
+
+
+def rope_angles(pos, inv_freq, axis=None):
+    """pos [axes, T], inv_freq [rot / 2] -> [T, rot / 2]"""
+    axis = np.zeros(len(inv_freq), dtype=int) if axis is None else np.asarray(axis, dtype=int)
+    return np.asarray(pos, dtype=np.float64)[axis].T * np.asarray(inv_freq, dtype=np.float64)
+
+
+def rope_forward_real(x, angle, neighbours, norm, gain, eps):
+    """One of q, k: x [T, H, D] -> y, and n (what is rotated)."""
+    n = np.array(x, dtype=np.float64)
+    if norm:
+        n = n / np.sqrt((n * n).mean(-1, keepdims=True) + eps)
+        n = n if gain is None else n * gain
+    return rope_rotate(n, angle, neighbours), n
+
+
+def rope_backward_real(x, angle, neighbours, norm, gain, eps, grad):
+    """-> grad_x, d_gain (None without the norm)"""
+    g = rope_rotate(grad, -angle, neighbours)
+    if not norm:
+        return g, None
+    r = 1.0 / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    d_gain = (g * x * r).sum((0, 1))
+    g = g if gain is None else g * gain
+    return r * (g - x * r * r * (g * x).mean(-1, keepdims=True)), d_gain
+
+
+# ---- weights that the keys receive, and eviction by them ------------------------------------------------------
+def key_weights_real(q, k, causal, scale, last=None):
+    """One sequence: what each key receives from the last `last` queries (None: all) -> [Hkv, nk]."""
+    Hq, Hkv = q.shape[1], k.shape[1]
+    w = np.zeros((Hkv, k.shape[0]))
+    first = 0 if last is None else max(0, q.shape[0] - last)
+    for h in range(Hq):
+        kh = h // (Hq // Hkv)
+        w[kh] += attn_weights(scale * (q[:, h] @ k[:, kh].T), causal)[first:].sum(0)
+    return w
+
+
+def evict_choice(w, n_keep, first, recent):
+    """Rows of one sequence and head that stay, ascending: the `first` first and `recent` last ones before all others, then by weight
+    (larger first, NaN after every number, equal ones by index)."""
+    n = len(w)
+    t = np.arange(n)
+    w = np.asarray(w, dtype=np.float64)
+    rank = np.where(np.isnan(w), np.inf, -w)
+    level = np.where((t < first) | (t >= n - recent), 0, np.where(np.isnan(w), 2, 1))
+    order = np.lexsort((t, np.where(level == 1, rank, 0.0), level))
+    return np.sort(order[:max(0, min(n_keep, n))])

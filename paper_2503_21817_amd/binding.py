@@ -23,6 +23,8 @@ FLAG_DW_ACCUMULATE = 0x2
 FLAG_NO_RESIDUAL = 0x4
 FLAG_BALANCED_SPLIT = 0x8
 FLAG_VALIDATE_IDX = 0x10
+FLAG_QK_NORM = 0x20
+FLAG_ROPE_PAIRS = 0x40
 
 OK, EINVAL, ESHAPE, EWORKSPACE, EHIP, EUNSUPPORTED, EIDX = range(7)
 
@@ -72,6 +74,11 @@ _SIGNATURES = {
     "skipffn_attn_decode_workspace_bytes": (c_size_t, [c_int64] * 7),
     "skipffn_attn_decode": (c_int, [c_int64] * 7 + [c_void_p] * 3 + [c_void_p] * 2 + [c_void_p] * 2 + [c_int64] * 2 +
                             [c_void_p, c_void_p, c_float, c_void_p, c_size_t, c_void_p]),
+    "skipffn_qk_rope_forward": (c_int, [c_int64] * 6 + [c_void_p] * 3 + [c_void_p] * 3 + [c_void_p] * 2 + [c_float, c_void_p, c_int64] +
+                                [c_void_p] * 3 + [c_uint32, c_void_p]),
+    "skipffn_qk_rope_backward_workspace_bytes": (c_size_t, [c_int64] * 4),
+    "skipffn_qk_rope_backward": (c_int, [c_int64] * 6 + [c_void_p] * 4 + [c_void_p] * 3 + [c_void_p] * 2 + [c_float] + [c_void_p] * 4 +
+                                 [c_void_p, c_size_t, c_uint32, c_void_p]),
     "skipffn_probe_mfma": (c_int, [c_int64, c_int64, c_int, c_void_p, c_void_p, c_void_p]),
     "skipffn_saved_layout": (c_int, [c_int64, c_int64, c_int64, POINTER(c_size_t)]),
     "skipffn_status_string": (c_char_p, [c_int]),
@@ -318,6 +325,8 @@ def _heads(where, device, *tensors):
     v = []
     for t, shape in tensors:
         *_, st, sh, sc = t.stride()
+        if t.numel() == 0:                               # its strides say nothing
+            st, sh, sc = shape[-2] * shape[-1], shape[-1], 1
         if t.shape != shape or t.dtype is not torch.bfloat16 or t.get_device() != device or (sc != 1 and shape[-1] > 1):
             raise ValueError(f"{where}: a bfloat16 tensor {tuple(shape)} on the device of the call, with contiguous columns, is wanted")
         # a stride that nothing is apart by is whatever the tensor was cut from
@@ -431,6 +440,84 @@ def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, 
                                      D ** -0.5 if scale is None else scale, ws, ws_bytes, _stream(dev)), where)
 
 
+def _floats(t, n, where, device):
+    """Address of a contiguous float32 tensor of n values on the device, or None."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.numel() != n or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{where}: a contiguous float32 tensor of {n} values on the device of the call is wanted")
+    return t.data_ptr()
+
+
+def _gain(t, D, where, device):
+    if t is None:
+        return None
+    if t.dtype is not torch.bfloat16 or t.numel() != D or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{where}: a contiguous bfloat16 tensor of {D} values on the device of the call is wanted")
+    return t.data_ptr()
+
+
+def _rope(where, dev, T, pos, inv_freq, axis):
+    """rot, n_axes, and the addresses of pos, inv_freq and axis"""
+    rot, n_axes = 2 * inv_freq.numel(), pos.shape[0] if pos.dim() == 2 else 1
+    at = _ints(pos, n_axes * T, where, dev)
+    if axis is not None:
+        axis = bytes(axis)
+        if len(axis) != rot // 2:
+            raise ValueError(f"{where}: an axis for each of {rot // 2} frequencies is wanted")
+    return rot, n_axes, at, _floats(inv_freq, rot // 2, where, dev), axis
+
+
+def skipffn_qk_rope_forward(q, k, q_out, k_out, pos, inv_freq, *, axis=None, v=None, v_out=None, row=None, gain_q=None, gain_k=None,
+                            eps=1e-6, flags=0):
+    """q, q_out bf16 [T, Hq, D]; k, v bf16 [T, Hkv, D]; k_out, v_out the same, or with row (i32 [T]) a cache [rows, Hkv, D] (any token and
+    head strides); pos i32 [T] or [axes, T]; inv_freq f32 [rot / 2]; axis: bytes or a host sequence of rot / 2 axes.
+    flags: FLAG_QK_NORM, FLAG_ROPE_PAIRS."""
+    where = "skipffn_qk_rope_forward"
+    dev = _device(q, where)
+    (T, Hq, D), Hkv = q.shape, k.shape[1]
+    if (v is None) != (v_out is None):
+        raise ValueError(f"{where}: v and v_out come together")
+    rows = T if row is None else k_out.shape[0]
+    kv, out = (T, Hkv, D), (rows, Hkv, D)
+    given = [(q, q.shape), (k, kv), (q_out, q.shape), (k_out, out)]
+    if v is not None:
+        given += [(v, kv), (v_out, out)]
+    hold, at = _heads(where, dev, *given)
+    rot, n_axes, hp, hf, ax = _rope(where, dev, T, pos, inv_freq, axis)
+    _check(lib().skipffn_qk_rope_forward(T, Hq, Hkv, D, rot, n_axes, at[0], at[1], at[4] if v is not None else None, hp, hf, ax,
+                                         _gain(gain_q, D, where, dev), _gain(gain_k, D, where, dev), eps,
+                                         None if row is None else _ints(row, T, where, dev), rows, at[2], at[3],
+                                         at[5] if v is not None else None, flags, _stream(dev)), where)
+
+
+def skipffn_qk_rope_backward_workspace_bytes(T, Hq, Hkv, D) -> int:
+    return lib().skipffn_qk_rope_backward_workspace_bytes(T, Hq, Hkv, D)
+
+
+def skipffn_qk_rope_backward(grad_q_out, grad_k_out, grad_q, grad_k, pos, inv_freq, *, axis=None, q=None, k=None, gain_q=None, gain_k=None,
+                             eps=1e-6, d_gain_q=None, d_gain_k=None, workspace=None, flags=0):
+    """The forward call's pos, inv_freq, axis, gains, eps and flags, with FLAG_QK_NORM its q and k too; grad_* as q and k;
+    d_gain_q, d_gain_k f32 [D] (FLAG_DW_ACCUMULATE: added to), which take a workspace."""
+    where = "skipffn_qk_rope_backward"
+    dev = _device(grad_q_out, where)
+    (T, Hq, D), Hkv = grad_q_out.shape, grad_k_out.shape[1]
+    qs, kv = grad_q_out.shape, (T, Hkv, D)
+    given = [(grad_q_out, qs), (grad_k_out, kv), (grad_q, qs), (grad_k, kv)]
+    norm = (flags & FLAG_QK_NORM) != 0
+    if norm:
+        if q is None or k is None:
+            raise ValueError(f"{where}: the norm's gradient takes the forward call's q and k")
+        given += [(q, qs), (k, kv)]
+    hold, at = _heads(where, dev, *given)
+    rot, n_axes, hp, hf, ax = _rope(where, dev, T, pos, inv_freq, axis)
+    ws, ws_bytes = _buffer(workspace, 0, where, dev)
+    _check(lib().skipffn_qk_rope_backward(T, Hq, Hkv, D, rot, n_axes, at[4] if norm else None, at[5] if norm else None, at[0], at[1], hp, hf,
+                                          ax, _gain(gain_q, D, where, dev), _gain(gain_k, D, where, dev), eps, at[2], at[3],
+                                          _floats(d_gain_q, D, where, dev), _floats(d_gain_k, D, where, dev), ws, ws_bytes, flags,
+                                          _stream(dev)), where)
+
+
 def skipffn_probe_mfma(blocks, iters, random_operands, out, clocks):
     """out f32 [blocks * 256]; clocks i64 [2 * blocks] (shader cycles, 100 MHz ticks per workgroup)."""
     _check(lib().skipffn_probe_mfma(blocks, iters, int(bool(random_operands)), _ptr(out), _ptr(clocks),
@@ -447,7 +534,7 @@ def skipffn_profile_begin():
 
 def skipffn_profile_end():
     """-> {kernel class: (total ms, launches)} for classes that ran."""
-    cap = 32
+    cap = 40
     names = (c_char_p * cap)()
     ms = (c_double * cap)()
     cnt = (c_int64 * cap)()

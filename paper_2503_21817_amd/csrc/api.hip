@@ -105,7 +105,7 @@ const char* kernel_class_name(int kc) {
         "passthrough_copy", "gather_rows", "gemm_dh_swiglu_bwd+dw_down", "gemm_dw_gate_up",
         "gemm_dxn", "rmsnorm_bwd_scatter", "fill_zero", "kv_compact", "summary_fwd", "summary_bwd", "select_retained", "token_merge",
         "gemm_dxn+dw_gate_up",
-        "attn_fwd", "attn_bwd", "attn_decode"};
+        "attn_fwd", "attn_bwd", "attn_decode", "qk_rope_fwd", "qk_rope_bwd", "attn_key_weights", "kv_evict"};
     return (kc >= 0 && kc < KC_COUNT) ? names[kc] : "?";
 }
 
@@ -1026,6 +1026,139 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
     profile_mark_begin(KC_ATTN_DECODE, s);
     hipError_t e = launch_attn_decode(a, s);
     profile_mark_end(KC_ATTN_DECODE, s);
+    return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
+}
+
+// ---- norm and rotation of queries and keys ---------------------------------------------------------------
+namespace {
+// Whether two tensors may share an element.  Column ranges of one tensor (heads inside a token's row, the same token stride) that lie apart do not,
+// though what they span meets.
+bool heads_share(const skipffn_heads* a, int64_t Ta, int64_t Ha, const skipffn_heads* b, int64_t Tb, int64_t Hb, int64_t D) {
+    if (!heads_meet(a, Ta, Ha, b, Tb, Hb, D)) return false;
+    const int64_t wide = a->token_stride, wa = (Ha - 1) * a->head_stride + D, wb = (Hb - 1) * b->head_stride + D;
+    if (b->token_stride != wide || wa > wide || wb > wide) return true;
+    const int64_t x = (int64_t)(reinterpret_cast<uintptr_t>(b->data) - reinterpret_cast<uintptr_t>(a->data)) / 2;      // 16-byte aligned both
+    const int64_t d = ((x % wide) + wide) % wide;
+    return d < wa || wide - d < wb;
+}
+bool same_heads(const skipffn_heads* a, const skipffn_heads* b) {
+    return a->data == b->data && a->token_stride == b->token_stride && a->head_stride == b->head_stride;
+}
+int check_rope(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, int64_t n_axes, const int32_t* pos, const float* inv_freq,
+               const uint8_t* axis, const void* gain_q, const void* gain_k, float eps, uint32_t flags) {
+    if (flags & ~(SKIPFFN_FLAG_QK_NORM | SKIPFFN_FLAG_ROPE_PAIRS | SKIPFFN_FLAG_DW_ACCUMULATE)) return SKIPFFN_EUNSUPPORTED;
+    if (T < 0 || Hq <= 0 || Hkv <= 0 || D <= 0 || rot < 0 || rot > D || n_axes <= 0) return SKIPFFN_EINVAL;
+    if ((D & 7) || D > ATTN_MAX_D || (rot & 7) || n_axes > ROPE_MAX_AXES || Hq > 65535 || Hkv > 65535 || T >= (1 << 30)) return SKIPFFN_ESHAPE;
+    if (!(eps >= 0.0f) || !std::isfinite(eps)) return SKIPFFN_EINVAL;
+    if ((gain_q != nullptr || gain_k != nullptr) && !(flags & SKIPFFN_FLAG_QK_NORM)) return SKIPFFN_EINVAL;
+    if (!aligned16(gain_q) || !aligned16(gain_k)) return SKIPFFN_EINVAL;
+    if (axis != nullptr)
+        for (int64_t j = 0; j < rot / 2; ++j)
+            if (axis[j] >= n_axes) return SKIPFFN_EINVAL;
+    if (T > 0 && rot > 0 && (bad_seg(pos) || inv_freq == nullptr || (reinterpret_cast<uintptr_t>(inv_freq) & 3u))) return SKIPFFN_EINVAL;
+    return SKIPFFN_OK;
+}
+RopeIn rope_in(const skipffn_heads* t) { return RopeIn{in(t), (int)t->token_stride, t->head_stride}; }
+RopeOut rope_out(const skipffn_heads* t) { return RopeOut{to(t), (int)t->token_stride, t->head_stride}; }
+RopeArgs rope_args(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, int64_t n_axes, const int32_t* pos, const float* inv_freq,
+                   const uint8_t* axis, const void* gain_q, const void* gain_k, float eps, uint32_t flags) {
+    RopeArgs a{};
+    a.T = (int)T; a.Hq = (int)Hq; a.Hkv = (int)Hkv; a.D = (int)D; a.rot = (int)rot;
+    a.n_axes = rot == 0 ? 0 : axis == nullptr ? 1 : (int)n_axes;
+    a.norm = (flags & SKIPFFN_FLAG_QK_NORM) != 0;
+    a.pairs = (flags & SKIPFFN_FLAG_ROPE_PAIRS) != 0;
+    a.eps = eps; a.pos = pos; a.inv_freq = inv_freq;
+    for (int64_t j = 0; axis != nullptr && j < rot / 2; ++j) a.axis[j] = axis[j];
+    a.gain_q = static_cast<const bf16_t*>(gain_q); a.gain_k = static_cast<const bf16_t*>(gain_k);
+    return a;
+}
+}  // namespace
+
+int skipffn_qk_rope_forward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, int64_t n_axes, const skipffn_heads* q,
+                            const skipffn_heads* k, const skipffn_heads* v, const int32_t* pos, const float* inv_freq, const uint8_t* axis,
+                            const void* gain_q, const void* gain_k, float eps, const int32_t* row, int64_t rows_out,
+                            const skipffn_heads* q_out, const skipffn_heads* k_out, const skipffn_heads* v_out, uint32_t flags, void* stream) {
+    int st = check_rope(T, Hq, Hkv, D, rot, n_axes, pos, inv_freq, axis, gain_q, gain_k, eps, flags);
+    if (st != SKIPFFN_OK) return st;
+    if (flags & SKIPFFN_FLAG_DW_ACCUMULATE) return SKIPFFN_EUNSUPPORTED;
+    if ((v == nullptr) != (v_out == nullptr) || rows_out < 0 || (row != nullptr && bad_seg(row))) return SKIPFFN_EINVAL;
+    if (rows_out >= ((int64_t)1 << 31)) return SKIPFFN_ESHAPE;
+    const int64_t To = row != nullptr ? rows_out : T;
+    if ((st = check_heads(q, T, Hq, D, false)) || (st = check_heads(k, T, Hkv, D, false)) || (st = check_heads(q_out, T, Hq, D, true)) ||
+        (st = check_heads(k_out, To, Hkv, D, true)))
+        return st;
+    if (v != nullptr && ((st = check_heads(v, T, Hkv, D, false)) || (st = check_heads(v_out, To, Hkv, D, true)))) return st;
+    if (T == 0) return SKIPFFN_OK;
+    const skipffn_heads* ins[3] = {q, k, v};
+    const skipffn_heads* outs[3] = {q_out, k_out, v_out};
+    for (int o = 0; o < 3; ++o) {
+        if (outs[o] == nullptr) continue;
+        const int64_t Ho = o == 0 ? Hq : Hkv, rows = o == 0 ? T : To;
+        for (int i = 0; i < 3; ++i) {
+            if (ins[i] == nullptr || (i == o && same_heads(ins[i], outs[o]) && (o == 0 || row == nullptr))) continue;     // in place
+            if (heads_share(outs[o], rows, Ho, ins[i], T, i == 0 ? Hq : Hkv, D)) return SKIPFFN_EINVAL;
+        }
+        for (int i = 0; i < o; ++i)
+            if (outs[i] != nullptr && heads_share(outs[o], rows, Ho, outs[i], i == 0 ? T : To, i == 0 ? Hq : Hkv, D)) return SKIPFFN_EINVAL;
+    }
+    RopeArgs a = rope_args(T, Hq, Hkv, D, rot, n_axes, pos, inv_freq, axis, gain_q, gain_k, eps, flags);
+    a.q = rope_in(q); a.k = rope_in(k);
+    a.q_out = rope_out(q_out); a.k_out = rope_out(k_out);
+    if (v != nullptr) {
+        a.v = rope_in(v);
+        a.v_out = rope_out(v_out);
+    }
+    a.row = row; a.rows_out = To;
+    if (rope_forward_workgroups(a) >= ((int64_t)1 << 24)) return SKIPFFN_ESHAPE;             // a launch has fewer than 2^32 threads
+    hipStream_t s = (hipStream_t)stream;
+    profile_mark_begin(KC_ROPE_FWD, s);
+    hipError_t e = launch_rope_forward(a, s);
+    profile_mark_end(KC_ROPE_FWD, s);
+    return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
+}
+
+size_t skipffn_qk_rope_backward_workspace_bytes(int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
+    if (T < 0 || Hq <= 0 || Hkv <= 0 || D <= 0 || D > ATTN_MAX_D) return 0;
+    return align_up((size_t)(2 * rope_backward_workgroups(T, Hq, Hkv, num_cus()) * D * 4));
+}
+
+int skipffn_qk_rope_backward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, int64_t n_axes, const skipffn_heads* q,
+                             const skipffn_heads* k, const skipffn_heads* grad_q_out, const skipffn_heads* grad_k_out, const int32_t* pos,
+                             const float* inv_freq, const uint8_t* axis, const void* gain_q, const void* gain_k, float eps,
+                             const skipffn_heads* grad_q, const skipffn_heads* grad_k, float* d_gain_q, float* d_gain_k,
+                             void* workspace, size_t workspace_bytes, uint32_t flags, void* stream) {
+    int st = check_rope(T, Hq, Hkv, D, rot, n_axes, pos, inv_freq, axis, gain_q, gain_k, eps, flags);
+    if (st != SKIPFFN_OK) return st;
+    const bool norm = (flags & SKIPFFN_FLAG_QK_NORM) != 0, gains = d_gain_q != nullptr || d_gain_k != nullptr;
+    if ((gains && !norm) || (reinterpret_cast<uintptr_t>(d_gain_q) & 3u) || (reinterpret_cast<uintptr_t>(d_gain_k) & 3u) ||
+        (gains && d_gain_q == d_gain_k))
+        return SKIPFFN_EINVAL;
+    if (norm && ((st = check_heads(q, T, Hq, D, false)) || (st = check_heads(k, T, Hkv, D, false)))) return st;
+    if ((st = check_heads(grad_q_out, T, Hq, D, false)) || (st = check_heads(grad_k_out, T, Hkv, D, false)) ||
+        (st = check_heads(grad_q, T, Hq, D, true)) || (st = check_heads(grad_k, T, Hkv, D, true)))
+        return st;
+    const skipffn_heads* ins[4] = {grad_q_out, grad_k_out, norm ? q : nullptr, norm ? k : nullptr};
+    const skipffn_heads* outs[2] = {grad_q, grad_k};
+    for (int o = 0; o < 2 && T > 0; ++o)
+        for (int i = 0; i < 4; ++i) {
+            if (ins[i] == nullptr || (i == o && same_heads(ins[i], outs[o]))) continue;      // in place
+            if (heads_share(outs[o], T, o == 0 ? Hq : Hkv, ins[i], T, (i & 1) == 0 ? Hq : Hkv, D)) return SKIPFFN_EINVAL;
+        }
+    if (T > 0 && heads_share(grad_q, T, Hq, grad_k, T, Hkv, D)) return SKIPFFN_EINVAL;
+    if (gains && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < skipffn_qk_rope_backward_workspace_bytes(T, Hq, Hkv, D)))
+        return SKIPFFN_EWORKSPACE;
+    if (T == 0 && !gains) return SKIPFFN_OK;
+    RopeArgs a = rope_args(T, Hq, Hkv, D, rot, n_axes, pos, inv_freq, axis, gain_q, gain_k, eps, flags);
+    if (norm) {
+        a.q = rope_in(q);
+        a.k = rope_in(k);
+    }
+    a.gq = rope_in(grad_q_out); a.gk = rope_in(grad_k_out);
+    a.dq = rope_out(grad_q); a.dk = rope_out(grad_k);
+    hipStream_t s = (hipStream_t)stream;
+    profile_mark_begin(KC_ROPE_BWD, s);
+    hipError_t e = launch_rope_backward(a, static_cast<float*>(workspace), d_gain_q, d_gain_k, (flags & SKIPFFN_FLAG_DW_ACCUMULATE) != 0, num_cus(), s);
+    profile_mark_end(KC_ROPE_BWD, s);
     return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
 }
 

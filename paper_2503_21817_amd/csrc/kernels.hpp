@@ -33,6 +33,10 @@ enum KernelClass : int {
     KC_ATTN_FWD,
     KC_ATTN_BWD,
     KC_ATTN_DECODE,
+    KC_ROPE_FWD,
+    KC_ROPE_BWD,
+    KC_KEY_WEIGHTS,
+    KC_EVICT,
     KC_COUNT
 };
 const char* kernel_class_name(int kc);
@@ -221,6 +225,29 @@ int attn_forward_splits(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64
 hipError_t launch_attn_forward(const AttnArgs& a, int ncu, hipStream_t s);
 int64_t attn_backward_workgroups(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv);   // of the larger of its launches
 hipError_t launch_attn_backward(const AttnArgs& a, const AttnGrads& g, hipStream_t s);
+
+// ---- norm and rotation of queries and keys (rope.hip) -------------------------------------------------------------
+// Element (t, h, d) of a tensor lies at p[t * tok + h * head + d]
+struct RopeIn { const bf16_t* p; int tok; int64_t head; };
+struct RopeOut { bf16_t* p; int tok; int64_t head; };
+constexpr int ROPE_MAX_AXES = 4;
+struct RopeArgs {
+    int T, Hq, Hkv, D, rot, n_axes, norm, pairs;   // n_axes: 0 where nothing is rotated
+    float eps;
+    RopeIn q, k, v;                               // v.p null: no values; backward: q and k with a norm only
+    RopeOut q_out, k_out, v_out;
+    const int32_t* pos;                           // [n_axes][T]
+    const float* inv_freq;                        // [rot / 2]
+    uint8_t axis[ATTN_MAX_D / 2];                 // of a frequency
+    const bf16_t *gain_q, *gain_k;                // [D] or null
+    const int32_t* row; int64_t rows_out;         // row of k_out and v_out of a token (outside [0, rows_out): none), or null: the token
+    RopeIn gq, gk; RopeOut dq, dk;                // backward
+};
+int64_t rope_forward_workgroups(const RopeArgs& a);
+hipError_t launch_rope_forward(const RopeArgs& a, hipStream_t s);
+// workgroups of the backward kernel at most, each with a row of D fp32 of part for q and for k
+int64_t rope_backward_workgroups(int64_t T, int64_t Hq, int64_t Hkv, int ncu);
+hipError_t launch_rope_backward(const RopeArgs& a, float* part, float* d_gain_q, float* d_gain_k, int accumulate, int ncu, hipStream_t s);
 
 // ---- GEMMs -----------------------------------------------------------------------
 hipError_t gemm_init();   // raises the dynamic-LDS limit of every instantiation (once per process)
