@@ -371,6 +371,25 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
                         const int32_t* suffix_len, const skipffn_heads* out, float scale,
                         void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---- what the keys receive (for evicting cache rows by it) ------------------------------
+ * For every key j and key/value head the attention weights that its queries give it,
+ *     w[h][j] = sum over the query heads of h and over the queries i that count of P_ij,   P as in skipffn_attn_forward,
+ * computed from the log-sum-exp that it saved (one product, no values).
+ *   q, k, seg_q, seg_k, causal, scale   what skipffn_attn_forward was given; any Tq, Tk, strides it takes
+ *   saved     what that call wrote: f32 [Hq, Tq], the base-2 logarithm of a row's sum of 2^(scale log2(e) q . k)
+ *             (+infinity: the row sees no key).  Not read where no query counts
+ *   last      queries that count: the last so many of every sequence; < 0: all
+ *   weights   f32 [Hkv, Tk] OUT, head h weights_head (>= Tk) elements after the one before it: overwritten, or += with
+ *             SKIPFFN_FLAG_DW_ACCUMULATE (the only flag).  Keys that no query sees get 0; keys of no sequence are left as they were
+ *   workspace at least skipffn_attn_key_weights_workspace_bytes(...) bytes (NULL where that is 0)
+ * A query whose scores are not finite where it sees (its log-sum-exp is NaN or minus infinity) makes NaN of the keys it
+ * sees, and of no others.  fp32 throughout.  Deterministic. */
+size_t skipffn_attn_key_weights_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int64_t last);
+int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, const skipffn_heads* q,
+                             const skipffn_heads* k, const int32_t* seg_q, const int32_t* seg_k, int causal, float scale, const void* saved,
+                             int64_t last, float* weights, int64_t weights_head, void* workspace, size_t workspace_bytes, uint32_t flags,
+                             void* stream);
+
 /* ---- norm and rotation of queries and keys (between the projection and the attention) ------
  * For every token t and every head x of q and k, with n = x, or with SKIPFFN_FLAG_QK_NORM
  *     n = x * rsqrt(mean(x^2) + eps) * gain          (mean over the head's D columns; gain_q, gain_k bf16 [D] or NULL = ones),

@@ -74,6 +74,9 @@ _SIGNATURES = {
     "skipffn_attn_decode_workspace_bytes": (c_size_t, [c_int64] * 7),
     "skipffn_attn_decode": (c_int, [c_int64] * 7 + [c_void_p] * 3 + [c_void_p] * 2 + [c_void_p] * 2 + [c_int64] * 2 +
                             [c_void_p, c_void_p, c_float, c_void_p, c_size_t, c_void_p]),
+    "skipffn_attn_key_weights_workspace_bytes": (c_size_t, [c_int64] * 7),
+    "skipffn_attn_key_weights": (c_int, [c_int64] * 6 + [c_void_p] * 4 + [c_int, c_float, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                                                        c_size_t, c_uint32, c_void_p]),
     "skipffn_qk_rope_forward": (c_int, [c_int64] * 6 + [c_void_p] * 3 + [c_void_p] * 3 + [c_void_p] * 2 + [c_float, c_void_p, c_int64] +
                                 [c_void_p] * 3 + [c_uint32, c_void_p]),
     "skipffn_qk_rope_backward_workspace_bytes": (c_size_t, [c_int64] * 4),
@@ -438,6 +441,35 @@ def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, 
     ws, ws_bytes = _buffer(workspace, 0, where, dev)
     _check(lib().skipffn_attn_decode(n_seq, n_groups, Hq, Hkv, D, Tp, cap, at[0], pk, pv, seg, off, sk, sv, seq_k, seq_v, lens, at[1],
                                      D ** -0.5 if scale is None else scale, ws, ws_bytes, _stream(dev)), where)
+
+
+def _weights(t, shape, where, device):
+    """(address, stride) of float32 weights [..., heads, rows] whose rows lie together, and of what is before them."""
+    if t.dtype is not torch.float32 or t.shape != shape or t.get_device() != device or (t.stride(-1) != 1 and t.numel() > 0 and shape[-1] > 1):
+        raise ValueError(f"{where}: a float32 tensor {tuple(shape)} on the device of the call, with contiguous rows, is wanted")
+    return (t.data_ptr(),) + tuple(st if t.numel() > 0 and n > 1 else 0 for st, n in zip(t.stride()[:-1], shape[:-1]))
+
+
+def skipffn_attn_key_weights_workspace_bytes(Tq, Tk, n_seq, Hq, Hkv, D, last=None) -> int:
+    return lib().skipffn_attn_key_weights_workspace_bytes(Tq, Tk, n_seq, Hq, Hkv, D, -1 if last is None else last)
+
+
+def skipffn_attn_key_weights(q, k, seg_q, seg_k, saved, weights, *, causal=True, scale=None, last=None, workspace=None, flags=0):
+    """q, k, seg_q, seg_k, causal, scale: the forward call's, saved: what it wrote; weights f32 [Hkv, Tk] (any head stride).
+    last: queries of a sequence that count, the last ones (None: all).  flags: FLAG_DW_ACCUMULATE."""
+    where = "skipffn_attn_key_weights"
+    dev = _device(q, where)
+    (Tq, Hq, D), (Tk, Hkv, _) = q.shape, k.shape
+    hold, (hq, hk) = _heads(where, dev, (q, q.shape), (k, (Tk, Hkv, D)))
+    n1 = seg_q.numel()
+    if last is not None and last < 0:
+        raise ValueError(f"{where}: a number of queries, or None for all, is wanted")
+    w, w_head = _weights(weights, (Hkv, Tk), where, dev)
+    ws, ws_bytes = _buffer(workspace, 0, where, dev)
+    _check(lib().skipffn_attn_key_weights(Tq, Tk, n1 - 1, Hq, Hkv, D, hq, hk, _ints(seg_q, n1, where, dev),
+                                          None if seg_k is None else _ints(seg_k, n1, where, dev), 1 if causal else 0,
+                                          D ** -0.5 if scale is None else scale, _buffer(saved, Tq * Hq * 4, where, dev)[0],
+                                          -1 if last is None else last, w, w_head, ws, ws_bytes, flags, _stream(dev)), where)
 
 
 def _floats(t, n, where, device):

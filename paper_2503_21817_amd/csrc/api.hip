@@ -1029,6 +1029,53 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
     return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
 }
 
+// ---- what the keys receive -----------------------------------------------------------------------------
+namespace {
+int check_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int64_t last, float scale, KeyWeightsPlan& plan) {
+    const int st = check_attn(Tq, Tk, n_seq, Hq, Hkv, D, scale);
+    if (st != SKIPFFN_OK) return st;
+    plan = key_weights_plan(Tq, Tk, n_seq, Hq, Hkv, last < 0 ? Tq : std::min(last, Tq), num_cus());
+    return plan.blocks * plan.parts >= ((int64_t)1 << 24) ? SKIPFFN_ESHAPE : SKIPFFN_OK;      // a launch has fewer than 2^32 threads
+}
+size_t key_weights_bytes(const KeyWeightsPlan& p, int64_t Tk, int64_t Hkv) { return p.parts > 1 ? align_up((size_t)p.parts * Hkv * Tk * 4) : 0; }
+}  // namespace
+
+size_t skipffn_attn_key_weights_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int64_t last) {
+    KeyWeightsPlan p;
+    return check_key_weights(Tq, Tk, n_seq, Hq, Hkv, D, last, 1.0f, p) == SKIPFFN_OK ? key_weights_bytes(p, Tk, Hkv) : 0;
+}
+
+int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, const skipffn_heads* q,
+                             const skipffn_heads* k, const int32_t* seg_q, const int32_t* seg_k, int causal, float scale, const void* saved,
+                             int64_t last, float* weights, int64_t weights_head, void* workspace, size_t workspace_bytes, uint32_t flags,
+                             void* stream) {
+    if (flags & ~SKIPFFN_FLAG_DW_ACCUMULATE) return SKIPFFN_EUNSUPPORTED;
+    KeyWeightsPlan plan;
+    int st = check_key_weights(Tq, Tk, n_seq, Hq, Hkv, D, last, scale, plan);
+    if (st != SKIPFFN_OK) return st;
+    if ((st = check_heads(q, Tq, Hq, D, false)) || (st = check_heads(k, Tk, Hkv, D, false))) return st;
+    if ((seg_k == nullptr && Tq != Tk) || weights_head < 0 || (Hkv > 1 && weights_head < Tk)) return SKIPFFN_EINVAL;
+    if (weights_head >= ((int64_t)1 << 44)) return SKIPFFN_ESHAPE;
+    if (n_seq == 0 || Tk == 0) return SKIPFFN_OK;
+    if (bad_seg(seg_q) || (seg_k != nullptr && bad_seg(seg_k)) || (Tq > 0 && last != 0 && bad_ptr(saved)) || weights == nullptr ||
+        (reinterpret_cast<uintptr_t>(weights) & 3u))
+        return SKIPFFN_EINVAL;
+    const size_t need = key_weights_bytes(plan, Tk, Hkv);
+    if (need > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < need)) return SKIPFFN_EWORKSPACE;
+    hipStream_t s = (hipStream_t)stream;
+    const skipffn_heads none{};
+    const AttnArgs a = attn_args(Tq, Tk, n_seq, Hq, Hkv, D, q, k, &none, &none, seg_q, seg_k, causal, scale,
+                                 const_cast<float*>(static_cast<const float*>(saved)));
+    KeyWeightsArgs w{};
+    w.last = last < 0 ? (int)Tq : (int)std::min(last, Tq);
+    w.accumulate = (flags & SKIPFFN_FLAG_DW_ACCUMULATE) != 0;
+    w.parts = plan.parts; w.w = weights; w.w_head = weights_head; w.part = static_cast<float*>(workspace);
+    profile_mark_begin(KC_KEY_WEIGHTS, s);
+    hipError_t e = launch_attn_key_weights(a, w, plan, s);
+    profile_mark_end(KC_KEY_WEIGHTS, s);
+    return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
+}
+
 // ---- norm and rotation of queries and keys ---------------------------------------------------------------
 namespace {
 // Whether two tensors may share an element.  Column ranges of one tensor (heads inside a token's row, the same token stride) that lie apart do not,

@@ -226,6 +226,18 @@ hipError_t launch_attn_forward(const AttnArgs& a, int ncu, hipStream_t s);
 int64_t attn_backward_workgroups(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv);   // of the larger of its launches
 hipError_t launch_attn_backward(const AttnArgs& a, const AttnGrads& g, hipStream_t s);
 
+// ---- what the keys receive (key_weights.hip) ------------------------------------------------------------------------
+struct KeyWeightsArgs {
+    int last, accumulate, parts;                  // queries of a sequence that count: the last ones
+    float* w; int64_t w_head;                     // weight of key j of the packed keys: w[kv head * w_head + j]
+    float* part;                                  // parts > 1: [parts][Hkv][Tk]
+};
+constexpr int KEY_WEIGHTS_MAX_PARTS = 32;
+// sets of 32 keys of a wavefront; workgroups of a part; parts that the queries are cut into
+struct KeyWeightsPlan { int sets; int64_t blocks; int parts; };
+KeyWeightsPlan key_weights_plan(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t last, int ncu);
+hipError_t launch_attn_key_weights(const AttnArgs& a, const KeyWeightsArgs& w, const KeyWeightsPlan& p, hipStream_t s);
+
 // ---- norm and rotation of queries and keys (rope.hip) -------------------------------------------------------------
 // Element (t, h, d) of a tensor lies at p[t * tok + h * head + d]
 struct RopeIn { const bf16_t* p; int tok; int64_t head; };
