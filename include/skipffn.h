@@ -371,6 +371,29 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
                         const int32_t* suffix_len, const skipffn_heads* out, float scale,
                         void* workspace, size_t workspace_bytes, void* stream);
 
+/* skipffn_attn_decode that also hands out what the rows of the cache receive (for evicting rows by it): with P the attention
+ * weights of a sequence's token,
+ *     prefix row t of a group:  w[h][t] = sum over the group's sequences and the query heads of h of P,
+ *     own row t of a sequence:  w[h][t] = sum over the query heads of h of P.
+ *   most_shared     most sequences that a group has (a bound that sizes the workspace).  Sequences of a group past the first most_shared
+ *                   of it add nothing to its prefix's weights.  >= 1 where there is a prefix
+ *   prefix_weights  f32 [Hkv, Tp] OUT, head h prefix_weights_head elements after the one before it; rows of no group left as they were.
+ *                   Not read or written where n_groups == 0 or Tp == 0
+ *   suffix_weights  f32 [n_seq, Hkv, suffix_capacity] OUT by strides of sequence and head (no element shared); rows past suffix_len are
+ *                   left as they were.  Not read or written where suffix_capacity == 0
+ * Both are overwritten, or += with SKIPFFN_FLAG_DW_ACCUMULATE (the only flag).  `out` has the bits that skipffn_attn_decode gives; all else as
+ * there.  A sequence whose row of `out` is NaN for its scores makes NaN of the weights of the rows it sees.  Deterministic.
+ * workspace: at least skipffn_attn_decode_weights_workspace_bytes(...): 4 Hq (most_shared Tp + n_seq suffix_capacity) and what decode takes. */
+size_t skipffn_attn_decode_weights_workspace_bytes(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp,
+                                                   int64_t suffix_capacity, int64_t most_shared);
+int skipffn_attn_decode_weights(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t suffix_capacity,
+                                const skipffn_heads* q, const skipffn_heads* prefix_k, const skipffn_heads* prefix_v,
+                                const int32_t* prefix_seg, const int32_t* group_off, const skipffn_heads* suffix_k,
+                                const skipffn_heads* suffix_v, int64_t suffix_k_seq, int64_t suffix_v_seq, const int32_t* suffix_len,
+                                const skipffn_heads* out, float scale, int64_t most_shared, float* prefix_weights,
+                                int64_t prefix_weights_head, float* suffix_weights, int64_t suffix_weights_seq,
+                                int64_t suffix_weights_head, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream);
+
 /* ---- what the keys receive (for evicting cache rows by it) ------------------------------
  * For every key j and key/value head the attention weights that its queries give it,
  *     w[h][j] = sum over the query heads of h and over the queries i that count of P_ij,   P as in skipffn_attn_forward,

@@ -74,6 +74,10 @@ _SIGNATURES = {
     "skipffn_attn_decode_workspace_bytes": (c_size_t, [c_int64] * 7),
     "skipffn_attn_decode": (c_int, [c_int64] * 7 + [c_void_p] * 3 + [c_void_p] * 2 + [c_void_p] * 2 + [c_int64] * 2 +
                             [c_void_p, c_void_p, c_float, c_void_p, c_size_t, c_void_p]),
+    "skipffn_attn_decode_weights_workspace_bytes": (c_size_t, [c_int64] * 8),
+    "skipffn_attn_decode_weights": (c_int, [c_int64] * 7 + [c_void_p] * 3 + [c_void_p] * 2 + [c_void_p] * 2 + [c_int64] * 2 +
+                                    [c_void_p, c_void_p, c_float, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_void_p, c_size_t,
+                                     c_uint32, c_void_p]),
     "skipffn_attn_key_weights_workspace_bytes": (c_size_t, [c_int64] * 7),
     "skipffn_attn_key_weights": (c_int, [c_int64] * 6 + [c_void_p] * 4 + [c_int, c_float, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
                                                                         c_size_t, c_uint32, c_void_p]),
@@ -406,12 +410,9 @@ def skipffn_attn_decode_workspace_bytes(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_
     return lib().skipffn_attn_decode_workspace_bytes(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity)
 
 
-def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, *, scale=None,
-                        workspace=None):
-    """q, out bf16 [n_seq, Hq, D]; prefix_k, prefix_v bf16 [Tp, Hkv, D] with prefix_seg, group_off i32 [n_groups + 1], or all
-    four None; suffix_k, suffix_v bf16 [n_seq, capacity, Hkv, D] with suffix_len i32 [n_seq], or all three None.
-    scale: None is 1 / sqrt(D)."""
-    where = "skipffn_attn_decode"
+def _decode(where, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, scale, workspace):
+    """The library's arguments up to the scale, the workspace's two and the stream; the sizes (Hkv, Tp, capacity), the device, and what has to live
+    until the call."""
     dev = _device(q, where)
     n_seq, Hq, D = q.shape
     if prefix_k is None and suffix_k is None:
@@ -439,8 +440,41 @@ def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, 
     pk, pv = at[2:4] if prefix_k is not None else (None, None)
     sk, sv = at[-2:] if suffix_k is not None and n_seq > 0 else (None, None)
     ws, ws_bytes = _buffer(workspace, 0, where, dev)
-    _check(lib().skipffn_attn_decode(n_seq, n_groups, Hq, Hkv, D, Tp, cap, at[0], pk, pv, seg, off, sk, sv, seq_k, seq_v, lens, at[1],
-                                     D ** -0.5 if scale is None else scale, ws, ws_bytes, _stream(dev)), where)
+    args = (n_seq, n_groups, Hq, Hkv, D, Tp, cap, at[0], pk, pv, seg, off, sk, sv, seq_k, seq_v, lens, at[1],
+            D ** -0.5 if scale is None else scale)
+    return args, (ws, ws_bytes), _stream(dev), (Hkv, Tp, cap), dev, hold
+
+
+def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, *, scale=None,
+                        workspace=None):
+    """q, out bf16 [n_seq, Hq, D]; prefix_k, prefix_v bf16 [Tp, Hkv, D] with prefix_seg, group_off i32 [n_groups + 1], or all
+    four None; suffix_k, suffix_v bf16 [n_seq, capacity, Hkv, D] with suffix_len i32 [n_seq], or all three None.
+    scale: None is 1 / sqrt(D)."""
+    where = "skipffn_attn_decode"
+    args, ws, stream, _, _, hold = _decode(where, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, scale,
+                                           workspace)
+    _check(lib().skipffn_attn_decode(*args, *ws, stream), where)
+
+
+def skipffn_attn_decode_weights_workspace_bytes(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, most_shared) -> int:
+    return lib().skipffn_attn_decode_weights_workspace_bytes(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, most_shared)
+
+
+def skipffn_attn_decode_weights(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, prefix_weights,
+                                suffix_weights, *, most_shared=1, scale=None, workspace=None, flags=0):
+    """skipffn_attn_decode, and what the rows receive: prefix_weights f32 [Hkv, Tp] and suffix_weights f32 [n_seq, Hkv, capacity] (None with
+    the rows they belong to).  most_shared: most sequences of a group.  flags: FLAG_DW_ACCUMULATE."""
+    where = "skipffn_attn_decode_weights"
+    args, ws, stream, (Hkv, Tp, cap), dev, hold = _decode(where, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len,
+                                                          out, scale, workspace)
+    if (prefix_k is None) != (prefix_weights is None) or (suffix_k is None) != (suffix_weights is None):
+        raise ValueError(f"{where}: a prefix, or own rows, come with their weights")
+    pw, sw = (None, 0), (None, 0, 0)
+    if prefix_weights is not None:
+        pw = _weights(prefix_weights, (Hkv, Tp), where, dev)
+    if suffix_weights is not None and q.shape[0] > 0:
+        sw = _weights(suffix_weights, (q.shape[0], Hkv, cap), where, dev)
+    _check(lib().skipffn_attn_decode_weights(*args, most_shared, *pw, *sw, *ws, flags, stream), where)
 
 
 def _weights(t, shape, where, device):

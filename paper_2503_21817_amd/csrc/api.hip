@@ -977,11 +977,42 @@ size_t skipffn_attn_decode_workspace_bytes(int64_t n_seq, int64_t n_groups, int6
     return parts_ws(n_seq * Hq, D, attn_decode_splits(n_seq, n_groups, Hq, Hkv, Tp, suffix_capacity, num_cus())).total;
 }
 
-int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t suffix_capacity,
-                        const skipffn_heads* q, const skipffn_heads* prefix_k, const skipffn_heads* prefix_v, const int32_t* prefix_seg,
+namespace {
+struct DecodeWeights { int64_t most_shared; float* prefix; int64_t prefix_head; float* own; int64_t own_seq, own_head; bool accumulate; };
+// the workspace of a call: parts' rows, then for weights the products and the log-sum-exps
+struct DecodeWs { PartsWs parts; size_t prefix, own, lse, total; };
+DecodeWs decode_ws(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t cap, bool weights, int64_t most_shared) {
+    DecodeWs W{};
+    W.parts = parts_ws(n_seq * Hq, D, attn_decode_splits(n_seq, n_groups, Hq, Hkv, Tp, cap, num_cus()));
+    W.total = W.parts.total;
+    if (!weights) return W;
+    W.prefix = W.total;
+    W.own = W.prefix + (n_groups > 0 ? align_up((size_t)(std::min(most_shared, n_seq) * Hq * Tp) * 4) : 0);
+    W.lse = W.own + align_up((size_t)(n_seq * Hq * cap) * 4);
+    W.total = W.lse + align_up((size_t)(n_seq * Hq) * 4);
+    return W;
+}
+
+int check_decode_weights(const DecodeWeights& w, int64_t n_seq, int64_t Hkv, int64_t Tp, int64_t cap) {
+    const int64_t most = (int64_t)1 << 44;
+    if (w.most_shared < 0 || w.prefix_head < 0 || w.own_seq < 0 || w.own_head < 0) return SKIPFFN_EINVAL;
+    if (w.prefix_head >= most || w.own_seq >= most || w.own_head >= most) return SKIPFFN_ESHAPE;
+    auto bad = [](const float* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; };
+    if (Tp > 0 && (w.most_shared == 0 || bad(w.prefix) || (Hkv > 1 && w.prefix_head < Tp))) return SKIPFFN_EINVAL;
+    if (cap > 0 && n_seq > 0) {
+        // rows are apart: heads inside a sequence's range, or sequences inside a head's
+        const bool heads_in = (Hkv == 1 || w.own_head >= cap) && (n_seq == 1 || w.own_seq >= (Hkv - 1) * w.own_head + cap);
+        const bool seqs_in = (n_seq == 1 || w.own_seq >= cap) && (Hkv == 1 || w.own_head >= (n_seq - 1) * w.own_seq + cap);
+        if (bad(w.own) || (!heads_in && !seqs_in)) return SKIPFFN_EINVAL;
+    }
+    return SKIPFFN_OK;
+}
+
+int decode_call(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t suffix_capacity,
+                const skipffn_heads* q, const skipffn_heads* prefix_k, const skipffn_heads* prefix_v, const int32_t* prefix_seg,
                         const int32_t* group_off, const skipffn_heads* suffix_k, const skipffn_heads* suffix_v, int64_t suffix_k_seq,
                         int64_t suffix_v_seq, const int32_t* suffix_len, const skipffn_heads* out, float scale,
-                        void* workspace, size_t workspace_bytes, void* stream) {
+                        void* workspace, size_t workspace_bytes, void* stream, const DecodeWeights* weights) {
     int st = check_decode(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, scale);
     if (st != SKIPFFN_OK) return st;
     if ((st = check_heads(q, n_seq, Hq, D, false)) || (st = check_heads(out, n_seq, Hq, D, true))) return st;
@@ -994,17 +1025,19 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
         if (suffix_k_seq < 0 || suffix_v_seq < 0 || bad_seg(suffix_len)) return SKIPFFN_EINVAL;
         if ((suffix_k_seq & 7) || (suffix_v_seq & 7) || suffix_k_seq >= ((int64_t)1 << 36) || suffix_v_seq >= ((int64_t)1 << 36)) return SKIPFFN_ESHAPE;
     }
-    if (n_seq == 0) return SKIPFFN_OK;
+    if (weights != nullptr && (st = check_decode_weights(*weights, n_seq, Hkv, Tg, cap)) != SKIPFFN_OK) return st;
+    if (n_seq == 0 && (weights == nullptr || weights->accumulate || Tg == 0)) return SKIPFFN_OK;
     const uintptr_t o0 = reinterpret_cast<uintptr_t>(out->data), o1 = o0 + (uintptr_t)heads_span(out, n_seq, Hq, D);
     auto meets = [&](const skipffn_heads* t, int64_t T, int64_t H, int64_t more) {
         const uintptr_t x = reinterpret_cast<uintptr_t>(t->data);
         return o0 < x + (uintptr_t)(more * 2 + heads_span(t, T, H, D)) && x < o1;
     };
-    if (meets(q, n_seq, Hq, 0) || (Tg > 0 && (meets(prefix_k, Tg, Hkv, 0) || meets(prefix_v, Tg, Hkv, 0))) ||
-        (cap > 0 && (meets(suffix_k, cap, Hkv, (n_seq - 1) * suffix_k_seq) || meets(suffix_v, cap, Hkv, (n_seq - 1) * suffix_v_seq))))
+    if (n_seq > 0 && (meets(q, n_seq, Hq, 0) || (Tg > 0 && (meets(prefix_k, Tg, Hkv, 0) || meets(prefix_v, Tg, Hkv, 0))) ||
+        (cap > 0 && (meets(suffix_k, cap, Hkv, (n_seq - 1) * suffix_k_seq) || meets(suffix_v, cap, Hkv, (n_seq - 1) * suffix_v_seq)))))
         return SKIPFFN_EINVAL;
-    const PartsWs W = parts_ws(n_seq * Hq, D, attn_decode_splits(n_seq, n_groups, Hq, Hkv, Tp, cap, num_cus()));
-    if (W.total > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < W.total)) return SKIPFFN_EWORKSPACE;
+    const DecodeWs ws_of = decode_ws(n_seq, n_groups, Hq, Hkv, D, Tp, cap, weights != nullptr, weights != nullptr ? weights->most_shared : 0);
+    const PartsWs& W = ws_of.parts;
+    if (ws_of.total > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < ws_of.total)) return SKIPFFN_EWORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     AttnDecodeArgs a{};
     a.n_seq = (int)n_seq; a.n_groups = (int)n_groups; a.Hq = (int)Hq; a.Hkv = (int)Hkv; a.D = (int)D;
@@ -1023,11 +1056,52 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
     a.prefix_seg = prefix_seg; a.group_off = group_off; a.suffix_len = suffix_len;
     char* ws = static_cast<char*>(workspace);
     a.part = reinterpret_cast<float*>(ws + W.part); a.stat = reinterpret_cast<float*>(ws + W.stat);
+    DecodeWeightsArgs w{};
+    if (weights != nullptr) {
+        a.most_shared = (int)std::min(weights->most_shared, n_seq);
+        a.prefix_scores = reinterpret_cast<float*>(ws + ws_of.prefix);
+        a.own_scores = reinterpret_cast<float*>(ws + ws_of.own);
+        a.lse = reinterpret_cast<float*>(ws + ws_of.lse);
+        w = DecodeWeightsArgs{weights->prefix, weights->prefix_head, weights->own, weights->own_seq, weights->own_head, weights->accumulate};
+        if (decode_weights_workgroups(a) >= ((int64_t)1 << 24)) return SKIPFFN_ESHAPE;        // a launch has fewer than 2^32 threads
+    }
     profile_mark_begin(KC_ATTN_DECODE, s);
-    hipError_t e = launch_attn_decode(a, s);
+    hipError_t e = n_seq > 0 ? launch_attn_decode(a, s) : hipSuccess;
+    if (e == hipSuccess && weights != nullptr) e = launch_decode_weights(a, w, s);
     profile_mark_end(KC_ATTN_DECODE, s);
     return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
 }
+}  // namespace
+
+int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t suffix_capacity,
+                        const skipffn_heads* q, const skipffn_heads* prefix_k, const skipffn_heads* prefix_v, const int32_t* prefix_seg,
+                        const int32_t* group_off, const skipffn_heads* suffix_k, const skipffn_heads* suffix_v, int64_t suffix_k_seq,
+                        int64_t suffix_v_seq, const int32_t* suffix_len, const skipffn_heads* out, float scale,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+    return decode_call(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v,
+                       suffix_k_seq, suffix_v_seq, suffix_len, out, scale, workspace, workspace_bytes, stream, nullptr);
+}
+
+size_t skipffn_attn_decode_weights_workspace_bytes(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp,
+                                                   int64_t suffix_capacity, int64_t most_shared) {
+    if (most_shared < 0 || check_decode(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, 1.0f) != SKIPFFN_OK) return 0;
+    return decode_ws(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, true, most_shared).total;
+}
+
+int skipffn_attn_decode_weights(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t suffix_capacity,
+                                const skipffn_heads* q, const skipffn_heads* prefix_k, const skipffn_heads* prefix_v,
+                                const int32_t* prefix_seg, const int32_t* group_off, const skipffn_heads* suffix_k,
+                                const skipffn_heads* suffix_v, int64_t suffix_k_seq, int64_t suffix_v_seq, const int32_t* suffix_len,
+                                const skipffn_heads* out, float scale, int64_t most_shared, float* prefix_weights,
+                                int64_t prefix_weights_head, float* suffix_weights, int64_t suffix_weights_seq,
+                                int64_t suffix_weights_head, void* workspace, size_t workspace_bytes, uint32_t flags, void* stream) {
+    if (flags & ~SKIPFFN_FLAG_DW_ACCUMULATE) return SKIPFFN_EUNSUPPORTED;
+    const DecodeWeights w{most_shared, prefix_weights, prefix_weights_head, suffix_weights, suffix_weights_seq, suffix_weights_head,
+                          (flags & SKIPFFN_FLAG_DW_ACCUMULATE) != 0};
+    return decode_call(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v,
+                       suffix_k_seq, suffix_v_seq, suffix_len, out, scale, workspace, workspace_bytes, stream, &w);
+}
+
 
 // ---- what the keys receive -----------------------------------------------------------------------------
 namespace {

@@ -18,7 +18,11 @@ namespace skipffn {
 
 constexpr int DEC_KEYS = 32;
 
-template <int DP>
+// SCORES: the products of every row and the keys it sees are left in the workspace as well, from which decode_weights.hip takes what the keys
+// receive once the rows' sums are known
+typedef float f32x4_dword __attribute__((ext_vector_type(4), aligned(4)));       // a group's rows begin anywhere
+
+template <int DP, bool SCORES>
 __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_kernel(const AttnDecodeArgs P) {
     constexpr int ROWB = tile_row_bytes<DP>(), TILE = DEC_KEYS * ROWB;
     static_assert(2 * TILE >= DP * 32 * 4, "a wavefront's sums fit where its tiles were");
@@ -34,7 +38,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
     // What depends on the group is loaded with its bounds, and so are the lengths if a wavefront holds them all: one latency, not three.
     const bool few = P.n_seq <= 64;
     const int all_own = few && lane < P.n_seq && P.cap > 0 ? P.suffix_len[lane] : 0;
-    int s0 = 0, ns = 0, p0 = 0, p1 = 0;
+    int s0 = 0, ns = 0, p0 = 0, p1 = 0, first_of_group = 0;
     for (int i0 = 0, before = 0; i0 <= P.n_groups; i0 += 64) {
         const int i = i0 + lane;
         int lo = 0, hi = 0, pb = 0, pe = 0;
@@ -53,6 +57,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
             ns = min(__builtin_amdgcn_readlane(hi, l) - s0, members);
             p0 = __builtin_amdgcn_readlane(pb, l);
             p1 = __builtin_amdgcn_readlane(pe, l);
+            if constexpr (SCORES) first_of_group = __builtin_amdgcn_readlane(lo, l);
             break;
         }
         before += __builtin_amdgcn_readlane(incl, 63);
@@ -82,7 +87,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
     const uint32_t pk_off = Load::first(lane, P.pk_tok, P.D), pv_off = Load::first(lane, P.pv_tok, P.D);
     const uint32_t sk_off = Load::first(lane, P.sk_tok, P.D), sv_off = Load::first(lane, P.sv_tok, P.D);
     Load lk, lv;
-    int next_keys = 0, next_of = -1;                     // of the tile under way: its keys, and whose they are (-1: all rows')
+    int next_keys = 0, next_of = -1, next_k0 = 0;        // of the tile under way: its keys, whose they are (-1: all rows'), the first of them
     bool dropped = false, seen = false;                  // seen: the row sees a key of the wavefront's
     auto own_tile = [&](int u, int& i, int& k0, int& n) {    // member, first key, its keys
         i = __builtin_ctzll(__ballot(u < own_sum));
@@ -93,12 +98,14 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
         if (t < prefix_tiles) {
             next_of = -1;
             next_keys = min(p1 - p0 - t * DEC_KEYS, DEC_KEYS);
+            next_k0 = t * DEC_KEYS;
             lk.load(HeadRows{P.pk + kvh * P.pk_head + (int64_t)p0 * P.pk_tok, P.pk_tok}, t * DEC_KEYS, p1 - p0, P.D, pk_off);
             lv.load(HeadRows{P.pv + kvh * P.pv_head + (int64_t)p0 * P.pv_tok, P.pv_tok}, t * DEC_KEYS, p1 - p0, P.D, pv_off);
         } else {
             int i, k0, n;
             own_tile(t - prefix_tiles, i, k0, n);
             next_of = i;
+            next_k0 = k0;
             next_keys = min(n - k0, DEC_KEYS);
             lk.load(HeadRows{P.sk + (s0 + i) * P.sk_seq + kvh * P.sk_head, P.sk_tok}, k0, n, P.D, sk_off);
             lv.load(HeadRows{P.sv + (s0 + i) * P.sv_seq + kvh * P.sv_head, P.sv_tok}, k0, n, P.D, sv_off);
@@ -119,6 +126,13 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
         }
         const bool sees = next_of < 0 || member == next_of;
         seen |= sees;
+        float* score = nullptr;                          // of the row and the tile's first key
+        if constexpr (SCORES) {
+            const int m = s0 - first_of_group + member;
+            if (r < rows && sees && next_of >= 0) score = P.own_scores + ((int64_t)(s0 + member) * P.Hq + head) * P.cap + next_k0;
+            else if (r < rows && sees && m < P.most_shared)
+                score = P.prefix_scores + ((int64_t)(kvh * P.most_shared + m) * g + hb * 32 + r % heads) * P.Tp + p0 + next_k0;
+        }
         lk.store(tk, lane);
         lv.store(tv, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -136,6 +150,19 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
             if (i + AHEAD < N) f[i % AHEAD] = frag_rows<DP>(rows_at, 0, i + AHEAD);
         }
         __builtin_amdgcn_sched_barrier(0);
+        if (SCORES && score != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                const int k = 2 * i + 4 * h;
+                if (k + 4 <= keys) {
+                    *reinterpret_cast<f32x4_dword*>(score + k) = f32x4_dword{s[i], s[i + 1], s[i + 2], s[i + 3]};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 3; ++e)
+                        if (k + e < keys) score[k + e] = s[i + e];
+                }
+            }
+        }
         if (keys < DEC_KEYS) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
@@ -229,6 +256,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
         for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(P.part + at * attn_padded_columns(DP) + jd + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
         return;
     }
+    if (SCORES && jd == 0) P.lse[(int64_t)hq * P.n_seq + seq] = top == -INFINITY ? INFINITY : fmaf(top, c, __builtin_amdgcn_logf(sum));
     const float inv = top == -INFINITY ? 0.0f : 1.0f / sum;   // a row that sees no key is zero
     bf16_t* out = P.out + (int64_t)seq * P.o_tok + hq * P.o_head;
 #pragma unroll
@@ -261,15 +289,20 @@ int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv,
 
 hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s) {
     const dim3 grid((uint32_t)decode_blocks(a.n_seq, a.n_groups, a.Hq, a.Hkv), (uint32_t)a.splits);
-    if (a.D <= 64) attn_decode_kernel<64><<<grid, ATT_THREADS, 0, s>>>(a);
-    else if (a.D <= 96) attn_decode_kernel<96><<<grid, ATT_THREADS, 0, s>>>(a);
-    else attn_decode_kernel<128><<<grid, ATT_THREADS, 0, s>>>(a);
+    if (a.lse != nullptr) {
+        if (a.D <= 64) attn_decode_kernel<64, true><<<grid, ATT_THREADS, 0, s>>>(a);
+        else if (a.D <= 96) attn_decode_kernel<96, true><<<grid, ATT_THREADS, 0, s>>>(a);
+        else attn_decode_kernel<128, true><<<grid, ATT_THREADS, 0, s>>>(a);
+    } else if (a.D <= 64) attn_decode_kernel<64, false><<<grid, ATT_THREADS, 0, s>>>(a);
+    else if (a.D <= 96) attn_decode_kernel<96, false><<<grid, ATT_THREADS, 0, s>>>(a);
+    else attn_decode_kernel<128, false><<<grid, ATT_THREADS, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     AttnJoinArgs j{};
     j.T = a.n_seq; j.Hq = a.Hq; j.D = a.D; j.splits = a.splits; j.scale_log2 = a.scale_log2;
     j.part = a.part; j.stat = a.stat;
     j.out = a.out; j.o_tok = a.o_tok; j.o_head = a.o_head;
+    j.lse = a.lse;
     return launch_attn_join(j, s);
 }
 

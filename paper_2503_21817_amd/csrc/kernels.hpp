@@ -216,7 +216,19 @@ struct AttnDecodeArgs {
     const bf16_t* sk; const bf16_t* sv; int sk_tok, sv_tok; int64_t sk_head, sv_head, sk_seq, sv_seq;
     const int32_t* prefix_seg; const int32_t* group_off; const int32_t* suffix_len;
     float* part; float* stat;                     // splits > 1: as in AttnJoinArgs
+    // With weights (lse not null): the products of a row and its keys, of the first most_shared sequences of a group [Hkv][most_shared][Hq / Hkv][Tp] and
+    // of own rows [n_seq][Hq][cap], and every row's log-sum-exp [Hq][n_seq], as AttnArgs::lse
+    int most_shared; float* prefix_scores; float* own_scores; float* lse;
 };
+// What the keys of single tokens receive, from what is left of launch_attn_decode: added to, or put into, the weights of prefix row t at
+// prefix_w[kv head * prefix_head + t], of own row t of a sequence at own_w[sequence * own_seq + kv head * own_head + t]
+struct DecodeWeightsArgs {
+    float* prefix_w; int64_t prefix_head;
+    float* own_w; int64_t own_seq, own_head;
+    int accumulate;
+};
+int64_t decode_weights_workgroups(const AttnDecodeArgs& a);
+hipError_t launch_decode_weights(const AttnDecodeArgs& a, const DecodeWeightsArgs& w, hipStream_t s);
 // parts that the keys of a sequence are cut into
 int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t Tp, int64_t cap, int ncu);
 hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s);
