@@ -343,11 +343,8 @@ def _own_step(s):
 
 def _own_evict(s):
     from paper_2503_21817_amd import binding as B
-    if "workspace" not in s:
-        n = s["seg_out"].numel() - (1 if s["packed"] else 0)
-        s["workspace"] = _bytes(B.skipffn_kv_evict_workspace_bytes(s["k"].shape[-3], n, s["k"].shape[-2]))
     B.skipffn_kv_evict(s["k"], s["v"], s["weights"], s["seg"], s["n_keep"], s["k_out"], s["v_out"], s["weights_out"], s["keep"],
-                       s["seg_out"], first=s["first"], recent=s["recent"], workspace=s["workspace"])
+                       s["seg_out"], first=s["first"], recent=s["recent"])
     return s["k_out"], s["v_out"], s["weights_out"], s["keep"], s["seg_out"]
 
 
