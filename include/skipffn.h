@@ -413,6 +413,29 @@ int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, 
                              int64_t last, float* weights, int64_t weights_head, void* workspace, size_t workspace_bytes, uint32_t flags,
                              void* stream);
 
+/* ---- eviction: a cache cut down to the rows that received most ---------------------------
+ * Of every sequence and key/value head, each on its own, n_keep rows stay (all of them where there are no more): the `first` first and the `recent`
+ * last rows before all others (by index where n_keep holds not even these), then by weight, the larger first; equal weights by index, a
+ * NaN after every number.  Kept rows stay in their order.
+ * packed != 0: rows of all sequences one after the other, as a prefix of skipffn_attn_decode:
+ *   k, v [T, Hkv, D], weights f32 [Hkv, T]; seg i32 [n_seq + 1] device: sequence s has the rows seg[s] .. seg[s+1])
+ *   k_out, v_out [T_out, Hkv, D] OUT, weights_out f32 and keep i32 [Hkv, T_out] OUT: sequence s has the rows seg_out[s] .. seg_out[s+1])
+ *   of them; seg_out i32 [n_seq + 1] device OUT.  Kept rows past T_out are dropped: T, or the sum of the budgets, holds all
+ * packed == 0: a capacity of rows for every sequence, as the own rows of skipffn_attn_decode:
+ *   k, v [n_seq][T, Hkv, D], weights [n_seq][Hkv, T] by strides of sequence and head; seg i32 [n_seq] device: rows in use (clamped to 0 .. T)
+ *   k_out, v_out [n_seq][T_out, Hkv, D], weights_out, keep [n_seq][Hkv, T_out] OUT; seg_out i32 [n_seq] device OUT: rows left, at most T_out
+ *   n_keep / n_keep_dev  one host value, or i32 [n_seq] on the device
+ *   weights_out     the kept rows' weights, or NULL
+ *   keep            the kept rows' numbers, counted from their sequence's first row
+ * Rows past a sequence's are left as they were, in every output.  Strides in elements; those of sequences are not read where packed.
+ * What k_out and v_out span meets neither k nor v, weights_out not weights (kept rows would race); no two elements of an output are one.
+ * Rows are copied bit for bit.  T, T_out < 2^30, D and strides of k, v as in skipffn_attn_forward.  Deterministic. */
+int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T_out, int packed, const skipffn_heads* k, const skipffn_heads* v,
+                     int64_t k_seq, int64_t v_seq, const float* weights, int64_t weights_head, int64_t weights_seq, const int32_t* seg,
+                     int64_t n_keep, const int32_t* n_keep_dev, int64_t first, int64_t recent, const skipffn_heads* k_out,
+                     const skipffn_heads* v_out, int64_t k_out_seq, int64_t v_out_seq, float* weights_out, int64_t weights_out_head,
+                     int64_t weights_out_seq, int32_t* keep, int64_t keep_head, int64_t keep_seq, int32_t* seg_out, void* stream);
+
 /* ---- norm and rotation of queries and keys (between the projection and the attention) ------
  * For every token t and every head x of q and k, with n = x, or with SKIPFFN_FLAG_QK_NORM
  *     n = x * rsqrt(mean(x^2) + eps) * gain          (mean over the head's D columns; gain_q, gain_k bf16 [D] or NULL = ones),

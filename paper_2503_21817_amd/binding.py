@@ -81,6 +81,8 @@ _SIGNATURES = {
     "skipffn_attn_key_weights_workspace_bytes": (c_size_t, [c_int64] * 7),
     "skipffn_attn_key_weights": (c_int, [c_int64] * 6 + [c_void_p] * 4 + [c_int, c_float, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
                                                                         c_size_t, c_uint32, c_void_p]),
+    "skipffn_kv_evict": (c_int, [c_int64] * 5 + [c_int] + [c_void_p] * 2 + [c_int64] * 2 + [c_void_p] + [c_int64] * 2 + [c_void_p, c_int64, c_void_p] +
+                         [c_int64] * 2 + [c_void_p] * 2 + [c_int64] * 2 + [c_void_p] + [c_int64] * 2 + [c_void_p] + [c_int64] * 2 + [c_void_p] * 2),
     "skipffn_qk_rope_forward": (c_int, [c_int64] * 6 + [c_void_p] * 3 + [c_void_p] * 3 + [c_void_p] * 2 + [c_float, c_void_p, c_int64] +
                                 [c_void_p] * 3 + [c_uint32, c_void_p]),
     "skipffn_qk_rope_backward_workspace_bytes": (c_size_t, [c_int64] * 4),
@@ -477,10 +479,10 @@ def skipffn_attn_decode_weights(q, prefix_k, prefix_v, prefix_seg, group_off, su
     _check(lib().skipffn_attn_decode_weights(*args, most_shared, *pw, *sw, *ws, flags, stream), where)
 
 
-def _weights(t, shape, where, device):
-    """(address, stride) of float32 weights [..., heads, rows] whose rows lie together, and of what is before them."""
-    if t.dtype is not torch.float32 or t.shape != shape or t.get_device() != device or (t.stride(-1) != 1 and t.numel() > 0 and shape[-1] > 1):
-        raise ValueError(f"{where}: a float32 tensor {tuple(shape)} on the device of the call, with contiguous rows, is wanted")
+def _weights(t, shape, where, device, dtype=torch.float32):
+    """(address, strides) of weights (or numbers) [..., heads, rows] whose rows lie together, and of what is before them."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or (t.stride(-1) != 1 and t.numel() > 0 and shape[-1] > 1):
+        raise ValueError(f"{where}: a {dtype} tensor {tuple(shape)} on the device of the call, with contiguous rows, is wanted")
     return (t.data_ptr(),) + tuple(st if t.numel() > 0 and n > 1 else 0 for st, n in zip(t.stride()[:-1], shape[:-1]))
 
 
@@ -504,6 +506,32 @@ def skipffn_attn_key_weights(q, k, seg_q, seg_k, saved, weights, *, causal=True,
                                           None if seg_k is None else _ints(seg_k, n1, where, dev), 1 if causal else 0,
                                           D ** -0.5 if scale is None else scale, _buffer(saved, Tq * Hq * 4, where, dev)[0],
                                           -1 if last is None else last, w, w_head, ws, ws_bytes, flags, _stream(dev)), where)
+
+
+def skipffn_kv_evict(k, v, weights, seg, n_keep, k_out, v_out, weights_out, keep, seg_out, *, first=0, recent=0):
+    """Packed rows: k, v bf16 [T, Hkv, D], weights f32 [Hkv, T], seg i32 [n_seq + 1] -> k_out, v_out [T_out, Hkv, D], weights_out (or None) and keep i32
+    [Hkv, T_out], seg_out i32 [n_seq + 1].  Own rows: k, v [n_seq, T, Hkv, D], weights [n_seq, Hkv, T], seg i32 [n_seq] -> k_out, v_out
+    [n_seq, T_out, Hkv, D], weights_out, keep [n_seq, Hkv, T_out], seg_out i32 [n_seq].  n_keep: int, or an i32 [n_seq] device tensor."""
+    where = "skipffn_kv_evict"
+    dev = _device(k, where)
+    packed = k.dim() == 3
+    *_, T, Hkv, D = k.shape
+    T_out = k_out.shape[-3]
+    n_seq = seg.numel() - 1 if packed else k.shape[0]
+    lead = () if packed else (n_seq,)
+    src, dst, put = (*lead, T, Hkv, D), (*lead, T_out, Hkv, D), (*lead, Hkv, T_out)
+    hold, at = _heads(where, dev, (k, src), (v, src), (k_out, dst), (v_out, dst))
+    seq = [0] * 4 if packed or n_seq <= 1 else [t.stride(0) if t.numel() > 0 else 0 for t in (k, v, k_out, v_out)]
+
+    def strides(t, shape, dtype=torch.float32):          # address, of heads, of sequences
+        a, *st = _weights(t, shape, where, dev, dtype)
+        return (a, st[-1], 0 if packed else st[0])
+    w, kp = strides(weights, (*lead, Hkv, T)), strides(keep, put, torch.int32)
+    wo = (None, 0, 0) if weights_out is None else strides(weights_out, put)
+    nk, nkd = (0, _ints(n_keep, n_seq, where, dev)) if isinstance(n_keep, torch.Tensor) else (int(n_keep), None)
+    n = n_seq + 1 if packed else n_seq
+    _check(lib().skipffn_kv_evict(n_seq, Hkv, D, T, T_out, 1 if packed else 0, at[0], at[1], seq[0], seq[1], *w, _ints(seg, n, where, dev), nk, nkd,
+                                  first, recent, at[2], at[3], seq[2], seq[3], *wo, *kp, _ints(seg_out, n, where, dev), _stream(dev)), where)
 
 
 def _floats(t, n, where, device):

@@ -21,7 +21,7 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 SOURCES = ["api.hip", "compact.hip", "rowops.hip", "summary.hip", "select.hip", "merge.hip", "probe.hip", "gemm_inst.hip", "fewrows.hip", "midrows.hip", "countrows.hip",
            "attn_fwd.hip", "attn_bwd.hip", "attn_decode.hip", "attn_join.hip",
-           "rope.hip", "key_weights.hip", "decode_weights.hip"]
+           "rope.hip", "key_weights.hip", "decode_weights.hip", "evict.hip"]
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

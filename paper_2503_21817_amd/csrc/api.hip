@@ -1283,6 +1283,92 @@ int skipffn_qk_rope_backward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int6
     return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
 }
 
+// ---- eviction by what the rows received -------------------------------------------------------------------
+namespace {
+// Elements of `inner` in a row and of dimensions with these strides and sizes: none is another's
+struct Dim { int64_t stride, n; };
+bool apart(int64_t inner, Dim a, Dim b, Dim c) {
+    Dim d[3] = {a, b, c};
+    std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
+    int64_t extent = inner;
+    for (const Dim& x : d) {
+        if (x.n <= 1) continue;
+        if (x.stride < extent) return false;
+        extent += (x.n - 1) * x.stride;
+    }
+    return true;
+}
+bool ranges_meet(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+bool bad4(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
+}  // namespace
+
+int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T_out, int packed, const skipffn_heads* k, const skipffn_heads* v,
+                     int64_t k_seq, int64_t v_seq, const float* weights, int64_t weights_head, int64_t weights_seq, const int32_t* seg,
+                     int64_t n_keep, const int32_t* n_keep_dev, int64_t first, int64_t recent, const skipffn_heads* k_out,
+                     const skipffn_heads* v_out, int64_t k_out_seq, int64_t v_out_seq, float* weights_out, int64_t weights_out_head,
+                     int64_t weights_out_seq, int32_t* keep, int64_t keep_head, int64_t keep_seq, int32_t* seg_out, void* stream) {
+    if (n_seq < 0 || Hkv <= 0 || D <= 0 || T < 0 || T_out < 0 || first < 0 || recent < 0 || (n_keep < 0 && n_keep_dev == nullptr)) return SKIPFFN_EINVAL;
+    if ((D & 7) || D > ATTN_MAX_D || n_seq > 65535 || Hkv > 65535 || T >= (1 << 30) || T_out >= (1 << 30)) return SKIPFFN_ESHAPE;
+    int st;
+    if ((st = check_heads(k, T, Hkv, D, false)) || (st = check_heads(v, T, Hkv, D, false)) || (st = check_heads(k_out, T_out, Hkv, D, true)) ||
+        (st = check_heads(v_out, T_out, Hkv, D, true)))
+        return st;
+    const int64_t seqs = packed ? 1 : n_seq, most = (int64_t)1 << 44;
+    if (packed) k_seq = v_seq = k_out_seq = v_out_seq = weights_seq = weights_out_seq = keep_seq = 0;
+    const int64_t strides[4] = {k_seq, v_seq, k_out_seq, v_out_seq};
+    const int64_t more[6] = {weights_head, weights_seq, weights_out_head, weights_out_seq, keep_head, keep_seq};
+    for (int64_t x : strides) {
+        if (x < 0) return SKIPFFN_EINVAL;
+        if ((x & 7) || x >= most) return SKIPFFN_ESHAPE;
+    }
+    for (int64_t x : more) {
+        if (x < 0) return SKIPFFN_EINVAL;
+        if (x >= most) return SKIPFFN_ESHAPE;
+    }
+    if (n_seq == 0) return SKIPFFN_OK;
+    if (bad_seg(seg) || bad_seg(seg_out) || (n_keep_dev != nullptr && bad_seg(n_keep_dev))) return SKIPFFN_EINVAL;
+    if (T > 0 && bad4(weights)) return SKIPFFN_EINVAL;
+    if (T_out > 0) {
+        if (bad4(keep) || (weights_out != nullptr && bad4(weights_out)) || k_out->data == v_out->data) return SKIPFFN_EINVAL;
+        const skipffn_heads *outs[2] = {k_out, v_out}, *ins[2] = {k, v};
+        for (int o = 0; o < 2; ++o) {
+            if (!apart(D, {outs[o]->token_stride, T_out}, {outs[o]->head_stride, Hkv}, {strides[2 + o], seqs})) return SKIPFFN_EINVAL;
+            for (int i = 0; i < 2 && T > 0; ++i)
+                if (ranges_meet(outs[o]->data, heads_span(outs[o], T_out, Hkv, D) + (seqs - 1) * strides[2 + o] * 2, ins[i]->data,
+                                heads_span(ins[i], T, Hkv, D) + (seqs - 1) * strides[i] * 2))
+                    return SKIPFFN_EINVAL;
+        }
+        auto span = [&](int64_t head, int64_t seq, int64_t rows) { return ((seqs - 1) * seq + (Hkv - 1) * head + rows) * 4; };
+        if (!apart(T_out, {keep_head, Hkv}, {keep_seq, seqs}, {0, 1})) return SKIPFFN_EINVAL;
+        if (weights_out != nullptr && (!apart(T_out, {weights_out_head, Hkv}, {weights_out_seq, seqs}, {0, 1}) ||
+                                       (T > 0 && ranges_meet(weights_out, span(weights_out_head, weights_out_seq, T_out), weights,
+                                                             span(weights_head, weights_seq, T)))))
+            return SKIPFFN_EINVAL;
+    }
+    const int64_t cap = (int64_t)1 << 30;
+    EvictArgs a{};
+    a.n_seq = (int)n_seq; a.Hkv = (int)Hkv; a.D = (int)D; a.T = (int)T; a.T_out = (int)T_out; a.packed = packed != 0;
+    a.n_keep = (int)std::min(std::max<int64_t>(n_keep, 0), cap); a.n_keep_dev = n_keep_dev;
+    a.first = (int)std::min(first, cap); a.recent = (int)std::min(recent, cap);
+    a.k = EvictSrc{in(k), (int)k->token_stride, k->head_stride}; a.v = EvictSrc{in(v), (int)v->token_stride, v->head_stride};
+    a.k_out = EvictDst{to(k_out), (int)k_out->token_stride, k_out->head_stride};
+    a.v_out = EvictDst{to(v_out), (int)v_out->token_stride, v_out->head_stride};
+    a.k_seq = k_seq; a.v_seq = v_seq; a.ko_seq = k_out_seq; a.vo_seq = v_out_seq;
+    a.w = weights; a.w_head = weights_head; a.w_seq = weights_seq;
+    a.w_out = weights_out; a.wo_head = weights_out_head; a.wo_seq = weights_out_seq;
+    a.keep = keep; a.keep_head = keep_head; a.keep_seq = keep_seq;
+    a.seg = seg; a.seg_out = seg_out;
+    if (evict_workgroups(a) >= ((int64_t)1 << 24)) return SKIPFFN_ESHAPE;                    // a launch has fewer than 2^32 threads
+    hipStream_t s = (hipStream_t)stream;
+    profile_mark_begin(KC_EVICT, s);
+    hipError_t e = launch_evict(a, s);
+    profile_mark_end(KC_EVICT, s);
+    return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
+}
+
 // ---- measurement aid ---------------------------------------------------------------------------------
 int skipffn_probe_mfma(int64_t blocks, int64_t iters, int random_operands, float* out, int64_t* clocks,
                        void* stream) {

@@ -250,6 +250,24 @@ struct KeyWeightsPlan { int sets; int64_t blocks; int parts; };
 KeyWeightsPlan key_weights_plan(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t last, int ncu);
 hipError_t launch_attn_key_weights(const AttnArgs& a, const KeyWeightsArgs& w, const KeyWeightsPlan& p, hipStream_t s);
 
+// ---- eviction by what the rows received (evict.hip) ---------------------------------------------------------------------
+// packed: the rows of sequence s are seg[s] .. seg[s + 1]) of T, what is left of them seg_out[s] .. of T_out; otherwise they are rows 0 .. seg[s]) of T, s times the
+// sequence strides on, and seg_out[s] of T_out are left
+struct EvictSrc { const bf16_t* p; int tok; int64_t head; };
+struct EvictDst { bf16_t* p; int tok; int64_t head; };
+struct EvictArgs {
+    int n_seq, Hkv, D, T, T_out, packed, n_keep, first, recent;
+    EvictSrc k, v; EvictDst k_out, v_out;
+    int64_t k_seq, v_seq, ko_seq, vo_seq;
+    const float* w; int64_t w_head, w_seq;
+    float* w_out; int64_t wo_head, wo_seq;        // or null
+    int32_t* keep; int64_t keep_head, keep_seq;   // rows kept, counted from their sequence's first
+    const int32_t* seg; int32_t* seg_out;
+    const int32_t* n_keep_dev;                    // [n_seq], or null: n_keep for all
+};
+int64_t evict_workgroups(const EvictArgs& a);     // of its larger launch, in workgroups of 256
+hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
+
 // ---- norm and rotation of queries and keys (rope.hip) -------------------------------------------------------------
 // Element (t, h, d) of a tensor lies at p[t * tok + h * head + d]
 struct RopeIn { const bf16_t* p; int tok; int64_t head; };

@@ -1,0 +1,204 @@
+"""Eviction through the C ABI against the oracle: rows, weights and numbers are equal, bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import skipffn_oracle as O
+from paper_2503_21817_amd import binding as B
+from helpers import bits_of, to_dev_bf16
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(v):
+    return torch.tensor(np.asarray(v, dtype=np.int32)).cuda()
+
+
+def some_weights(rng, n, kind):
+    if kind == "sums":
+        return np.where(rng.random(n) < 0.1, 0.0, np.exp(2 * rng.standard_normal(n))).astype(np.float32)
+    if kind == "few values":
+        return rng.integers(0, 3, n).astype(np.float32)
+    if kind == "one value":
+        return np.full(n, 0.25, dtype=np.float32)
+    x = rng.standard_normal(n).astype(np.float32)        # "any": signs, infinities, NaN, zeros of both signs
+    for v in (np.nan, np.inf, -np.inf, 0.0, -0.0):
+        x[rng.random(n) < 0.1] = v
+    return x
+
+
+class Evict:
+    def __init__(self, rows, Hkv, D, packed, T_out, kind="sums", by_head=True, seed=0):
+        rng = self.rng = np.random.default_rng(seed + sum(rows) + D)
+        self.rows, self.Hkv, self.D, self.packed, self.T_out, self.n = list(rows), Hkv, D, packed, T_out, len(rows)
+        self.T = sum(rows) + 3 if packed else max(rows) + 2
+        lead = () if packed else (self.n,)
+
+        def cache(T, fill=None):
+            shape = (*lead, Hkv, T, D) if by_head else (*lead, T, Hkv, D)
+            t = to_dev_bf16(O.f64_to_bf16_bits(rng.standard_normal(shape))) if fill is None else torch.full(shape, fill, dtype=torch.bfloat16, device="cuda")
+            return t.transpose(-3, -2) if by_head else t
+        self.k, self.v, self.ko, self.vo = cache(self.T), cache(self.T), cache(T_out, 7.0), cache(T_out, 7.0)
+        self.w_host = np.stack([some_weights(rng, self.T, kind) for _ in range(Hkv * max(1, len(lead) * self.n))]).reshape(*lead, Hkv, self.T)
+        self.w = torch.from_numpy(self.w_host).cuda()
+        self.wo = torch.full((*lead, Hkv, T_out + 1), 7.0, device="cuda")[..., :T_out]
+        self.keep = torch.full((*lead, Hkv, T_out), -7, dtype=torch.int32, device="cuda")
+        self.seg = ints(np.concatenate([[0], np.cumsum(rows)])) if packed else ints(rows)
+        self.seg_out = torch.full_like(self.seg, -7)
+
+    def run(self, n_keep, first=0, recent=0, weights_out=True):
+        budget = ints(n_keep) if isinstance(n_keep, (list, tuple)) else n_keep
+        B.skipffn_kv_evict(self.k, self.v, self.w, self.seg, budget, self.ko, self.vo, self.wo if weights_out else None, self.keep, self.seg_out,
+                           first=first, recent=recent)
+
+    def check(self, n_keep, first=0, recent=0, weights_out=True):
+        torch.cuda.synchronize()
+        k, v, ko, vo = (bits_of(t).reshape(t.shape) for t in (self.k, self.v, self.ko, self.vo))
+        wo, keep, seven = self.wo.cpu().numpy(), self.keep.cpu().numpy(), O.f64_to_bf16_bits(np.array([7.0]))[0]
+        seg, at, used = [0], 0, np.zeros((self.n, self.T_out), dtype=bool)
+        for s, n in enumerate(self.rows):
+            a = sum(self.rows[:s]) if self.packed else 0
+            for h in range(self.Hkv):
+                w = self.w_host[h, a:a + n] if self.packed else self.w_host[s, h, :n]
+                budget = n_keep[s] if isinstance(n_keep, (list, tuple)) else n_keep
+                want = O.evict_choice(w, budget, first, recent)
+                # what T_out has no room for is dropped: packed rows at the end, own rows by a smaller budget
+                want = want[:self.T_out - at] if self.packed else O.evict_choice(w, min(budget, self.T_out), first, recent)
+                m = len(want)
+                i, src = ((h, slice(at, at + m)), (a + want, h)) if self.packed else ((s, h, slice(0, m)), (s, want, h))
+                dst = (slice(at, at + m), h) if self.packed else (s, slice(0, m), h)
+                used[0 if self.packed else s, at:at + m] = True
+                if self.packed and at + m == self.T_out:
+                    m_all = len(O.evict_choice(w, budget, first, recent))
+                    if m < m_all:                        # dropped rows: the budget is cut, not the list
+                        want = O.evict_choice(w, m, first, recent)
+                        src = (a + want, h)
+                assert np.array_equal(keep[i], want), (s, h)
+                assert np.array_equal(ko[dst], k[src]) and np.array_equal(vo[dst], v[src]), (s, h)
+                if weights_out:
+                    assert np.array_equal(wo[i].view(np.int32), w[want].view(np.int32)), (s, h)
+            at = at + m if self.packed else 0
+            seg.append(at if self.packed else m)
+        assert self.seg_out.cpu().tolist() == (seg if self.packed else seg[1:])
+        rest = ~used[0] if self.packed else ~used
+        assert (ko[rest] == seven).all() and (vo[rest] == seven).all()
+        keep, wo = (np.moveaxis(x, -2, 0)[:, rest] for x in (keep, wo))
+        assert (keep == -7).all() and (wo == 7.0).all()
+
+
+ROWS = [(1,), (40, 0, 300, 7), (1000, 1024, 1025, 3), (2049, 4096), (5000, 200)]
+
+
+@pytest.mark.parametrize("rows", ROWS, ids=str)
+@pytest.mark.parametrize("Hkv,D", [(1, 128), (3, 64), (2, 72), (8, 8)])
+@pytest.mark.parametrize("packed", [True, False], ids=["packed", "own"])
+@pytest.mark.parametrize("kind", ["sums", "few values", "one value", "any"])
+def test_rows_that_received_most_stay(rows, Hkv, D, packed, kind):
+    print(f"evict {rows} heads {Hkv} D={D} packed={packed} {kind}", flush=True)
+    for n_keep, first, recent in ((100, 4, 30), (1, 0, 0), (max(rows) // 2, 0, 0), (33, 50, 60)):
+        e = Evict(rows, Hkv, D, packed, sum(min(n, n_keep) for n in rows) + 2 if packed else n_keep + 1, kind, by_head=D != 64)
+        e.run(n_keep, first, recent)
+        e.check(n_keep, first, recent)
+
+
+@pytest.mark.parametrize("rows", [(20000,), (33000, 17), (65536,), (70000, 5)], ids=str)
+@pytest.mark.parametrize("kind", ["sums", "few values", "any"])
+def test_long_caches(rows, kind):
+    """Up to 64 keys a thread in registers, and past that."""
+    for n_keep in (1, 8000, max(rows) - 1):
+        e = Evict(rows, 2, 8, True, sum(min(n, n_keep) for n in rows), kind)
+        e.run(n_keep, 4, n_keep // 2)
+        e.check(n_keep, 4, n_keep // 2)
+    e = Evict(rows, 1, 8, False, 500, kind)
+    e.run(500, 4, 100)
+    e.check(500, 4, 100)
+
+
+def test_a_budget_for_every_sequence():
+    rows, budget = (300, 0, 5, 1000, 64), (100, 3, 9, 0, 64)
+    for packed in (True, False):
+        e = Evict(rows, 4, 64, packed, 169 + 3 if packed else 100, "sums")
+        e.run(budget, 2, 10)
+        e.check(budget, 2, 10)
+    e = Evict(rows, 4, 64, True, 172, "sums")
+    e.run((-5, 3, -1, 50, 64), 2, 10)                    # below nothing is nothing
+    e.check((0, 3, 0, 50, 64), 2, 10)
+
+
+def test_nothing_goes_and_nothing_stays():
+    for packed in (True, False):
+        e = Evict((50, 7), 2, 64, packed, 57 if packed else 60, "any")
+        e.run(1000)
+        e.check(1000)
+        e = Evict((50, 7), 2, 64, packed, 0 if packed else 4)
+        e.run(0, 3, 3)
+        e.check(0, 3, 3)
+
+
+def test_more_rows_than_there_is_room_for():
+    e = Evict((50, 70, 30), 2, 64, True, 60)
+    e.run(40, 2, 2)
+    e.check(40, 2, 2)
+    e = Evict((50, 70, 30), 2, 64, False, 25)
+    e.run(40, 2, 2)
+    e.check(40, 2, 2)
+
+
+def test_weights_need_not_be_kept():
+    e = Evict((300, 20), 2, 64, True, 120)
+    e.run(100, 1, 5, weights_out=False)
+    e.check(100, 1, 5, weights_out=False)
+
+
+def test_many_sequences():
+    rows = [i * 13 % 200 for i in range(150)]
+    e = Evict(rows, 2, 16, True, sum(min(n, 70) for n in rows))
+    e.run(70, 1, 30)
+    e.check(70, 1, 30)
+
+
+def test_offsets_that_are_no_offsets_read_and_write_inside():
+    e = Evict((50, 7), 2, 64, True, 40)
+    e.seg.copy_(ints([-5, 2 ** 31 - 1, 30]))             # clamped: all rows, then none
+    e.run(20)
+    torch.cuda.synchronize()
+    assert e.seg_out.tolist() == [0, 20, 20]
+    e = Evict((50, 7), 2, 64, False, 40)
+    e.seg.copy_(ints([2 ** 31 - 1, -4]))
+    e.run(20)
+    torch.cuda.synchronize()
+    assert e.seg_out.tolist() == [20, 0]
+
+
+def test_offsets_past_32_bits():
+    """Own rows of two sequences 2^31 elements apart."""
+    n, far = 5000, 2 ** 31 + 64
+    big = torch.zeros(far + n * 256, dtype=torch.bfloat16, device="cuda").as_strided((2, n, 2, 128), (far, 256, 128, 1))
+    rng = np.random.default_rng(1)
+    src = to_dev_bf16(O.f64_to_bf16_bits(rng.standard_normal((2, 300, 2, 128))))
+    big[:, n - 300:] = src
+    w = torch.zeros(2, 2, n, device="cuda")
+    w[..., n - 300::2] = 1.0
+    e = lambda *s, **k: torch.zeros(*s, device="cuda", **k)
+    ko, vo, keep, seg_out = e(2, 150, 2, 128, dtype=torch.bfloat16), e(2, 150, 2, 128, dtype=torch.bfloat16), e(2, 2, 150, dtype=torch.int32), e(2, dtype=torch.int32)
+    B.skipffn_kv_evict(big, big, w, ints([n, n]), 150, ko, vo, None, keep, seg_out)
+    assert seg_out.tolist() == [150, 150] and bool((keep == torch.arange(n - 300, n, 2, device="cuda")).all())
+    assert torch.equal(ko, src[:, ::2]) and torch.equal(vo, src[:, ::2])
+
+
+def test_captured_and_replayed():
+    e = Evict((3000, 700, 1), 4, 64, True, 901)
+    e.run(450, 4, 100)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        e.run(450, 4, 100)
+    for turn in range(3):
+        e.w_host = np.stack([some_weights(e.rng, e.T, "sums") for _ in range(4)])
+        e.w.copy_(torch.from_numpy(e.w_host))
+        for t in (e.ko, e.vo, e.wo):
+            t.fill_(7.0)
+        e.keep.fill_(-7)
+        torch.cuda.synchronize()
+        graph.replay()
+        e.check(450, 4, 100)
