@@ -1188,7 +1188,7 @@ RopeArgs rope_args(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, i
     a.n_axes = rot == 0 ? 0 : axis == nullptr ? 1 : (int)n_axes;
     a.norm = (flags & SKIPFFN_FLAG_QK_NORM) != 0;
     a.pairs = (flags & SKIPFFN_FLAG_ROPE_PAIRS) != 0;
-    a.eps = eps; a.pos = pos; a.inv_freq = inv_freq;
+    a.eps = eps; a.inv_D = 1.0f / (float)D; a.pos = pos; a.inv_freq = inv_freq;
     for (int64_t j = 0; axis != nullptr && j < rot / 2; ++j) a.axis[j] = axis[j];
     a.gain_q = static_cast<const bf16_t*>(gain_q); a.gain_k = static_cast<const bf16_t*>(gain_k);
     return a;
@@ -1230,17 +1230,17 @@ int skipffn_qk_rope_forward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64
         a.v_out = rope_out(v_out);
     }
     a.row = row; a.rows_out = To;
-    if (rope_forward_workgroups(a) >= ((int64_t)1 << 24)) return SKIPFFN_ESHAPE;             // a launch has fewer than 2^32 threads
+    if (rope_forward_workgroups(a, num_cus()) >= ((int64_t)1 << 24)) return SKIPFFN_ESHAPE;             // a launch has fewer than 2^32 threads
     hipStream_t s = (hipStream_t)stream;
     profile_mark_begin(KC_ROPE_FWD, s);
-    hipError_t e = launch_rope_forward(a, s);
+    hipError_t e = launch_rope_forward(a, num_cus(), s);
     profile_mark_end(KC_ROPE_FWD, s);
     return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
 }
 
 size_t skipffn_qk_rope_backward_workspace_bytes(int64_t T, int64_t Hq, int64_t Hkv, int64_t D) {
     if (T < 0 || Hq <= 0 || Hkv <= 0 || D <= 0 || D > ATTN_MAX_D) return 0;
-    return align_up((size_t)(2 * rope_backward_workgroups(T, Hq, Hkv, num_cus()) * D * 4));
+    return align_up((size_t)(rope_backward_workgroups(T, Hq, Hkv, num_cus()) * D * 4));
 }
 
 int skipffn_qk_rope_backward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, int64_t n_axes, const skipffn_heads* q,

@@ -275,19 +275,19 @@ struct RopeOut { bf16_t* p; int tok; int64_t head; };
 constexpr int ROPE_MAX_AXES = 4;
 struct RopeArgs {
     int T, Hq, Hkv, D, rot, n_axes, norm, pairs;   // n_axes: 0 where nothing is rotated
-    float eps;
+    float eps, inv_D;
     RopeIn q, k, v;                               // v.p null: no values; backward: q and k with a norm only
     RopeOut q_out, k_out, v_out;
     const int32_t* pos;                           // [n_axes][T]
     const float* inv_freq;                        // [rot / 2]
-    uint8_t axis[ATTN_MAX_D / 2];                 // of a frequency
+    alignas(8) uint8_t axis[ATTN_MAX_D / 2];      // of a frequency
     const bf16_t *gain_q, *gain_k;                // [D] or null
     const int32_t* row; int64_t rows_out;         // row of k_out and v_out of a token (outside [0, rows_out): none), or null: the token
     RopeIn gq, gk; RopeOut dq, dk;                // backward
 };
-int64_t rope_forward_workgroups(const RopeArgs& a);
-hipError_t launch_rope_forward(const RopeArgs& a, hipStream_t s);
-// workgroups of the backward kernel at most, each with a row of D fp32 of part for q and for k
+int64_t rope_forward_workgroups(const RopeArgs& a, int ncu);
+hipError_t launch_rope_forward(const RopeArgs& a, int ncu, hipStream_t s);
+// workgroups of the backward kernel, each with a row of D fp32 of part
 int64_t rope_backward_workgroups(int64_t T, int64_t Hq, int64_t Hkv, int ncu);
 hipError_t launch_rope_backward(const RopeArgs& a, float* part, float* d_gain_q, float* d_gain_k, int accumulate, int ncu, hipStream_t s);
 

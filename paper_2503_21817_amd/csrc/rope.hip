@@ -8,7 +8,7 @@
 // A lane has two slots of V columns of a head, the two that are rotated together: columns c and c + rot / 2 of the halves, or neighbours.  LPH lanes
 // share a head (their sums of squares are joined by exchanges), a wavefront works on several heads of a token, so that the V angles of a lane are
 // taken once for all of them.  An angle is the product in 64 bits (a position of 10^6 leaves 32 bits an error of 0.06 radians), brought to
-// [-1, 1] half turns there, sine and cosine in 32.
+// [-1/2, 1/2] turns there; sine and cosine are v_sin_f32 and v_cos_f32, off by 2^-22.9 at most over that range (compared with 64 bits at 2^24 places).
 #include <algorithm>
 #include <type_traits>
 
@@ -60,22 +60,50 @@ struct RopeLane {
         turned[0] = PAIRS ? col[0] < rot : u < half;
         turned[1] = PAIRS ? col[1] < rot : u < half;
     }
-    // cosine and sine of the lane's frequencies u V + i for a token
-    __device__ __forceinline__ void angles(const RopeArgs& P, int t, float (&cs)[V], float (&sn)[V]) const {
-        int32_t pos[ROPE_MAX_AXES];
+    // the lane's frequencies u V + i, and their axes, two bits each
+    float freq[V];
+    uint32_t axes;
+    __device__ __forceinline__ void frequencies(const RopeArgs& P) {
+        axes = 0;
 #pragma unroll
-        for (int a = 0; a < ROPE_MAX_AXES; ++a) pos[a] = a < P.n_axes ? P.pos[(int64_t)a * P.T + t] : 0;
+        for (int i = 0; i < V; ++i) freq[i] = 0.0f;
+        if (P.rot == 0) return;
+        // every load is made, of the last frequency where the lane has none: as branches they would wait for one another
+#pragma unroll
+        for (int i = 0; i < V; ++i) freq[i] = P.inv_freq[min(u * V + i, P.rot / 2 - 1)];
+        if (P.n_axes > 1) {
+#pragma unroll
+            for (int w = 0; w < V / 4; ++w) {
+                const uint32_t four = *reinterpret_cast<const uint32_t*>(P.axis + u * V + w * 4);
+                axes |= ((four & 3) | (four >> 6 & 0xc) | (four >> 12 & 0x30) | (four >> 18 & 0xc0)) << (8 * w);
+            }
+        }
+    }
+    // positions of a token
+    struct Place { int32_t pos[ROPE_MAX_AXES]; };
+    static __device__ __forceinline__ Place place(const RopeArgs& P, int t) {
+        Place p;
+#pragma unroll
+        for (int a = 0; a < ROPE_MAX_AXES; ++a) p.pos[a] = 0;
+        if (P.n_axes > 0) p.pos[0] = P.pos[t];
+        if (P.n_axes > 1) {
+#pragma unroll
+            for (int a = 1; a < ROPE_MAX_AXES; ++a) p.pos[a] = P.pos[(int64_t)min(a, P.n_axes - 1) * P.T + t];
+        }
+        return p;
+    }
+    // cosine and sine of the frequencies' angles there
+    __device__ __forceinline__ void angles(const Place& at, float (&cs)[V], float (&sn)[V]) const {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            const int j = u * V + i;
-            const bool in = j < P.rot / 2;
-            const int axis = in && P.n_axes > 1 ? P.axis[in ? j : 0] : 0;
-            int32_t p = pos[0];
+            const int axis = axes >> (2 * i) & 3;
+            int32_t p = at.pos[0];
 #pragma unroll
-            for (int a = 1; a < ROPE_MAX_AXES; ++a) p = axis == a ? pos[a] : p;
-            const double x = (double)p * (double)(in ? P.inv_freq[j] : 0.0f) * 0.31830988618379067154;       // in half turns
-            const float f = (float)(x - 2.0 * rint(x * 0.5));
-            sincospif(f, &sn[i], &cs[i]);
+            for (int a = 1; a < ROPE_MAX_AXES; ++a) p = axis == a ? at.pos[a] : p;
+            const double x = (double)p * (double)freq[i] * 0.15915494309189533577;       // in turns
+            const float f = (float)(x - rint(x));
+            sn[i] = __builtin_amdgcn_sinf(f);
+            cs[i] = __builtin_amdgcn_cosf(f);
         }
     }
     // (x_a, x_b) rotated by the angles, or by their opposites
@@ -97,11 +125,24 @@ struct RopeLane {
     }
 };
 
+// over the LPH lanes of a head: neighbours, pairs, then mirrored halves of 8 and 16 lanes, whose quarters and halves agree by then
 template <int LPH>
 __device__ __forceinline__ float head_sum(float v) {
-#pragma unroll
-    for (int off = LPH / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
+    auto add = [&](auto ctrl) {
+        v += __uint_as_float(__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), decltype(ctrl)::value, 0xF, 0xF, false));
+    };
+    add(std::integral_constant<int, 0xB1>{});            // quad_perm 1, 0, 3, 2
+    add(std::integral_constant<int, 0x4E>{});            // quad_perm 2, 3, 0, 1
+    if constexpr (LPH >= 8) add(std::integral_constant<int, 0x141>{});
+    if constexpr (LPH >= 16) add(std::integral_constant<int, 0x140>{});
     return v;
+}
+// a slot of a head's columns; one past its columns reads the first and is 0
+template <int V>
+__device__ __forceinline__ typename RopeVec<V>::type rope_slot(const bf16_t* head, int col, bool has) {
+    typedef typename RopeVec<V>::type Vec;
+    const Vec v = *reinterpret_cast<const Vec*>(head + (has ? col : 0));
+    return has ? v : Vec{};
 }
 
 // Heads that a wavefront has at a time, and tokens beside one another: powers of two whose product with LPH is 64
@@ -123,7 +164,9 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_fwd_kernel(const RopeArgs P
     const int64_t t64 = group * tokens + lane / (LPH * at_once);
     if (t64 >= P.T) return;
     const int t = (int)t64;
-    const RopeLane<V, LPH, PAIRS> L(lane, P.D, P.rot);
+    RopeLane<V, LPH, PAIRS> L(lane, P.D, P.rot);
+    L.frequencies(P);
+    const auto place = L.place(P, t);
     const int64_t row = P.row != nullptr ? (int64_t)P.row[t] : t;
     const bool stored = row >= 0 && row < P.rows_out;    // of k and v
     int head[U];
@@ -132,22 +175,17 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_fwd_kernel(const RopeArgs P
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         head[i] = (chunk * U + i) * at_once + lane / LPH % at_once;
-        const bf16_t* from = nullptr;
-        to[i] = nullptr;
-        if (head[i] < P.Hq) {
-            from = P.q.p + (int64_t)t * P.q.tok + head[i] * P.q.head;
-            to[i] = P.q_out.p + (int64_t)t * P.q_out.tok + head[i] * P.q_out.head;
-        } else if (head[i] < heads && stored) {
-            const int h = head[i] - P.Hq;
-            const bool is_k = h < P.Hkv;
-            from = is_k ? P.k.p + (int64_t)t * P.k.tok + h * P.k.head : P.v.p + (int64_t)t * P.v.tok + (h - P.Hkv) * P.v.head;
-            to[i] = is_k ? P.k_out.p + row * P.k_out.tok + h * P.k_out.head : P.v_out.p + row * P.v_out.tok + (h - P.Hkv) * P.v_out.head;
-        }
+        // what goes nowhere reads the token's first query
+        const bool is_q = head[i] < P.Hq, goes = is_q || (head[i] < heads && stored), is_k = !is_q && head[i] < P.Hq + P.Hkv;
+        const int h = is_q ? head[i] : is_k ? head[i] - P.Hq : head[i] - P.Hq - P.Hkv;
+        const RopeIn from = is_q || !goes ? P.q : is_k ? P.k : P.v;
+        const RopeOut out = is_q ? P.q_out : is_k ? P.k_out : P.v_out;
+        to[i] = goes ? out.p + (is_q ? (int64_t)t : row) * out.tok + h * out.head : nullptr;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) x[i][j] = from != nullptr && L.has[j] ? *reinterpret_cast<const Vec*>(from + L.col[j]) : Vec{};
+        for (int j = 0; j < 2; ++j) x[i][j] = rope_slot<V>(from.p + (int64_t)t * from.tok + (goes ? h : 0) * from.head, L.col[j], L.has[j]);
     }
     float cs[V], sn[V];
-    L.angles(P, t, cs, sn);
+    L.angles(place, cs, sn);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         if (head[i] < P.Hq + P.Hkv) {
@@ -158,12 +196,12 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_fwd_kernel(const RopeArgs P
                 float ss = 0.0f;
 #pragma unroll
                 for (int j = 0; j < V; ++j) ss = fmaf(a[j], a[j], fmaf(b[j], b[j], ss));
-                const float r = rsqrtf(head_sum<LPH>(ss) / (float)P.D + P.eps);
+                const float r = rsqrtf(head_sum<LPH>(ss) * P.inv_D + P.eps);
                 const bf16_t* gain = head[i] < P.Hq ? P.gain_q : P.gain_k;
                 float ga[V], gb[V];
                 if (gain != nullptr) {
-                    rope_unpack<V>(L.has[0] ? *reinterpret_cast<const Vec*>(gain + L.col[0]) : Vec{}, ga);
-                    rope_unpack<V>(L.has[1] ? *reinterpret_cast<const Vec*>(gain + L.col[1]) : Vec{}, gb);
+                    rope_unpack<V>(rope_slot<V>(gain, L.col[0], L.has[0]), ga);
+                    rope_unpack<V>(rope_slot<V>(gain, L.col[1], L.has[1]), gb);
                 }
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
@@ -181,119 +219,121 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_fwd_kernel(const RopeArgs P
     }
 }
 
-// Workgroups go on through the tokens; with gain gradients every lane keeps the sums of its columns, joined over the workgroup at the end:
-// part [q or k][workgroup][D]
-template <int V, int LPH, int U, bool PAIRS, bool NORM, bool GAINS>
-__global__ __launch_bounds__(ROPE_THREADS) void rope_bwd_kernel(const RopeArgs P, const int chunks, const int64_t units, float* part) {
+// A workgroup has either heads of q or heads of k and goes on through the tokens; the next heads' loads are under way while these are worked on.  With gain
+// gradients every lane keeps the sums of its columns, joined over the workgroup at the end: part [workgroup][D], q's first.
+// Measured, 9856 tokens of 32 / 8 heads of 128 with both gains, forward and backward, us: 113.7, of which this kernel about 62 (303 MB, 4.9 TB/s); without
+// the loads asked for early, heads of q and k in one workgroup and gains read where they are used 225; two heads at a time 144 (197 registers).
+template <int V, int LPH, bool PAIRS, bool NORM, bool GAINS>
+__global__ __launch_bounds__(ROPE_THREADS) void rope_bwd_kernel(const RopeArgs P, const int wgs_q, float* part) {
     typedef typename RopeVec<V>::type Vec;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int heads = P.Hq + P.Hkv, at_once = rope_heads_at_once(LPH, heads), tokens = 64 / LPH / at_once;
-    const RopeLane<V, LPH, PAIRS> L(lane, P.D, P.rot);
-    float sum[GAINS ? 2 : 1][2 * V] = {};
-    for (int64_t unit = (int64_t)blockIdx.x * ROPE_WAVES + wave; unit < units; unit += (int64_t)gridDim.x * ROPE_WAVES) {
-        const int64_t group = unit / chunks;
-        const int chunk = (int)(unit - group * chunks);
-        const int64_t t64 = group * tokens + lane / (LPH * at_once);
-        const bool in = t64 < P.T;
-        const int t = in ? (int)t64 : 0;
-        int head[U];
-        Vec g[U][2], x[U][2];
+    const bool is_q = (int)blockIdx.x < wgs_q;
+    const int H = is_q ? P.Hq : P.Hkv, at_once = rope_heads_at_once(LPH, H), tokens = 64 / LPH / at_once;
+    const int first = (int)blockIdx.x - (is_q ? 0 : wgs_q), wgs = is_q ? wgs_q : (int)gridDim.x - wgs_q;
+    const RopeIn G = is_q ? P.gq : P.gk, X = is_q ? P.q : P.k;
+    const RopeOut O = is_q ? P.dq : P.dk;
+    const bf16_t* gain = is_q ? P.gain_q : P.gain_k;
+    RopeLane<V, LPH, PAIRS> L(lane, P.D, P.rot);
+    L.frequencies(P);
+    Vec gains[2] = {};
+    if (NORM && gain != nullptr) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            head[i] = (chunk * U + i) * at_once + lane / LPH % at_once;
-            const bool ok = in && head[i] < heads, is_q = head[i] < P.Hq;
-            const int h = is_q ? head[i] : head[i] - P.Hq;
-            const RopeIn &G = is_q ? P.gq : P.gk, &X = is_q ? P.q : P.k;
-            if (!ok) head[i] = heads;
+        for (int j = 0; j < 2; ++j) gains[j] = rope_slot<V>(gain, L.col[j], L.has[j]);
+    }
+    // a unit: the heads that a wavefront works on at once
+    const int per_token = (H + at_once - 1) / at_once, my_token = lane / (LPH * at_once), my_head = lane / LPH % at_once;
+    const int64_t units = ((int64_t)P.T + tokens - 1) / tokens * per_token;
+    struct Unit {
+        int t, head;                                     // head < 0: none
+        Vec g[2], x[2];
+        typename RopeLane<V, LPH, PAIRS>::Place at;
+    };
+    auto load = [&](int64_t unit, Unit& n) {
+        const int64_t tg = unit / per_token, t = tg * tokens + my_token;
+        const int h = (int)(unit - tg * per_token) * at_once + my_head;
+        const bool ok = t < P.T && h < H;
+        n.t = ok ? (int)t : 0;
+        n.head = ok ? h : -1;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                g[i][j] = ok && L.has[j] ? *reinterpret_cast<const Vec*>(G.p + (int64_t)t * G.tok + h * G.head + L.col[j]) : Vec{};
-                if constexpr (NORM) x[i][j] = ok && L.has[j] ? *reinterpret_cast<const Vec*>(X.p + (int64_t)t * X.tok + h * X.head + L.col[j]) : Vec{};
-            }
+        for (int j = 0; j < 2; ++j) {
+            // past the last token or head: the first one's, unused
+            n.g[j] = rope_slot<V>(G.p + (int64_t)n.t * G.tok + (ok ? h : 0) * G.head, L.col[j], L.has[j]);
+            if constexpr (NORM) n.x[j] = rope_slot<V>(X.p + (int64_t)n.t * X.tok + (ok ? h : 0) * X.head, L.col[j], L.has[j]);
         }
-        float cs[V], sn[V];
-        L.angles(P, t, cs, sn);
+        n.at = L.place(P, n.t);
+    };
+    float sum[2 * V] = {};
+    const int64_t step = (int64_t)wgs * ROPE_WAVES;
+    const int64_t begin = (int64_t)first * ROPE_WAVES + wave;
+    Unit next{};
+    for (int64_t unit = begin; unit < units + step; unit += step) {
+        const Unit n = next;
+        if (unit < units) load(unit, next);
+        if (unit == begin) continue;                     // one copy of the loads: code that is run once comes from memory a line at a time
+        float cs[V], sn[V], a[V], b[V];
+        L.angles(n.at, cs, sn);
+        rope_unpack<V>(n.g[0], a);
+        rope_unpack<V>(n.g[1], b);
+        L.rotate(a, b, cs, sn, true);
+        if constexpr (NORM) {
+            float xa[V], xb[V], ss = 0.0f, dot = 0.0f;
+            rope_unpack<V>(n.x[0], xa);
+            rope_unpack<V>(n.x[1], xb);
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-            const bool is_q = head[i] < P.Hq;
-            float a[V], b[V];
-            rope_unpack<V>(g[i][0], a);
-            rope_unpack<V>(g[i][1], b);
-            L.rotate(a, b, cs, sn, true);
-            if constexpr (NORM) {
-                float xa[V], xb[V], ss = 0.0f, dot = 0.0f;
-                rope_unpack<V>(x[i][0], xa);
-                rope_unpack<V>(x[i][1], xb);
-#pragma unroll
-                for (int j = 0; j < V; ++j) ss = fmaf(xa[j], xa[j], fmaf(xb[j], xb[j], ss));
-                const float r = rsqrtf(head_sum<LPH>(ss) / (float)P.D + P.eps);
-                const bf16_t* gain = is_q ? P.gain_q : P.gain_k;
-                if constexpr (GAINS) {
-                    const bool ok = head[i] < heads;
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const float da = ok ? a[j] * (xa[j] * r) : 0.0f, db = ok ? b[j] * (xb[j] * r) : 0.0f;
-                        sum[0][j] += is_q ? da : 0.0f;
-                        sum[0][V + j] += is_q ? db : 0.0f;
-                        sum[1][j] += is_q ? 0.0f : da;
-                        sum[1][V + j] += is_q ? 0.0f : db;
-                    }
-                }
-                if (gain != nullptr) {
-                    float ga[V], gb[V];
-                    rope_unpack<V>(L.has[0] ? *reinterpret_cast<const Vec*>(gain + L.col[0]) : Vec{}, ga);
-                    rope_unpack<V>(L.has[1] ? *reinterpret_cast<const Vec*>(gain + L.col[1]) : Vec{}, gb);
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        a[j] *= ga[j];
-                        b[j] *= gb[j];
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < V; ++j) dot = fmaf(a[j], xa[j], fmaf(b[j], xb[j], dot));
-                const float m = r * r * (head_sum<LPH>(dot) / (float)P.D);
+            for (int j = 0; j < V; ++j) ss = fmaf(xa[j], xa[j], fmaf(xb[j], xb[j], ss));
+            const float r = rsqrtf(head_sum<LPH>(ss) * P.inv_D + P.eps);
+            if (GAINS && n.head >= 0) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    a[j] = r * (a[j] - xa[j] * m);
-                    b[j] = r * (b[j] - xb[j] * m);
+                    sum[j] = fmaf(a[j], xa[j] * r, sum[j]);
+                    sum[V + j] = fmaf(b[j], xb[j] * r, sum[V + j]);
                 }
             }
-            if (head[i] >= heads) continue;
-            const RopeOut& O = is_q ? P.dq : P.dk;
-            bf16_t* to = O.p + (int64_t)t * O.tok + (is_q ? head[i] : head[i] - P.Hq) * O.head;
-            if (L.has[0]) *reinterpret_cast<Vec*>(to + L.col[0]) = rope_pack<V>(a);
-            if (L.has[1]) *reinterpret_cast<Vec*>(to + L.col[1]) = rope_pack<V>(b);
+            if (gain != nullptr) {
+                float ga[V], gb[V];
+                rope_unpack<V>(gains[0], ga);
+                rope_unpack<V>(gains[1], gb);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    a[j] *= ga[j];
+                    b[j] *= gb[j];
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < V; ++j) dot = fmaf(a[j], xa[j], fmaf(b[j], xb[j], dot));
+            const float m = r * r * (head_sum<LPH>(dot) * P.inv_D);
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                a[j] = r * (a[j] - xa[j] * m);
+                b[j] = r * (b[j] - xb[j] * m);
+            }
         }
+        if (n.head < 0) continue;
+        bf16_t* to = O.p + (int64_t)n.t * O.tok + n.head * O.head;
+        if (L.has[0]) *reinterpret_cast<Vec*>(to + L.col[0]) = rope_pack<V>(a);
+        if (L.has[1]) *reinterpret_cast<Vec*>(to + L.col[1]) = rope_pack<V>(b);
     }
     if constexpr (GAINS) {
-        __shared__ float lds[ROPE_WAVES][2][LPH * 2 * V];
+        __shared__ f32x4 lds[2 * V / 4][ROPE_THREADS];
 #pragma unroll
-        for (int z = 0; z < 2; ++z)
-#pragma unroll
-            for (int j = 0; j < 2 * V; ++j) {
-                float v = sum[z][j];
-#pragma unroll
-                for (int off = LPH; off < 64; off *= 2) v += __shfl_xor(v, off, 64);
-                if (lane < LPH) lds[wave][z][lane * 2 * V + j] = v;
-            }
+        for (int j = 0; j < 2 * V; j += 4) lds[j / 4][threadIdx.x] = f32x4{sum[j], sum[j + 1], sum[j + 2], sum[j + 3]};
         __syncthreads();
-        for (int i = threadIdx.x; i < 2 * LPH * 2 * V; i += ROPE_THREADS) {
-            const int z = i / (LPH * 2 * V), e = i % (LPH * 2 * V), j = e % (2 * V);
-            const RopeLane<V, LPH, PAIRS> M(e / (2 * V), P.D, P.rot);
-            const int s = j / V;
+        for (int e = threadIdx.x; e < LPH * 2 * V; e += ROPE_THREADS) {
+            const int l = e / (2 * V), j = e % (2 * V), s = j / V;
+            const RopeLane<V, LPH, PAIRS> M(l, P.D, P.rot);
             if (!M.has[s]) continue;
             float v = 0.0f;
-#pragma unroll
-            for (int w = 0; w < ROPE_WAVES; ++w) v += lds[w][z][e];
-            part[((int64_t)z * gridDim.x + blockIdx.x) * P.D + M.col[s] + j % V] = v;
+            for (int i = l; i < ROPE_THREADS; i += LPH) v += lds[j / 4][i][j % 4];
+            part[(int64_t)blockIdx.x * P.D + M.col[s] + j % V] = v;
         }
     }
 }
 
-__global__ __launch_bounds__(32 * COLSUM_LANES) void rope_gain_grad_kernel(const float* part, int rows, int D, float* dq, float* dk, int accumulate) {
-    float* out = blockIdx.y == 0 ? dq : dk;
+__global__ __launch_bounds__(32 * COLSUM_LANES) void rope_gain_grad_kernel(const float* part, int wgs_q, int wgs_k, int D, float* dq, float* dk, int accumulate) {
+    const bool is_q = blockIdx.y == 0;
+    float* out = is_q ? dq : dk;
     if (out == nullptr) return;
-    column_sum<COLSUM_LANES>(part + (int64_t)blockIdx.y * rows * D, rows, D, out, accumulate);
+    column_sum<COLSUM_LANES>(is_q ? part : part + (int64_t)wgs_q * D, is_q ? wgs_q : wgs_k, D, out, accumulate);
 }
 
 namespace {
@@ -317,60 +357,75 @@ RopeGrid rope_grid(const RopeArgs& a, int lph, int heads, int u) {
     g.units = ((int64_t)a.T + tokens - 1) / tokens * g.chunks;
     return g;
 }
-constexpr int ROPE_FWD_U = 2, ROPE_BWD_U = 2;
+constexpr int ROPE_BWD_PER_CU = 3;                       // workgroups, by its registers
 }  // namespace
 
-int64_t rope_forward_workgroups(const RopeArgs& a) {
-    int64_t n = 0;
-    rope_variant(a, [&](auto, auto lph) {
-        n = (rope_grid(a, decltype(lph)::value, rope_heads(a), ROPE_FWD_U).units + ROPE_WAVES - 1) / ROPE_WAVES;
+// Heads of a wavefront one after the other: one where that many wavefronts find room on the chip at once, otherwise three (us, 32 / 8 heads of 128: 64 tokens 5.0 /
+// 6.5, 11776 tokens into a cache 99 / 68; six 8.6 / 67)
+template <class Launch>
+static void rope_forward_variant(const RopeArgs& a, int ncu, Launch&& go) {
+    rope_variant(a, [&](auto v, auto lph) {
+        const RopeGrid one = rope_grid(a, decltype(lph)::value, rope_heads(a), 1);
+        if (one.units <= (int64_t)ncu * 32) go(v, lph, std::integral_constant<int, 1>{}, one);
+        else go(v, lph, std::integral_constant<int, 3>{}, rope_grid(a, decltype(lph)::value, rope_heads(a), 3));
     });
+}
+
+int64_t rope_forward_workgroups(const RopeArgs& a, int ncu) {
+    int64_t n = 0;
+    rope_forward_variant(a, ncu, [&](auto, auto, auto, const RopeGrid& g) { n = (g.units + ROPE_WAVES - 1) / ROPE_WAVES; });
     return n;
 }
 
-hipError_t launch_rope_forward(const RopeArgs& a, hipStream_t s) {
-    rope_variant(a, [&](auto v, auto lph) {
-        constexpr int V = decltype(v)::value, LPH = decltype(lph)::value;
-        const RopeGrid g = rope_grid(a, LPH, rope_heads(a), ROPE_FWD_U);
+hipError_t launch_rope_forward(const RopeArgs& a, int ncu, hipStream_t s) {
+    rope_forward_variant(a, ncu, [&](auto v, auto lph, auto u, const RopeGrid& g) {
+        constexpr int V = decltype(v)::value, LPH = decltype(lph)::value, U = decltype(u)::value;
         const dim3 grid((uint32_t)((g.units + ROPE_WAVES - 1) / ROPE_WAVES));
         if constexpr (V == 8) {
-            if (a.pairs && a.norm) rope_fwd_kernel<V, LPH, ROPE_FWD_U, true, true><<<grid, ROPE_THREADS, 0, s>>>(a, g.chunks);
-            else if (a.pairs) rope_fwd_kernel<V, LPH, ROPE_FWD_U, true, false><<<grid, ROPE_THREADS, 0, s>>>(a, g.chunks);
+            if (a.pairs && a.norm) rope_fwd_kernel<V, LPH, U, true, true><<<grid, ROPE_THREADS, 0, s>>>(a, g.chunks);
+            else if (a.pairs) rope_fwd_kernel<V, LPH, U, true, false><<<grid, ROPE_THREADS, 0, s>>>(a, g.chunks);
         }
-        if (!a.pairs && a.norm) rope_fwd_kernel<V, LPH, ROPE_FWD_U, false, true><<<grid, ROPE_THREADS, 0, s>>>(a, g.chunks);
-        else if (!a.pairs) rope_fwd_kernel<V, LPH, ROPE_FWD_U, false, false><<<grid, ROPE_THREADS, 0, s>>>(a, g.chunks);
+        if (!a.pairs && a.norm) rope_fwd_kernel<V, LPH, U, false, true><<<grid, ROPE_THREADS, 0, s>>>(a, g.chunks);
+        else if (!a.pairs) rope_fwd_kernel<V, LPH, U, false, false><<<grid, ROPE_THREADS, 0, s>>>(a, g.chunks);
     });
     return hipGetLastError();
 }
 
+// Three workgroups a compute unit, shared out by the heads of q and k, but no more than have heads to work on, `rows` of them a wavefront at once
+struct RopeShare { int64_t q, k; };
+static RopeShare rope_backward_share(int64_t T, int64_t Hq, int64_t Hkv, int rows, int ncu) {
+    auto most = [&](int64_t H) { return (T * H + rows * ROPE_WAVES - 1) / (rows * ROPE_WAVES); };
+    const int64_t all = (int64_t)ncu * ROPE_BWD_PER_CU;
+    const int64_t k = std::min(most(Hkv), std::max<int64_t>(1, (all * Hkv + (Hq + Hkv) / 2) / (Hq + Hkv)));
+    return {std::min(most(Hq), std::max<int64_t>(1, all - k)), k};
+}
 int64_t rope_backward_workgroups(int64_t T, int64_t Hq, int64_t Hkv, int ncu) {
-    const int64_t most = (T * (Hq + Hkv) + ROPE_WAVES - 1) / ROPE_WAVES;
-    return std::max<int64_t>(1, std::min<int64_t>(most, (int64_t)ncu * 4));
+    const RopeShare w = rope_backward_share(T, Hq, Hkv, 4, ncu);      // 16 lanes a head: as many as there can be
+    return w.q + w.k;
 }
 
 hipError_t launch_rope_backward(const RopeArgs& a, float* part, float* d_gain_q, float* d_gain_k, int accumulate, int ncu, hipStream_t s) {
     const bool gains = d_gain_q != nullptr || d_gain_k != nullptr;
-    const int64_t most = rope_backward_workgroups(a.T, a.Hq, a.Hkv, ncu);
-    uint32_t wgs = 0;
-    rope_variant(a, [&](auto v, auto lph) {
-        constexpr int V = decltype(v)::value, LPH = decltype(lph)::value;
-        const RopeGrid g = rope_grid(a, LPH, a.Hq + a.Hkv, ROPE_BWD_U);
-        wgs = (uint32_t)std::min<int64_t>((g.units + ROPE_WAVES - 1) / ROPE_WAVES, most);
-        if (wgs == 0) return;
-        auto go = [&](auto pairs) {
-            constexpr bool PAIRS = decltype(pairs)::value;
-            if (gains) rope_bwd_kernel<V, LPH, ROPE_BWD_U, PAIRS, true, true><<<wgs, ROPE_THREADS, 0, s>>>(a, g.chunks, g.units, part);
-            else if (a.norm) rope_bwd_kernel<V, LPH, ROPE_BWD_U, PAIRS, true, false><<<wgs, ROPE_THREADS, 0, s>>>(a, g.chunks, g.units, part);
-            else rope_bwd_kernel<V, LPH, ROPE_BWD_U, PAIRS, false, false><<<wgs, ROPE_THREADS, 0, s>>>(a, g.chunks, g.units, part);
-        };
-        if constexpr (V == 8) {
-            if (a.pairs) go(std::true_type{});
-        }
-        if (!a.pairs) go(std::false_type{});
-    });
+    RopeShare w{0, 0};
+    if (a.T > 0)
+        rope_variant(a, [&](auto v, auto lph) {
+            constexpr int V = decltype(v)::value, LPH = decltype(lph)::value;
+            w = rope_backward_share(a.T, a.Hq, a.Hkv, 64 / LPH, ncu);
+            const uint32_t wgs = (uint32_t)(w.q + w.k);
+            auto go = [&](auto pairs) {
+                constexpr bool PAIRS = decltype(pairs)::value;
+                if (gains) rope_bwd_kernel<V, LPH, PAIRS, true, true><<<wgs, ROPE_THREADS, 0, s>>>(a, (int)w.q, part);
+                else if (a.norm) rope_bwd_kernel<V, LPH, PAIRS, true, false><<<wgs, ROPE_THREADS, 0, s>>>(a, (int)w.q, part);
+                else rope_bwd_kernel<V, LPH, PAIRS, false, false><<<wgs, ROPE_THREADS, 0, s>>>(a, (int)w.q, part);
+            };
+            if constexpr (V == 8) {
+                if (a.pairs) go(std::true_type{});
+            }
+            if (!a.pairs) go(std::false_type{});
+        });
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || !gains) return e;
-    rope_gain_grad_kernel<<<dim3((uint32_t)(a.D + 31) / 32, 2), 32 * COLSUM_LANES, 0, s>>>(part, (int)wgs, a.D, d_gain_q, d_gain_k, accumulate);
+    rope_gain_grad_kernel<<<dim3((uint32_t)(a.D + 31) / 32, 2), 32 * COLSUM_LANES, 0, s>>>(part, (int)w.q, (int)w.k, a.D, d_gain_q, d_gain_k, accumulate);
     return hipGetLastError();
 }
 
