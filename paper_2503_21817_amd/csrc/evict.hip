@@ -1,14 +1,12 @@
 // A cache cut down to the rows that received most: of every sequence and key/value head the n_keep rows of largest weight, where the `first` first and
 // the `recent` last ones come before all others; equal weights by index, a NaN after every number.  The choice is unique for the weights given.
 //
-// Two kernels.  One workgroup a (sequence, head) finds the cut (topk.hpp; the keys stay in registers up to 64 a thread, longer lists are read again from
-// L2 for every step) and writes the kept rows' numbers, ascending, and their weights.  Then the rows themselves: a lane takes 16 bytes of a row of
-// k and of v, a workgroup 64 rows of a head.
+// Two kernels.  One workgroup a (sequence, head) finds the cut and writes the kept rows' numbers, ascending, and their weights.  Then the rows themselves: a lane takes 16 bytes of a row of
+// k and of v, a workgroup 16 rows of a head.
 #include <algorithm>
 
 #include "kernels.hpp"
 #include "segments.hpp"
-#include "topk.hpp"
 
 namespace skipffn {
 
@@ -41,14 +39,124 @@ __device__ __forceinline__ EvictSeq evict_seq(const EvictArgs& P, int s) {
     return q;
 }
 
-constexpr int EVICT_MAXV = 64;                           // keys of a thread that stay in registers
+// The cut between what stays and what goes: the k smallest of a list's keys (rank_key) are those below `below`, and the first `ties` of those equal to it.
+// Keys are counted by their first 11 bits (the sign, the exponent and two more, for weights), a prefix sum over the counts finds where the k-th lies, and
+// those that share its bits are collected in LDS, where the next 11 and the last 10 bits are found the same way; in the list itself if they
+// are too many.
+struct EvictCut { uint32_t below; int ties; };
+constexpr uint32_t EVICT_NONE = 0xFFFFFFFFu;             // key of a NaN
+constexpr int EVICT_BINS = 2048, EVICT_CAND = 4096;
+struct EvictShared {
+    int hist[EVICT_BINS];
+    uint32_t cand[EVICT_CAND];
+    int waves[16], n_cand, bin, before, inside;
+};
+// rank_key<true> in fewer operations: with -0 made +0, a number that is not negative is turned round, a negative one increases already
+__device__ __forceinline__ uint32_t evict_key(float v) {
+    const uint32_t b = __float_as_uint(v + 0.0f), k = b ^ (~(uint32_t)((int32_t)b >> 31) >> 1);
+    return v != v ? EVICT_NONE : k;
+}
+// The number with a key, or for a key that no number has one that compares as the key would: a NaN (no weight is at least that) before all numbers, minus
+// infinity (every number is) after them
+__device__ __forceinline__ float evict_number(uint32_t key) {
+    return key > 0xFF800000u ? -INFINITY : __uint_as_float(key < 0x80000000u ? key ^ 0x7FFFFFFFu : key);
+}
+// for_keys(f) calls f with every key of the list that takes part, spread over the threads
+template <int THREADS, class ForKeys>
+__device__ __forceinline__ EvictCut evict_cut(ForKeys&& for_keys, int k, EvictShared& sh) {
+    constexpr int WAVES = THREADS / 64, PER = EVICT_BINS / THREADS;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sh.hist[tid + i * THREADS] = 0;
+    if (tid == 0) sh.n_cand = 0;
+    __syncthreads();
+    for_keys([&](uint32_t v) { atomicAdd(&sh.hist[v >> 21], 1); });        // numbers end below bin 2047, which has the NaN
+    uint32_t prefix = 0;                                 // the digits found so far
+    bool in_lds = false;
+    int cands = 0;
+    for (int digit = 0;; ++digit) {
+        const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0;
+        if (digit > 0) {
+            const uint32_t mask = 0xFFFFFFFFu << (digit == 1 ? 21 : 10), bits = digit == 1 ? EVICT_BINS - 1 : 1023;
+            auto count = [&](uint32_t v) {
+                if ((v & mask) == prefix) atomicAdd(&sh.hist[v >> shift & bits], 1);
+            };
+            if (in_lds) {
+                for (int i = tid; i < cands; i += THREADS) count(sh.cand[i]);
+            } else {
+                for_keys(count);
+            }
+        }
+        __syncthreads();
+        int h[PER], mine = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            h[i] = sh.hist[PER * tid + i];
+            sh.hist[PER * tid + i] = 0;                  // for the next digit
+            mine += h[i];
+        }
+        const int incl = wave_inclusive_sum(mine);
+        if (lane == 63) sh.waves[wave] = incl;
+        __syncthreads();
+        int before = incl - mine;
+#pragma unroll
+        for (int w = 0; w < WAVES - 1; ++w) before += w < wave ? sh.waves[w] : 0;
+        if (before < k && k <= before + mine) {          // one thread
+            int bin = 0, inside = h[0];
+#pragma unroll
+            for (int i = 1; i < PER; ++i)
+                if (bin == i - 1 && k > before + inside) {
+                    before += inside;
+                    inside = h[i];
+                    bin = i;
+                }
+            sh.bin = PER * tid + bin;
+            sh.before = before;
+            sh.inside = inside;
+        }
+        __syncthreads();
+        if (digit == 0 && sh.bin == EVICT_BINS - 1) return EvictCut{EVICT_NONE, k - sh.before};       // all numbers, and the first of the others
+        prefix |= (uint32_t)sh.bin << shift;
+        if (k == sh.before + sh.inside) return EvictCut{prefix + (1u << shift), 0};       // numbers end below 2^32 - 2^22: no wrap
+        k -= sh.before;
+        if (digit == 2) return EvictCut{prefix, k};
+        if (!in_lds && sh.inside <= EVICT_CAND) {        // uniform
+            const uint32_t with = 0xFFFFFFFFu << shift;
+            for_keys([&](uint32_t v) {
+                if ((v & with) == prefix) sh.cand[atomicAdd(&sh.n_cand, 1)] = v;
+            });
+            cands = sh.inside;
+            in_lds = true;
+            __syncthreads();
+        }
+    }
+}
 
-// MAXV > 0: lists of up to MAXV * 1024 rows in registers; LONG: longer ones too
-template <int MAXV, bool LONG>
-__global__ __launch_bounds__(TOPK_THREADS) void evict_select_kernel(const EvictArgs P) {
-    __shared__ TopkShared sh;
-    __shared__ int counts[MAXV * TOPK_WAVES];
-    const int s = (int)blockIdx.x / P.Hkv, head = (int)blockIdx.x % P.Hkv, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// Weights of a list of n rows, four consecutive ones a load (and a thread); those past its end are any of it
+typedef float f32x4_dword __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ f32x4 four_weights(const float* w, int t, int n) {
+    if (n < 4) return f32x4{w[min(t, n - 1)], w[min(t + 1, n - 1)], w[min(t + 2, n - 1)], w[min(t + 3, n - 1)]};      // uniform
+    // the last rows are read with those before them, and moved up
+    const int at = min(t, n - 4), up = t - at;
+    f32x4 v = *reinterpret_cast<const f32x4_dword*>(w + at);
+    if (__ballot(up != 0) != 0) {
+        v[0] = up == 1 ? v[1] : up == 2 ? v[2] : up == 3 ? v[3] : v[0];
+        v[1] = up == 1 ? v[2] : up == 2 ? v[3] : v[1];
+        v[2] = up == 1 ? v[3] : v[2];
+    }
+    return v;
+}
+
+// A list of up to 4 THREADS rows is read once and lies in registers.  A longer one is read again for every step, some loads of a thread under way at a time (a
+// compute unit's share of a list's bytes is bound by latency).  For the kept rows a wavefront has a range of them: it counts those that stay and those equal
+// to the cut, and when the counts of the wavefronts before it are known goes over them again and writes, without a barrier in between.
+template <int THREADS, bool LONG>
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictArgs P) {
+    constexpr int WAVES = THREADS / 64, AHEAD = LONG ? 4 : 1;
+    __shared__ EvictShared sh;
+    __shared__ int counts[WAVES][2];                     // below the cut, equal to it
+    const int s = (int)blockIdx.x / P.Hkv, head = (int)blockIdx.x % P.Hkv, tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const EvictSeq q = evict_seq(P, s);
     if (head == 0 && tid == 0) {
         if (P.packed) {
@@ -62,87 +170,133 @@ __global__ __launch_bounds__(TOPK_THREADS) void evict_select_kernel(const EvictA
     const float* w = P.w + (P.packed ? 0 : s * P.w_seq) + head * P.w_head + q.lo;
     float* w_out = P.w_out == nullptr ? nullptr : P.w_out + (P.packed ? 0 : s * P.wo_seq) + head * P.wo_head + q.to;
     int32_t* keep = P.keep + (P.packed ? 0 : s * P.keep_seq) + head * P.keep_head + q.to;
-    const int n = q.n, nv = (n + TOPK_THREADS - 1) / TOPK_THREADS;
-    auto key_of = [&](int t) { return t >= n ? TOPK_NONE : t < P.first || t >= n - P.recent ? 0u : rank_key<true>(w[t]); };
-    const bool all = q.keep >= n;                        // uniform
-    auto put = [&](int at, int t) {
-        keep[at] = t;
-        if (w_out != nullptr) w_out[at] = w[t];
+    const int n = q.n;
+    // rows that stay before all others: [0, first) and [recent, n)
+    const int first = min(P.first, n), recent = max(n - P.recent, first), stay = first + n - recent;
+    const bool in_regs = !LONG || n <= 4 * THREADS;      // uniform
+    const f32x4 mine = four_weights(w, 4 * tid, n);
+    EvictCut cut{0, 0};                                  // of the rows that do not stay anyway
+    bool among_stay = false;                             // `ties` rows of those that stay are all that is kept
+    auto give = [&](auto&& f, const f32x4& v, int t) {
+        const int t0 = __builtin_amdgcn_readfirstlane(t);           // of the wavefront's 256 rows
+        if (t0 >= first && t0 + 256 <= recent) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f(evict_key(v[j]));
+        } else if (t0 < recent && t0 + 256 > first) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (t + j >= first && t + j < recent) f(evict_key(v[j]));
+        }
     };
-    if (!LONG || nv <= MAXV) {
-        uint32_t key[MAXV];
-        // before[i]: entries flagged before entry i * 1024 + tid; every wavefront's counts go through LDS
-        auto prefix = [&](auto&& flag, int (&before)[MAXV]) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < MAXV; ++i)
-                if (i < nv) {
-                    const uint64_t m = __ballot(flag(i));
-                    before[i] = lanes_below(m);
-                    if (lane == 0) counts[i * TOPK_WAVES + wave] = __popcll(m);
-                }
-            __syncthreads();
-            if (wave == 0) {
-                int carry = 0;
-                for (int c = 0; c < nv * TOPK_WAVES; c += 64) {
-                    const bool in = c + lane < nv * TOPK_WAVES;
-                    const int v = in ? counts[c + lane] : 0, incl = wave_inclusive_sum(v);
-                    if (in) counts[c + lane] = carry + incl - v;
-                    carry += __builtin_amdgcn_readlane(incl, 63);
-                }
+    if (q.keep >= n) {
+        cut = EvictCut{EVICT_NONE, n};
+    } else if (q.keep <= stay) {
+        among_stay = true;
+        cut.ties = q.keep;
+    } else {
+        cut = evict_cut<THREADS>([&](auto&& f) {
+            if (in_regs) {
+                give(f, mine, 4 * tid);
+                return;
             }
-            __syncthreads();
+            for (int t = 4 * tid; t < recent; t += 4 * AHEAD * THREADS) {
+                f32x4 v[AHEAD];
 #pragma unroll
-            for (int i = 0; i < MAXV; ++i)
-                if (i < nv) before[i] += counts[i * TOPK_WAVES + wave];
-        };
+                for (int i = 0; i < AHEAD; ++i) v[i] = four_weights(w, t + i * 4 * THREADS, n);
 #pragma unroll
-        for (int i = 0; i < MAXV; ++i)
-            if (i < nv) key[i] = key_of(i * TOPK_THREADS + tid);
-        TopkCut cut{TOPK_NONE, n};                       // everything: every key <= NONE
-        if (!all) cut = topk_cut<MAXV>([&](int i) { return key[i]; }, nv, q.keep, sh);
-        int before[MAXV];
-        uint64_t kept = 0;                               // bit i: entry i of the thread
-        if (cut.ties > 0 && !all) {
-            prefix([&](int i) { return key[i] == cut.cut && i * TOPK_THREADS + tid < n; }, before);
+                for (int i = 0; i < AHEAD; ++i) give(f, v[i], t + i * 4 * THREADS);
+            }
+        }, q.keep - stay, sh);
+    }
+    // The wavefront's rows, 256 at a time: f(weights, the lane's first row)
+    const int blocks = (n + 255) / 256, b0 = in_regs ? wave : blocks * wave / WAVES, b1 = in_regs ? min(wave + 1, blocks) : blocks * (wave + 1) / WAVES;
+    auto for_rows = [&](auto&& f) {
+        if (in_regs) {
+            if (b0 < b1) f(mine, 4 * tid);
+            return;
+        }
+        for (int b = b0; b < b1; b += AHEAD) {
+            f32x4 v[AHEAD];
 #pragma unroll
-            for (int i = 0; i < MAXV; ++i)
-                if (i < nv && key[i] == cut.cut && before[i] < cut.ties) kept |= (uint64_t)1 << i;
+            for (int i = 0; i < AHEAD; ++i) v[i] = four_weights(w, (b + i) * 256 + 4 * lane, n);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (b + i < b1) f(v[i], (b + i) * 256 + 4 * lane);
+        }
+    };
+    // The cut as comparisons of weights, whose order is that of their keys: kept are those not below `least`, and ties are equal to `tie`
+    const float least = among_stay ? NAN : evict_number(cut.below - 1), tie = evict_number(cut.below);
+    const bool ties = cut.ties > 0, tie_nan = cut.below == EVICT_NONE;       // uniform
+    // flags of four rows, those kept below the cut and ties
+    auto flags = [&](const f32x4& x, int t, bool (&below)[4], bool (&equal)[4]) {
+        const int t0 = __builtin_amdgcn_readfirstlane(t);
+        const bool inside = t0 >= first && t0 + 256 <= recent;               // uniform
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            below[j] = x[j] >= least;
+            equal[j] = tie_nan ? x[j] != x[j] : x[j] == tie;
+        }
+        if (among_stay || !inside) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool in = t + j < n, must = t + j < first || t + j >= recent;
+                below[j] = in && !among_stay && (must || below[j]);
+                equal[j] = in && (among_stay ? must : !must && equal[j]);
+            }
+        }
+    };
+    int below = 0, equal = 0;
+    for_rows([&](const f32x4& x, int t) {
+        bool fb[4], fe[4];
+        flags(x, t, fb, fe);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            below += __popcll(__ballot(fb[j]));
+            if (ties) equal += __popcll(__ballot(fe[j]));
+        }
+    });
+    if (lane == 0) {
+        counts[wave][0] = below;
+        counts[wave][1] = equal;
+    }
+    __syncthreads();
+    int at = 0, ties_before = 0;                         // kept rows and ties of the wavefronts before this one
+    for (int i = 0; i < wave; ++i) {
+        at += counts[i][0] + min(max(cut.ties - ties_before, 0), counts[i][1]);
+        ties_before += counts[i][1];
+    }
+    for_rows([&](const f32x4& x, int t) {
+        bool kept[4], fe[4];
+        flags(x, t, kept, fe);
+        if (ties) {
+            int tie_at = ties_before;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint64_t m = __ballot(fe[j]);
+                tie_at += lanes_below(m);
+                ties_before += __popcll(m);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) kept[j] = kept[j] || (fe[j] && tie_at++ < cut.ties);
+        }
+        int to = at;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint64_t m = __ballot(kept[j]);
+            to += lanes_below(m);
+            at += __popcll(m);
         }
 #pragma unroll
-        for (int i = 0; i < MAXV; ++i)
-            if (i < nv && (key[i] < cut.cut || (all && i * TOPK_THREADS + tid < n))) kept |= (uint64_t)1 << i;
-#pragma unroll
-        for (int i = 0; i < MAXV; ++i)
-            if (i < nv && i * TOPK_THREADS + tid >= n) kept &= ~((uint64_t)1 << i);
-        prefix([&](int i) { return (kept >> i & 1) != 0; }, before);
-#pragma unroll
-        for (int i = 0; i < MAXV; ++i)
-            if (i < nv && (kept >> i & 1) != 0) put(before[i], i * TOPK_THREADS + tid);
-        return;
-    }
-    if constexpr (LONG) {
-        TopkCut cut{TOPK_NONE, n};
-        if (!all) cut = topk_cut<0>([&](int i) { return key_of(i * TOPK_THREADS + tid); }, nv, q.keep, sh);
-        int ties_before = 0, kept_before = 0;
-        for (int i = 0; i < nv; ++i) {
-            const int t = i * TOPK_THREADS + tid;
-            const uint32_t key = key_of(t);
-            int before[1] = {0};
-            if (cut.ties > 0 && !all) {
-                const int here = topk_prefix<1>([&](int) { return key == cut.cut && t < n; }, 1, sh, before);
-                before[0] += ties_before;
-                ties_before += here;
+        for (int j = 0; j < 4; ++j)
+            if (kept[j]) {
+                keep[to] = t + j;
+                if (w_out != nullptr) w_out[to] = x[j];
+                ++to;
             }
-            const bool in = t < n && (all || key < cut.cut || (key == cut.cut && before[0] < cut.ties));
-            const int here = topk_prefix<1>([&](int) { return in; }, 1, sh, before);
-            if (in) put(kept_before + before[0], t);
-            kept_before += here;
-        }
-    }
+    });
 }
 
-constexpr int EVICT_ROWS = 64, EVICT_THREADS = 256;
+constexpr int EVICT_ROWS = 16, EVICT_THREADS = 256, EVICT_SHORT = 2048, EVICT_LONG_THREADS = 1024;
 
 __global__ __launch_bounds__(EVICT_THREADS) void evict_gather_kernel(const EvictArgs P, const int chunks) {
     const int head = (int)blockIdx.x % P.Hkv, q = (int)blockIdx.x / P.Hkv;
@@ -181,15 +335,13 @@ int64_t gather_chunks(const EvictArgs& a) {
 }  // namespace
 
 int64_t evict_workgroups(const EvictArgs& a) {
-    return std::max<int64_t>((int64_t)a.n_seq * a.Hkv * (TOPK_THREADS / EVICT_THREADS), gather_chunks(a) * (a.packed ? 1 : a.n_seq) * a.Hkv);
+    return std::max<int64_t>((int64_t)a.n_seq * a.Hkv * (EVICT_LONG_THREADS / EVICT_THREADS), gather_chunks(a) * (a.packed ? 1 : a.n_seq) * a.Hkv);
 }
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
-    const dim3 grid((uint32_t)(a.n_seq * a.Hkv));
-    if (a.T <= 4 * TOPK_THREADS) evict_select_kernel<4, false><<<grid, TOPK_THREADS, 0, s>>>(a);
-    else if (a.T <= 16 * TOPK_THREADS) evict_select_kernel<16, false><<<grid, TOPK_THREADS, 0, s>>>(a);
-    else if (a.T <= EVICT_MAXV * TOPK_THREADS) evict_select_kernel<EVICT_MAXV, false><<<grid, TOPK_THREADS, 0, s>>>(a);
-    else evict_select_kernel<EVICT_MAXV, true><<<grid, TOPK_THREADS, 0, s>>>(a);
+    const uint32_t lists = (uint32_t)(a.n_seq * a.Hkv);
+    if (a.T <= EVICT_SHORT) evict_select_kernel<EVICT_SHORT / 4, false><<<lists, EVICT_SHORT / 4, 0, s>>>(a);
+    else evict_select_kernel<EVICT_LONG_THREADS, true><<<lists, EVICT_LONG_THREADS, 0, s>>>(a);
     const hipError_t e = hipGetLastError();
     const int64_t chunks = gather_chunks(a), wgs = chunks * (a.packed ? 1 : a.n_seq) * a.Hkv;
     if (e != hipSuccess || wgs == 0) return e;
