@@ -245,8 +245,8 @@ struct KeyWeightsArgs {
     float* part;                                  // parts > 1: [parts][Hkv][Tk]
 };
 constexpr int KEY_WEIGHTS_MAX_PARTS = 32;
-// sets of 32 keys of a wavefront; workgroups of a part; parts that the queries are cut into
-struct KeyWeightsPlan { int sets; int64_t blocks; int parts; };
+// workgroups of a part; parts that the queries are cut into
+struct KeyWeightsPlan { int64_t blocks; int parts; };
 KeyWeightsPlan key_weights_plan(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t last, int ncu);
 hipError_t launch_attn_key_weights(const AttnArgs& a, const KeyWeightsArgs& w, const KeyWeightsPlan& p, hipStream_t s);
 

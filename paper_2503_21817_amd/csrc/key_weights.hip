@@ -7,20 +7,20 @@
 // rounded below fp32 and every sum has one owner and a fixed order.  Where keys are few for the chip, or a causal prompt's pieces uneven, the
 // queries are cut into parts whose sums a second kernel adds.
 #include <algorithm>
+#include <cmath>
 
 #include "attn.hpp"
 
 namespace skipffn {
 
-constexpr int KW_ROWS = 64;                              // queries of a tile
-
-template <int KW> constexpr int kw_keys() { return ATT_WAVES * 32 * KW; }        // of a workgroup
+// queries of a tile; sets of 32 keys of a wavefront (one: every operand of the queries is read for one product instead of two, and LDS is the bound: 1 x 16384
+// tokens 1080 -> 1319 us, 16 x up to 616 the same); keys of a workgroup
+constexpr int KW_ROWS = 64, KW = 2, KW_KEYS = ATT_WAVES * 32 * KW;
 
 // keys of a workgroup, the longest pieces first
-template <int KW>
 __device__ __forceinline__ bool locate_keys(const AttnArgs& P, const KeyWeightsArgs& W, int lane, int q, SeqItem& it) {
     return locate_longest(P, lane, q, P.causal && W.last >= P.Tq ? ATT_WAVES * KW : 0, 1,
-                          [](int nq, int nk, int& n, int& top) { n = (nk + kw_keys<KW>() - 1) / kw_keys<KW>(); top = (nq + 31) / 32; }, it);
+                          [](int nq, int nk, int& n, int& top) { n = (nk + KW_KEYS - 1) / KW_KEYS; top = (nq + 31) / 32; }, it);
 }
 
 __device__ __forceinline__ void put_weight(const KeyWeightsArgs& W, int kvh, int key, float v) {
@@ -28,7 +28,7 @@ __device__ __forceinline__ void put_weight(const KeyWeightsArgs& W, int kvh, int
     *w = W.accumulate ? *w + v : v;
 }
 
-template <int DP, int KW>
+template <int DP>
 __global__ __launch_bounds__(ATT_THREADS, 2) void attn_key_weights_kernel(const AttnArgs P, const KeyWeightsArgs W) {
     constexpr int ROWB = tile_row_bytes<DP>(), TILE = KW_ROWS * ROWB, STAGE = TILE + KW_ROWS * 4, N = DP / 16;
     __shared__ __align__(256) char smem[2 * STAGE];
@@ -39,26 +39,14 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_key_weights_kernel(const 
     const int kvh = b % P.Hkv; b /= P.Hkv;
     const int part = b % W.parts; b /= W.parts;
     SeqItem it;
-    if (!locate_keys<KW>(P, W, lane, b, it)) return;
+    if (!locate_keys(P, W, lane, b, it)) return;
     const int nq = it.q1 - it.q0, nk = it.k1 - it.k0, ahead = nk - nq;
-    const int key0 = it.item * kw_keys<KW>() + wave * 32 * KW;           // of the wavefront
+    const int key0 = it.item * KW_KEYS + wave * 32 * KW;           // of the wavefront
     // counted rows are base .. nq; row i sees key j if j <= i + ahead
     const int base = max(nq - W.last, 0), count = nq - base;
-    const int tile0 = P.causal ? max(it.item * kw_keys<KW>() - ahead - base, 0) / KW_ROWS : 0;
+    const int tile0 = P.causal ? max(it.item * KW_KEYS - ahead - base, 0) / KW_ROWS : 0;
     const int steps = max((count + KW_ROWS - 1) / KW_ROWS - tile0, 0) * g;
     const int first = (int)((int64_t)steps * part / W.parts), last = (int)((int64_t)steps * (part + 1) / W.parts);
-
-    bf16x8 kf[KW][N];
-    {
-        char* lds = smem + wave * 32 * ROWB;
-        const bf16_t* k = P.k + kvh * P.k_head + (int64_t)(it.k0 + key0) * P.k_tok;
-        RowsIn<DP> in[KW];
-#pragma unroll
-        for (int i = 0; i < KW; ++i) in[i].load(k + (int64_t)i * 32 * P.k_tok, P.k_tok, min(nk - key0 - i * 32, 32), P.D, lane);
-#pragma unroll
-        for (int i = 0; i < KW; ++i) in[i].operands(lds, lane, kf[i]);
-    }
-    __syncthreads();
 
     const uint32_t q_off = TileLoad<DP, KW_ROWS>::first(tid, P.q_tok, P.D);
     TileLoad<DP, KW_ROWS> lq;
@@ -75,14 +63,24 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_key_weights_kernel(const 
         lq.store(st, tid);
         if (tid < KW_ROWS) reinterpret_cast<float*>(st + TILE)[tid] = -lse;
     };
+    if (first < last) load();                            // with the keys
+    bf16x8 kf[KW][N];
+    {
+        char* lds = smem + wave * 32 * ROWB;
+        const bf16_t* k = P.k + kvh * P.k_head + (int64_t)(it.k0 + key0) * P.k_tok;
+        RowsIn<DP> in[KW];
+#pragma unroll
+        for (int i = 0; i < KW; ++i) in[i].load(k + (int64_t)i * 32 * P.k_tok, P.k_tok, min(nk - key0 - i * 32, 32), P.D, lane);
+#pragma unroll
+        for (int i = 0; i < KW; ++i) in[i].operands(lds, lane, kf[i]);
+    }
+    __syncthreads();
+
     float sum[KW][16] = {};
     const float c = P.scale_log2;
     const uint32_t rows_at = lds_addr_of(smem) + rows_lane<DP>(lane);
     int tile = tile0 + first / g, head = first % g;
-    if (first < last) {
-        load();
-        store(first);
-    }
+    if (first < last) store(first);
     __syncthreads();
     for (int n = first; n < last; ++n) {
         if (n + 1 < last) load();
@@ -93,32 +91,41 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_key_weights_kernel(const 
             const int row0 = base + tile * KW_ROWS + rb * 32;
             const int seen = P.causal ? min(min(row0 + 32, nq) + ahead, nk) : nk;      // keys that the last row sees
             if (row0 >= nq || key0 >= seen) continue;
-            const float nl = st[rb * 32 + (lane & 31)];
+            float nl = st[rb * 32 + (lane & 31)];
+            // operands a few products ahead of them
+            constexpr int AHEAD = 3;
+            bf16x8 f[AHEAD];
+#pragma unroll
+            for (int d = 0; d < AHEAD; ++d) f[d] = frag_rows<DP>(at, rb * 32, d);
             f32x16 s[KW];
 #pragma unroll
             for (int i = 0; i < KW; ++i) s[i] = f32x16{};
 #pragma unroll
             for (int d = 0; d < N; ++d) {
-                const bf16x8 f = frag_rows<DP>(at, rb * 32, d);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < KW; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i][d], f, s[i], 0, 0, 0);
+                for (int i = 0; i < KW; ++i) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i][d], f[d % AHEAD], s[i], 0, 0, 0);
+                if (d + AHEAD < N) f[d % AHEAD] = frag_rows<DP>(at, rb * 32, d + AHEAD);
             }
+            __builtin_amdgcn_sched_barrier(0);
             if (row0 + 32 > nq || (P.causal && key0 + 32 * KW > row0 + 1 + ahead)) {
-                // some rows are past the sequence's, or do not see some keys: their weights are none, whatever their scores are
+                // Some rows are past the sequence's, or do not see some keys: minus infinity.  That is a weight of 0 beside a log-sum-exp that is a number; a
+                // row with another one has NaN where it sees
                 const int row = row0 + (lane & 31), keys = row >= nq ? 0 : P.causal ? row + 1 + ahead : nk;
+                const bool number = fabsf(nl) < INFINITY;
 #pragma unroll
                 for (int i = 0; i < KW; ++i)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const float w = __builtin_amdgcn_exp2f(fmaf(s[i][e], c, nl));
-                        sum[i][e] += key0 + i * 32 + 8 * (e >> 2) + 4 * h + (e & 3) < keys ? w : 0.0f;
+                        const bool sees = key0 + i * 32 + 8 * (e >> 2) + 4 * h + (e & 3) < keys;
+                        s[i][e] = !sees ? -INFINITY : number ? s[i][e] : NAN;
                     }
-            } else {
-#pragma unroll
-                for (int i = 0; i < KW; ++i)
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) sum[i][e] += __builtin_amdgcn_exp2f(fmaf(s[i][e], c, nl));
+                nl = number ? nl : 0.0f;
             }
+#pragma unroll
+            for (int i = 0; i < KW; ++i)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) sum[i][e] += __builtin_amdgcn_exp2f(fmaf(s[i][e], c, nl));
         }
         if (n + 1 < last) store(n + 1);
         __syncthreads();
@@ -147,12 +154,11 @@ __global__ __launch_bounds__(ATT_THREADS, 2) void attn_key_weights_kernel(const 
 }
 
 // the parts' sums, added in order
-template <int KW>
-__global__ __launch_bounds__(kw_keys<KW>()) void key_weights_join_kernel(const AttnArgs P, const KeyWeightsArgs W) {
+__global__ __launch_bounds__(KW_KEYS) void key_weights_join_kernel(const AttnArgs P, const KeyWeightsArgs W) {
     const int kvh = (int)blockIdx.x % P.Hkv;
     SeqItem it;
-    if (!locate_keys<KW>(P, W, threadIdx.x & 63, (int)blockIdx.x / P.Hkv, it)) return;
-    const int key = it.k0 + it.item * kw_keys<KW>() + (int)threadIdx.x;
+    if (!locate_keys(P, W, threadIdx.x & 63, (int)blockIdx.x / P.Hkv, it)) return;
+    const int key = it.k0 + it.item * KW_KEYS + (int)threadIdx.x;
     if (key >= it.k1) return;
     const float* p = W.part + (int64_t)kvh * P.Tk + key;
     float v = 0.0f;
@@ -160,20 +166,21 @@ __global__ __launch_bounds__(kw_keys<KW>()) void key_weights_join_kernel(const A
     put_weight(W, kvh, key, v);
 }
 
+// Parts that the queries are cut into.  A piece takes 1.2 us a step and 6 us to begin and end; the last ones leave the chip to themselves, so pieces are made
+// shorter until what that saves goes into beginning more of them; the second kernel takes about 4 us
 KeyWeightsPlan key_weights_plan(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t last, int ncu) {
     KeyWeightsPlan p{};
-    p.sets = 2;
-    p.blocks = (Tk / (ATT_WAVES * 32 * p.sets) + n_seq) * Hkv;
+    p.blocks = (Tk / KW_KEYS + n_seq) * Hkv;
     const int64_t rows = n_seq > 0 ? std::min(Tq / n_seq, last) : 0, steps = (rows + KW_ROWS - 1) / KW_ROWS * (Hq / Hkv);
-    p.parts = (int)std::max<int64_t>(1, std::min<int64_t>({steps / 16, (8 * (int64_t)ncu + p.blocks) / std::max<int64_t>(p.blocks, 1), KEY_WEIGHTS_MAX_PARTS}));
+    const double piece = 1.2 * (double)steps, begin = 6.0 * (double)p.blocks / (2.0 * ncu);
+    const int64_t parts = std::min<int64_t>({steps / 4, (int64_t)std::lround(std::sqrt(piece / std::max(begin, 1e-3))), KEY_WEIGHTS_MAX_PARTS});
+    p.parts = parts > 1 && piece - piece / (double)parts > 5.0 ? (int)parts : 1;
     return p;
 }
 
 template <int DP>
 static void launch_kw(const AttnArgs& a, const KeyWeightsArgs& w, const KeyWeightsPlan& p, hipStream_t s) {
-    const dim3 grid((uint32_t)(p.blocks * p.parts));
-    if (p.sets == 1) attn_key_weights_kernel<DP, 1><<<grid, ATT_THREADS, 0, s>>>(a, w);
-    else attn_key_weights_kernel<DP, 2><<<grid, ATT_THREADS, 0, s>>>(a, w);
+    attn_key_weights_kernel<DP><<<(uint32_t)(p.blocks * p.parts), ATT_THREADS, 0, s>>>(a, w);
 }
 
 hipError_t launch_attn_key_weights(const AttnArgs& a, const KeyWeightsArgs& w, const KeyWeightsPlan& p, hipStream_t s) {
@@ -182,8 +189,7 @@ hipError_t launch_attn_key_weights(const AttnArgs& a, const KeyWeightsArgs& w, c
     else launch_kw<128>(a, w, p, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.parts == 1) return e;
-    if (p.sets == 1) key_weights_join_kernel<1><<<(uint32_t)p.blocks, kw_keys<1>(), 0, s>>>(a, w);
-    else key_weights_join_kernel<2><<<(uint32_t)p.blocks, kw_keys<2>(), 0, s>>>(a, w);
+    key_weights_join_kernel<<<(uint32_t)p.blocks, KW_KEYS, 0, s>>>(a, w);
     return hipGetLastError();
 }
 
