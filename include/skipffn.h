@@ -383,7 +383,8 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
  *                   left as they were.  Not read or written where suffix_capacity == 0
  * Both are overwritten, or += with SKIPFFN_FLAG_DW_ACCUMULATE (the only flag).  `out` has the bits that skipffn_attn_decode gives; all else as
  * there.  A sequence whose row of `out` is NaN for its scores makes NaN of the weights of the rows it sees.  Deterministic.
- * workspace: at least skipffn_attn_decode_weights_workspace_bytes(...): 4 Hq (most_shared Tp + n_seq suffix_capacity) and what decode takes. */
+ * Tp + 36 n_groups and suffix_capacity < 2^24 - 64.
+ * workspace: at least skipffn_attn_decode_weights_workspace_bytes(...): about 4 Hq (most_shared Tp + n_seq suffix_capacity) and what decode takes. */
 size_t skipffn_attn_decode_weights_workspace_bytes(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp,
                                                    int64_t suffix_capacity, int64_t most_shared);
 int skipffn_attn_decode_weights(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp, int64_t suffix_capacity,

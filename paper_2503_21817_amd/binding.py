@@ -334,7 +334,7 @@ def _heads(where, device, *tensors):
     v = []
     for t, shape in tensors:
         *_, st, sh, sc = t.stride()
-        if t.numel() == 0:                               # its strides say nothing
+        if sc != 1 and t.numel() == 0:                   # its strides say nothing
             st, sh, sc = shape[-2] * shape[-1], shape[-1], 1
         if t.shape != shape or t.dtype is not torch.bfloat16 or t.get_device() != device or (sc != 1 and shape[-1] > 1):
             raise ValueError(f"{where}: a bfloat16 tensor {tuple(shape)} on the device of the call, with contiguous columns, is wanted")

@@ -987,16 +987,17 @@ DecodeWs decode_ws(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int
     W.total = W.parts.total;
     if (!weights) return W;
     W.prefix = W.total;
-    W.own = W.prefix + (n_groups > 0 ? align_up((size_t)(std::min(most_shared, n_seq) * Hq * Tp) * 4) : 0);
-    W.lse = W.own + align_up((size_t)(n_seq * Hq * cap) * 4);
+    W.own = W.prefix + (n_groups > 0 ? align_up((size_t)(std::min(most_shared, n_seq) * Hq * decode_prefix_ld(Tp, n_groups)) * 4) : 0);
+    W.lse = W.own + align_up((size_t)(n_seq * Hq * decode_own_ld(cap)) * 4);
     W.total = W.lse + align_up((size_t)(n_seq * Hq) * 4);
     return W;
 }
 
-int check_decode_weights(const DecodeWeights& w, int64_t n_seq, int64_t Hkv, int64_t Tp, int64_t cap) {
+int check_decode_weights(const DecodeWeights& w, int64_t n_seq, int64_t n_groups, int64_t Hkv, int64_t Tp, int64_t cap) {
     const int64_t most = (int64_t)1 << 44;
     if (w.most_shared < 0 || w.prefix_head < 0 || w.own_seq < 0 || w.own_head < 0) return SKIPFFN_EINVAL;
     if (w.prefix_head >= most || w.own_seq >= most || w.own_head >= most) return SKIPFFN_ESHAPE;
+    if (decode_prefix_ld(Tp, n_groups) >= DECODE_MAX_LD || decode_own_ld(cap) >= DECODE_MAX_LD) return SKIPFFN_ESHAPE;
     auto bad = [](const float* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; };
     if (Tp > 0 && (w.most_shared == 0 || bad(w.prefix) || (Hkv > 1 && w.prefix_head < Tp))) return SKIPFFN_EINVAL;
     if (cap > 0 && n_seq > 0) {
@@ -1025,7 +1026,7 @@ int decode_call(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_
         if (suffix_k_seq < 0 || suffix_v_seq < 0 || bad_seg(suffix_len)) return SKIPFFN_EINVAL;
         if ((suffix_k_seq & 7) || (suffix_v_seq & 7) || suffix_k_seq >= ((int64_t)1 << 36) || suffix_v_seq >= ((int64_t)1 << 36)) return SKIPFFN_ESHAPE;
     }
-    if (weights != nullptr && (st = check_decode_weights(*weights, n_seq, Hkv, Tg, cap)) != SKIPFFN_OK) return st;
+    if (weights != nullptr && (st = check_decode_weights(*weights, n_seq, n_groups, Hkv, Tg, cap)) != SKIPFFN_OK) return st;
     if (n_seq == 0 && (weights == nullptr || weights->accumulate || Tg == 0)) return SKIPFFN_OK;
     const uintptr_t o0 = reinterpret_cast<uintptr_t>(out->data), o1 = o0 + (uintptr_t)heads_span(out, n_seq, Hq, D);
     auto meets = [&](const skipffn_heads* t, int64_t T, int64_t H, int64_t more) {
@@ -1059,6 +1060,7 @@ int decode_call(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_
     DecodeWeightsArgs w{};
     if (weights != nullptr) {
         a.most_shared = (int)std::min(weights->most_shared, n_seq);
+        a.prefix_ld = (int)decode_prefix_ld(Tg, n_groups); a.own_ld = (int)decode_own_ld(cap);
         a.prefix_scores = reinterpret_cast<float*>(ws + ws_of.prefix);
         a.own_scores = reinterpret_cast<float*>(ws + ws_of.own);
         a.lse = reinterpret_cast<float*>(ws + ws_of.lse);
@@ -1066,8 +1068,7 @@ int decode_call(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_
         if (decode_weights_workgroups(a) >= ((int64_t)1 << 24)) return SKIPFFN_ESHAPE;        // a launch has fewer than 2^32 threads
     }
     profile_mark_begin(KC_ATTN_DECODE, s);
-    hipError_t e = n_seq > 0 ? launch_attn_decode(a, s) : hipSuccess;
-    if (e == hipSuccess && weights != nullptr) e = launch_decode_weights(a, w, s);
+    hipError_t e = launch_attn_decode(a, weights != nullptr ? &w : nullptr, s);
     profile_mark_end(KC_ATTN_DECODE, s);
     return e == hipSuccess ? SKIPFFN_OK : hip_fail(e);
 }

@@ -18,12 +18,10 @@ namespace skipffn {
 
 constexpr int DEC_KEYS = 32;
 
-// SCORES: the products of every row and the keys it sees are left in the workspace as well, from which decode_weights.hip takes what the keys
-// receive once the rows' sums are known
-typedef float f32x4_dword __attribute__((ext_vector_type(4), aligned(4)));       // a group's rows begin anywhere
-
+// SCORES: the products of every row and the keys it sees are left in the workspace as well, from which what the keys receive is taken once the rows'
+// sums are known: here, where a workgroup has all rows that see its keys and all their keys (P.weigh), otherwise in decode_weights.hip
 template <int DP, bool SCORES>
-__global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_kernel(const AttnDecodeArgs P) {
+__global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_kernel(const AttnDecodeArgs P, const DecodeWeightsArgs W) {
     constexpr int ROWB = tile_row_bytes<DP>(), TILE = DEC_KEYS * ROWB;
     static_assert(2 * TILE >= DP * 32 * 4, "a wavefront's sums fit where its tiles were");
     __shared__ __align__(256) char smem[ATT_WAVES * 2 * TILE];
@@ -38,7 +36,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
     // What depends on the group is loaded with its bounds, and so are the lengths if a wavefront holds them all: one latency, not three.
     const bool few = P.n_seq <= 64;
     const int all_own = few && lane < P.n_seq && P.cap > 0 ? P.suffix_len[lane] : 0;
-    int s0 = 0, ns = 0, p0 = 0, p1 = 0, first_of_group = 0;
+    int s0 = 0, ns = 0, p0 = 0, p1 = 0, first_of_group = 0, score_at = 0;
     for (int i0 = 0, before = 0; i0 <= P.n_groups; i0 += 64) {
         const int i = i0 + lane;
         int lo = 0, hi = 0, pb = 0, pe = 0;
@@ -49,7 +47,9 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
             lo = P.n_groups > 0 ? min(max(P.group_off[P.n_groups], 0), P.n_seq) : 0;
             hi = P.n_seq;
         }
-        const int n = (hi - lo + members - 1) / members, incl = wave_inclusive_sum(n);
+        int n = (hi - lo + members - 1) / members;
+        if (SCORES && P.weigh && i < P.n_groups && n == 0) n = 1;      // a prefix that nobody reads
+        const int incl = wave_inclusive_sum(n);
         const uint64_t past = __ballot(b < before + incl);
         if (past != 0) {
             const int l = __builtin_ctzll(past);
@@ -57,12 +57,23 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
             ns = min(__builtin_amdgcn_readlane(hi, l) - s0, members);
             p0 = __builtin_amdgcn_readlane(pb, l);
             p1 = __builtin_amdgcn_readlane(pe, l);
-            if constexpr (SCORES) first_of_group = __builtin_amdgcn_readlane(lo, l);
+            if constexpr (SCORES) {
+                first_of_group = __builtin_amdgcn_readlane(lo, l);
+                score_at = decode_score_at(p0, i0 + l);
+            }
             break;
         }
         before += __builtin_amdgcn_readlane(incl, 63);
     }
-    if (ns == 0) return;
+    auto put_prefix = [&](int t, float v) {
+        float* w = W.prefix_w + kvh * W.prefix_head + p0 + t;
+        *w = W.accumulate ? *w + v : v;
+    };
+    if (ns == 0) {
+        if (SCORES && P.weigh)
+            for (int t = tid; t < p1 - p0; t += ATT_THREADS) put_prefix(t, 0.0f);
+        return;
+    }
     const int heads = min(g - hb * 32, 32), rows = ns * heads;
     const int prefix_tiles = (p1 - p0 + DEC_KEYS - 1) / DEC_KEYS;
     // lane i: own keys of sequence s0 + i and the tiles up to it
@@ -126,12 +137,20 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
         }
         const bool sees = next_of < 0 || member == next_of;
         seen |= sees;
-        float* score = nullptr;                          // of the row and the tile's first key
+        // products leave by stores that every lane makes, those without a row past the resource's end: under a branch the wait for the next tile, which is
+        // older, would have to be one for them too
+        uint32_t score_off = kOobOffset;
+        const float* scores = nullptr;
         if constexpr (SCORES) {
-            const int m = s0 - first_of_group + member;
-            if (r < rows && sees && next_of >= 0) score = P.own_scores + ((int64_t)(s0 + member) * P.Hq + head) * P.cap + next_k0;
-            else if (r < rows && sees && m < P.most_shared)
-                score = P.prefix_scores + ((int64_t)(kvh * P.most_shared + m) * g + hb * 32 + r % heads) * P.Tp + p0 + next_k0;
+            const int row = kvh * g + hb * 32;           // the first query head
+            if (next_of >= 0) {
+                scores = P.own_scores + ((int64_t)(s0 + next_of) * P.Hq + row) * P.own_ld + next_k0;
+                if (r < rows && sees) score_off = (uint32_t)((r % heads) * P.own_ld + 4 * h) * 4u;
+            } else {
+                const int m = s0 - first_of_group;
+                scores = P.prefix_scores + ((int64_t)(kvh * P.most_shared + m) * g + hb * 32) * P.prefix_ld + score_at + next_k0;
+                if (r < rows && m + member < P.most_shared) score_off = (uint32_t)((member * g + r % heads) * P.prefix_ld + 4 * h) * 4u;
+            }
         }
         lk.store(tk, lane);
         lv.store(tv, lane);
@@ -150,18 +169,11 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
             if (i + AHEAD < N) f[i % AHEAD] = frag_rows<DP>(rows_at, 0, i + AHEAD);
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (SCORES && score != nullptr) {
+        if constexpr (SCORES) {
+            const __amdgpu_buffer_rsrc_t to = make_rsrc(scores, 0x7fffffffu);
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-                const int k = 2 * i + 4 * h;
-                if (k + 4 <= keys) {
-                    *reinterpret_cast<f32x4_dword*>(score + k) = f32x4_dword{s[i], s[i + 1], s[i + 2], s[i + 3]};
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 3; ++e)
-                        if (k + e < keys) score[k + e] = s[i + e];
-                }
-            }
+            for (int i = 0; i < 16; i += 4)
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{s[i], s[i + 1], s[i + 2], s[i + 3]}), to, (int)(score_off + 8 * i), 0, 0);
         }
         if (keys < DEC_KEYS) {
 #pragma unroll
@@ -230,7 +242,8 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
     __syncthreads();
     constexpr int PER = DP / 8;                          // columns of a thread: eight threads a row
     const int jr = tid & 31, jd = (tid >> 5) * PER;
-    if (jr >= rows) return;
+    const bool mine_row = jr < rows;
+    if (!SCORES && !mine_row) return;
     float top = -INFINITY, w[ATT_WAVES], sum = 0.0f, o[PER];
 #pragma unroll
     for (int i = 0; i < ATT_WAVES; ++i) top = fmaxf(top, stat[i][0][jr]);
@@ -247,6 +260,7 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
     }
     const int seq = s0 + jr / heads, hq = kvh * g + hb * 32 + jr % heads;
     if (P.splits > 1) {
+        if (!mine_row) return;
         const int64_t at = ((int64_t)seq * P.Hq + hq) * P.splits + z;
         if (jd == 0) {
             P.stat[2 * at] = top;
@@ -256,14 +270,44 @@ __global__ __launch_bounds__(ATT_THREADS, DP <= 64 ? 3 : 2) void attn_decode_ker
         for (int j = 0; j < PER; j += 4) *reinterpret_cast<f32x4*>(P.part + at * attn_padded_columns(DP) + jd + j) = f32x4{o[j], o[j + 1], o[j + 2], o[j + 3]};
         return;
     }
-    if (SCORES && jd == 0) P.lse[(int64_t)hq * P.n_seq + seq] = top == -INFINITY ? INFINITY : fmaf(top, c, __builtin_amdgcn_logf(sum));
     const float inv = top == -INFINITY ? 0.0f : 1.0f / sum;   // a row that sees no key is zero
     bf16_t* out = P.out + (int64_t)seq * P.o_tok + hq * P.o_head;
 #pragma unroll
     for (int j = 0; j < PER; j += 4)
-        if (jd + j < P.D)
+        if ((!SCORES || mine_row) && jd + j < P.D)
             *reinterpret_cast<u32x2*>(out + jd + j) =
                 u32x2{pack_bf16x2(o[j] * inv, o[j + 1] * inv), pack_bf16x2(o[j + 2] * inv, o[j + 3] * inv)};
+    if constexpr (SCORES) {
+        const float lse = top == -INFINITY ? INFINITY : fmaf(top, c, __builtin_amdgcn_logf(sum));
+        if (!P.weigh) {
+            if (mine_row && jd == 0) P.lse[(int64_t)hq * P.n_seq + seq] = lse;
+            return;
+        }
+        __shared__ float row_lse[32];
+        if (jd == 0) row_lse[jr] = lse;
+        __syncthreads();                                 // and the wavefronts' products are in memory
+        // rows of a group past the first most_shared sequences, and they alone, are in other workgroups: they add nothing
+        const int shared_rows = s0 == first_of_group ? min(ns, P.most_shared) * g : 0;
+        const float* score = P.prefix_scores + (int64_t)kvh * P.most_shared * g * P.prefix_ld + score_at;
+        if (s0 == first_of_group)
+            for (int t = tid; t < p1 - p0; t += ATT_THREADS) {
+                float v = 0.0f;
+#pragma unroll 4
+                for (int i = 0; i < shared_rows; ++i) v += __builtin_amdgcn_exp2f(fmaf(score[(int64_t)i * P.prefix_ld + t], c, -row_lse[i]));
+                put_prefix(t, v);
+            }
+        for (int i = 0; i < ns; ++i) {
+            const int n = __builtin_amdgcn_readlane(own_keys, i);
+            const float* own = P.own_scores + ((int64_t)(s0 + i) * P.Hq + kvh * g) * P.own_ld;
+            for (int t = tid; t < n; t += ATT_THREADS) {
+                float v = 0.0f;
+#pragma unroll 4
+                for (int e = 0; e < g; ++e) v += __builtin_amdgcn_exp2f(fmaf(own[(int64_t)e * P.own_ld + t], c, -row_lse[i * g + e]));
+                float* w = W.own_w + (s0 + i) * W.own_seq + kvh * W.own_head + t;
+                *w = W.accumulate ? *w + v : v;
+            }
+        }
+    }
 }
 
 namespace {
@@ -287,23 +331,37 @@ int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv,
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min(want, most), ATTN_MAX_SPLITS));
 }
 
-hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s) {
-    const dim3 grid((uint32_t)decode_blocks(a.n_seq, a.n_groups, a.Hq, a.Hkv), (uint32_t)a.splits);
-    if (a.lse != nullptr) {
-        if (a.D <= 64) attn_decode_kernel<64, true><<<grid, ATT_THREADS, 0, s>>>(a);
-        else if (a.D <= 96) attn_decode_kernel<96, true><<<grid, ATT_THREADS, 0, s>>>(a);
-        else attn_decode_kernel<128, true><<<grid, ATT_THREADS, 0, s>>>(a);
-    } else if (a.D <= 64) attn_decode_kernel<64, false><<<grid, ATT_THREADS, 0, s>>>(a);
-    else if (a.D <= 96) attn_decode_kernel<96, false><<<grid, ATT_THREADS, 0, s>>>(a);
-    else attn_decode_kernel<128, false><<<grid, ATT_THREADS, 0, s>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
+// Whether a workgroup of the attention's kernel has every row that sees its keys, and all their keys
+static bool decode_weighs(const AttnDecodeArgs& a) {
+    const int g = a.Hq / a.Hkv;
+    return a.splits == 1 && g <= 32 && (a.Tp == 0 || a.most_shared <= 32 / g);
+}
+
+hipError_t launch_attn_decode(const AttnDecodeArgs& in, const DecodeWeightsArgs* w, hipStream_t s) {
+    AttnDecodeArgs a = in;
+    a.weigh = w != nullptr && a.n_seq > 0 && decode_weighs(a);
+    hipError_t e = hipSuccess;
+    if (a.n_seq > 0) {
+        // with weights an empty group has a workgroup too
+        const int g = a.Hq / a.Hkv, members = g >= 32 ? 1 : 32 / g;
+        const int64_t blocks = a.weigh ? ((int64_t)a.n_seq / members + a.n_groups + 1) * a.Hkv : decode_blocks(a.n_seq, a.n_groups, a.Hq, a.Hkv);
+        const dim3 grid((uint32_t)blocks, (uint32_t)a.splits);
+        const DecodeWeightsArgs to = w != nullptr ? *w : DecodeWeightsArgs{};
+        if (w != nullptr) {
+            if (a.D <= 64) attn_decode_kernel<64, true><<<grid, ATT_THREADS, 0, s>>>(a, to);
+            else if (a.D <= 96) attn_decode_kernel<96, true><<<grid, ATT_THREADS, 0, s>>>(a, to);
+            else attn_decode_kernel<128, true><<<grid, ATT_THREADS, 0, s>>>(a, to);
+        } else if (a.D <= 64) attn_decode_kernel<64, false><<<grid, ATT_THREADS, 0, s>>>(a, to);
+        else if (a.D <= 96) attn_decode_kernel<96, false><<<grid, ATT_THREADS, 0, s>>>(a, to);
+        else attn_decode_kernel<128, false><<<grid, ATT_THREADS, 0, s>>>(a, to);
+        e = hipGetLastError();
+    }
+    if (e != hipSuccess || a.weigh || (w == nullptr && a.splits == 1)) return e;
     AttnJoinArgs j{};
     j.T = a.n_seq; j.Hq = a.Hq; j.D = a.D; j.splits = a.splits; j.scale_log2 = a.scale_log2;
     j.part = a.part; j.stat = a.stat;
     j.out = a.out; j.o_tok = a.o_tok; j.o_head = a.o_head;
-    j.lse = a.lse;
-    return launch_attn_join(j, s);
+    return w != nullptr ? launch_decode_weights(a, *w, j, s) : launch_attn_join(j, s);
 }
 
 }  // namespace skipffn

@@ -216,10 +216,16 @@ struct AttnDecodeArgs {
     const bf16_t* sk; const bf16_t* sv; int sk_tok, sv_tok; int64_t sk_head, sv_head, sk_seq, sv_seq;
     const int32_t* prefix_seg; const int32_t* group_off; const int32_t* suffix_len;
     float* part; float* stat;                     // splits > 1: as in AttnJoinArgs
-    // With weights (lse not null): the products of a row and its keys, of the first most_shared sequences of a group [Hkv][most_shared][Hq / Hkv][Tp] and
-    // of own rows [n_seq][Hq][cap], and every row's log-sum-exp [Hq][n_seq], as AttnArgs::lse
-    int most_shared; float* prefix_scores; float* own_scores; float* lse;
+    // With weights: the products of a row and its keys, of the first most_shared sequences of a group [Hkv][most_shared][Hq / Hkv][prefix_ld], those of
+    // group i from decode_score_at on, and of own rows [n_seq][Hq][own_ld], and with splits 1 every row's log-sum-exp [Hq][n_seq], as AttnArgs::lse
+    int most_shared, weigh, prefix_ld, own_ld; float* prefix_scores; float* own_scores; float* lse;      // weigh: set by the launch
 };
+// Products leave in whole tiles of 32 keys: room for the last tile of every group, whose first product is 16-byte aligned.  Rows of p0 .. are at most
+// the next group's 36 - 3 before it
+constexpr __host__ __device__ int decode_score_at(int p0, int group) { return (p0 & ~3) + 36 * group; }
+constexpr int64_t decode_prefix_ld(int64_t Tp, int64_t n_groups) { return ((Tp + 3) & ~(int64_t)3) + 36 * (n_groups + 1); }
+constexpr int64_t decode_own_ld(int64_t cap) { return (cap + 31) & ~(int64_t)31; }
+constexpr int64_t DECODE_MAX_LD = (int64_t)1 << 24;              // 32 rows of it by 32-bit offsets
 // What the keys of single tokens receive, from what is left of launch_attn_decode: added to, or put into, the weights of prefix row t at
 // prefix_w[kv head * prefix_head + t], of own row t of a sequence at own_w[sequence * own_seq + kv head * own_head + t]
 struct DecodeWeightsArgs {
@@ -228,10 +234,11 @@ struct DecodeWeightsArgs {
     int accumulate;
 };
 int64_t decode_weights_workgroups(const AttnDecodeArgs& a);
-hipError_t launch_decode_weights(const AttnDecodeArgs& a, const DecodeWeightsArgs& w, hipStream_t s);
+// the second kernel of a call with weights: joins the parts' rows (j) and takes the weights
+hipError_t launch_decode_weights(const AttnDecodeArgs& a, const DecodeWeightsArgs& w, const AttnJoinArgs& j, hipStream_t s);
 // parts that the keys of a sequence are cut into
 int attn_decode_splits(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t Tp, int64_t cap, int ncu);
-hipError_t launch_attn_decode(const AttnDecodeArgs& a, hipStream_t s);
+hipError_t launch_attn_decode(const AttnDecodeArgs& a, const DecodeWeightsArgs* w, hipStream_t s);      // w null: no weights
 // parts that the keys of a query are cut into
 int attn_forward_splits(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int ncu);
 hipError_t launch_attn_forward(const AttnArgs& a, int ncu, hipStream_t s);
