@@ -381,7 +381,7 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
  *                   Not read or written where n_groups == 0 or Tp == 0
  *   suffix_weights  f32 [n_seq, Hkv, suffix_capacity] OUT by strides of sequence and head (no element shared); rows past suffix_len are
  *                   left as they were.  Not read or written where suffix_capacity == 0
- * Both are overwritten, or += with SKIPFFN_FLAG_DW_ACCUMULATE (the only flag).  `out` has the bits that skipffn_attn_decode gives; all else as
+ * Both are overwritten, or += with SKIPFFN_FLAG_DW_ACCUMULATE (the only flag); what they span does not meet.  `out` has the bits that skipffn_attn_decode gives; all else as
  * there.  A sequence whose row of `out` is NaN for its scores makes NaN of the weights of the rows it sees.  Deterministic.
  * Tp + 36 n_groups and suffix_capacity < 2^24 - 64.
  * workspace: at least skipffn_attn_decode_weights_workspace_bytes(...): about 4 Hq (most_shared Tp + n_seq suffix_capacity) and what decode takes. */
@@ -407,7 +407,7 @@ int skipffn_attn_decode_weights(int64_t n_seq, int64_t n_groups, int64_t Hq, int
  *             SKIPFFN_FLAG_DW_ACCUMULATE (the only flag).  Keys that no query sees get 0; keys of no sequence are left as they were
  *   workspace at least skipffn_attn_key_weights_workspace_bytes(...) bytes (NULL where that is 0)
  * A query whose scores are not finite where it sees (its log-sum-exp is NaN or minus infinity) makes NaN of the keys it
- * sees, and of no others.  fp32 throughout.  Deterministic. */
+ * sees, and of no others.  fp32 throughout.  weights meets neither q nor k.  Deterministic. */
 size_t skipffn_attn_key_weights_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int64_t last);
 int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, const skipffn_heads* q,
                              const skipffn_heads* k, const int32_t* seg_q, const int32_t* seg_k, int causal, float scale, const void* saved,

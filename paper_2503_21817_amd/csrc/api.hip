@@ -140,7 +140,7 @@ const char* skipffn_status_string(int status) {
         case SKIPFFN_OK: return "ok";
         case SKIPFFN_EINVAL: return "invalid argument (null or misaligned pointer, negative size, R > T)";
         case SKIPFFN_ESHAPE: return "unsupported shape (C, I must be multiples of 8; tensors below 2 GiB; skipffn_compact_static: T above skipffn_compact_static_max_tokens(); "
-                                      "attention: columns a head, strides, heads or tokens outside their limits)";
+                                      "attention and what is around it: columns a head, strides, heads or tokens outside their limits)";
         case SKIPFFN_EWORKSPACE: return "workspace too small";
         case SKIPFFN_EHIP: return "HIP runtime error";
         case SKIPFFN_EUNSUPPORTED: return "unsupported flag";
@@ -150,7 +150,7 @@ const char* skipffn_status_string(int status) {
 }
 
 int skipffn_last_hip_error(void) { return g_last_hip; }
-int skipffn_version(void) { return 20200; }   // 2.2.0: attention
+int skipffn_version(void) { return 20300; }   // 2.3.0: norm and rotation of queries and keys, what keys receive, eviction
 
 int skipffn_profile_begin(void) {
     std::lock_guard<std::mutex> lk(g_prof_mu);
@@ -853,6 +853,11 @@ bool heads_meet(const skipffn_heads* a, int64_t Ta, int64_t Ha, const skipffn_he
     const uintptr_t x = reinterpret_cast<uintptr_t>(a->data), y = reinterpret_cast<uintptr_t>(b->data);
     return x < y + (uintptr_t)heads_span(b, Tb, Hb, D) && y < x + (uintptr_t)heads_span(a, Ta, Ha, D);
 }
+bool ranges_meet(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+    return a_bytes > 0 && b_bytes > 0 && x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
+}
+bool bad4(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 bool bad_seg(const int32_t* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 const bf16_t* in(const skipffn_heads* t) { return static_cast<const bf16_t*>(t->data); }
 bf16_t* to(const skipffn_heads* t) { return static_cast<bf16_t*>(t->data); }
@@ -998,13 +1003,14 @@ int check_decode_weights(const DecodeWeights& w, int64_t n_seq, int64_t n_groups
     if (w.most_shared < 0 || w.prefix_head < 0 || w.own_seq < 0 || w.own_head < 0) return SKIPFFN_EINVAL;
     if (w.prefix_head >= most || w.own_seq >= most || w.own_head >= most) return SKIPFFN_ESHAPE;
     if (decode_prefix_ld(Tp, n_groups) >= DECODE_MAX_LD || decode_own_ld(cap) >= DECODE_MAX_LD) return SKIPFFN_ESHAPE;
-    auto bad = [](const float* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; };
-    if (Tp > 0 && (w.most_shared == 0 || bad(w.prefix) || (Hkv > 1 && w.prefix_head < Tp))) return SKIPFFN_EINVAL;
+    if (Tp > 0 && (w.most_shared == 0 || bad4(w.prefix) || (Hkv > 1 && w.prefix_head < Tp))) return SKIPFFN_EINVAL;
     if (cap > 0 && n_seq > 0) {
         // rows are apart: heads inside a sequence's range, or sequences inside a head's
         const bool heads_in = (Hkv == 1 || w.own_head >= cap) && (n_seq == 1 || w.own_seq >= (Hkv - 1) * w.own_head + cap);
         const bool seqs_in = (n_seq == 1 || w.own_seq >= cap) && (Hkv == 1 || w.own_head >= (n_seq - 1) * w.own_seq + cap);
-        if (bad(w.own) || (!heads_in && !seqs_in)) return SKIPFFN_EINVAL;
+        if (bad4(w.own) || (!heads_in && !seqs_in)) return SKIPFFN_EINVAL;
+        if (Tp > 0 && ranges_meet(w.prefix, ((Hkv - 1) * w.prefix_head + Tp) * 4, w.own, ((n_seq - 1) * w.own_seq + (Hkv - 1) * w.own_head + cap) * 4))
+            return SKIPFFN_EINVAL;
     }
     return SKIPFFN_OK;
 }
@@ -1132,8 +1138,10 @@ int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, 
     if ((seg_k == nullptr && Tq != Tk) || weights_head < 0 || (Hkv > 1 && weights_head < Tk)) return SKIPFFN_EINVAL;
     if (weights_head >= ((int64_t)1 << 44)) return SKIPFFN_ESHAPE;
     if (n_seq == 0 || Tk == 0) return SKIPFFN_OK;
-    if (bad_seg(seg_q) || (seg_k != nullptr && bad_seg(seg_k)) || (Tq > 0 && last != 0 && bad_ptr(saved)) || weights == nullptr ||
-        (reinterpret_cast<uintptr_t>(weights) & 3u))
+    if (bad_seg(seg_q) || (seg_k != nullptr && bad_seg(seg_k)) || (Tq > 0 && last != 0 && bad_ptr(saved)) || bad4(weights))
+        return SKIPFFN_EINVAL;
+    const int64_t w_bytes = ((Hkv - 1) * weights_head + Tk) * 4;
+    if (ranges_meet(weights, w_bytes, q->data, heads_span(q, Tq, Hq, D)) || ranges_meet(weights, w_bytes, k->data, heads_span(k, Tk, Hkv, D)))
         return SKIPFFN_EINVAL;
     const size_t need = key_weights_bytes(plan, Tk, Hkv);
     if (need > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < need)) return SKIPFFN_EWORKSPACE;
@@ -1299,11 +1307,6 @@ bool apart(int64_t inner, Dim a, Dim b, Dim c) {
     }
     return true;
 }
-bool ranges_meet(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
-    const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-    return x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
-}
-bool bad4(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 }  // namespace
 
 int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T_out, int packed, const skipffn_heads* k, const skipffn_heads* v,

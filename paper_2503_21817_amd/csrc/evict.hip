@@ -10,7 +10,9 @@
 
 namespace skipffn {
 
-// rows [lo, hi) of sequence s, how many of them stay, and the first of these among the rows that are kept
+constexpr int EVICT_SCAN = 64;                           // packed sequences whose offsets every workgroup finds by itself
+
+// rows lo .. of sequence s and how many, how many of them stay, and the first of these among the rows that are kept
 struct EvictSeq { int lo, n, keep, to; };
 __device__ __forceinline__ int evict_kept(const EvictArgs& P, int s, int n) {
     return min(max(P.n_keep_dev != nullptr ? P.n_keep_dev[s] : P.n_keep, 0), n);
@@ -25,18 +27,55 @@ __device__ __forceinline__ EvictSeq evict_seq(const EvictArgs& P, int s) {
     int hi;
     seg_bounds(P.seg, s, P.T, q.lo, hi);
     q.n = hi - q.lo;
-    const int lane = threadIdx.x & 63;
-    int64_t before = 0;
-    for (int i = lane; i < s; i += 64) {
-        int a, b;
-        seg_bounds(P.seg, i, P.T, a, b);
-        before += evict_kept(P, i, b - a);
+    if (P.n_seq > EVICT_SCAN) {                          // evict_offsets_kernel has been there
+        q.to = P.seg_out[s];
+        q.keep = P.seg_out[s + 1] - q.to;
+        return q;
     }
+    static_assert(EVICT_SCAN == 64, "a lane a sequence");
+    const int lane = threadIdx.x & 63;
+    int a = 0, b = 0;
+    if (lane < P.n_seq) seg_bounds(P.seg, lane, P.T, a, b);
+    const int mine = lane < P.n_seq ? evict_kept(P, lane, b - a) : 0;
+    int64_t before = lane < s ? mine : 0;
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) before += __shfl_xor(before, off, 64);
     q.to = (int)(before < P.T_out ? before : P.T_out);
     q.keep = min(evict_kept(P, s, q.n), P.T_out - q.to);
     return q;
+}
+
+// More than 64 packed sequences: where the kept rows of each begin, by one workgroup
+__global__ __launch_bounds__(1024) void evict_offsets_kernel(const EvictArgs P) {
+    __shared__ int64_t waves[16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int64_t carry = 0;
+    if (tid == 0) P.seg_out[0] = 0;
+    for (int s0 = 0; s0 < P.n_seq; s0 += 1024) {
+        int64_t v = 0;
+        if (s0 + tid < P.n_seq) {
+            int a, b;
+            seg_bounds(P.seg, s0 + tid, P.T, a, b);
+            v = evict_kept(P, s0 + tid, b - a);
+        }
+#pragma unroll
+        for (int off = 1; off < 64; off *= 2) {
+            const int64_t u = __shfl_up(v, off, 64);
+            v += lane >= off ? u : 0;
+        }
+        __syncthreads();                                 // the last round's sums have been read
+        if (lane == 63) waves[wave] = v;
+        __syncthreads();
+        int64_t all = 0;
+        v += carry;
+#pragma unroll
+        for (int w = 0; w < 16; ++w) {
+            v += w < wave ? waves[w] : 0;
+            all += waves[w];
+        }
+        if (s0 + tid < P.n_seq) P.seg_out[s0 + tid + 1] = (int)(v < P.T_out ? v : P.T_out);
+        carry += all;
+    }
 }
 
 // The cut between what stays and what goes: the k smallest of a list's keys (rank_key) are those below `below`, and the first `ties` of those equal to it.
@@ -158,7 +197,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictArgs P
     const int s = (int)blockIdx.x / P.Hkv, head = (int)blockIdx.x % P.Hkv, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const EvictSeq q = evict_seq(P, s);
-    if (head == 0 && tid == 0) {
+    if (head == 0 && tid == 0 && (!P.packed || P.n_seq <= EVICT_SCAN)) {
         if (P.packed) {
             P.seg_out[s + 1] = q.to + q.keep;
             if (s == 0) P.seg_out[0] = 0;
@@ -340,6 +379,7 @@ int64_t evict_workgroups(const EvictArgs& a) {
 
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
     const uint32_t lists = (uint32_t)(a.n_seq * a.Hkv);
+    if (a.packed && a.n_seq > EVICT_SCAN) evict_offsets_kernel<<<1, 1024, 0, s>>>(a);
     if (a.T <= EVICT_SHORT) evict_select_kernel<EVICT_SHORT / 4, false><<<lists, EVICT_SHORT / 4, 0, s>>>(a);
     else evict_select_kernel<EVICT_LONG_THREADS, true><<<lists, EVICT_LONG_THREADS, 0, s>>>(a);
     const hipError_t e = hipGetLastError();

@@ -154,3 +154,22 @@ def test_captured_and_replayed():
         first, second = w.pw[:, :8001], want[0][:, :8001]
         assert torch.equal(first, second) and torch.equal(d.out, want[2]), turn
         assert all(torch.equal(w.sw[i, :, :n], want[1][i, :, :n]) for i, n in enumerate(d.own)), turn
+
+
+def test_products_past_32_bits():
+    """16 sequences on one prefix of 2^20 rows: 2^29 products of a head of the cache, 2^31 in all."""
+    n, Hq, Hkv, D, Tp = 16, 128, 2, 8, 2 ** 20
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda").to(torch.bfloat16)
+    q, k, v = rand(n, Hq, D), rand(Tp, Hkv, D), rand(Tp, Hkv, D)
+    out, pw = torch.empty_like(q), torch.zeros(Hkv, Tp, device="cuda")
+    ws = torch.empty(B.skipffn_attn_decode_weights_workspace_bytes(n, 1, Hq, Hkv, D, Tp, 0, n), dtype=torch.uint8, device="cuda")
+    assert ws.numel() > 2 ** 33
+    B.skipffn_attn_decode_weights(q, k, v, ints([0, Tp]), ints([0, n]), None, None, None, out, pw, None, most_shared=n, scale=0.4, workspace=ws)
+    torch.cuda.synchronize()
+    for h in range(Hkv):
+        want = torch.zeros(Tp, dtype=torch.float64, device="cuda")
+        for i in range(n):
+            x = (q[i, h * 64:(h + 1) * 64].double() @ k[:, h].double().T) * 0.4
+            want += torch.softmax(x, -1).sum(0)
+        assert_within(f64_of(pw[h]), want.cpu().numpy(), 2 * F * want.cpu().numpy(), f"head {h}")

@@ -150,11 +150,13 @@ def test_weights_need_not_be_kept():
     e.check(100, 1, 5, weights_out=False)
 
 
-def test_many_sequences():
-    rows = [i * 13 % 200 for i in range(150)]
-    e = Evict(rows, 2, 16, True, sum(min(n, 70) for n in rows))
-    e.run(70, 1, 30)
-    e.check(70, 1, 30)
+@pytest.mark.parametrize("n", [64, 65, 150, 1100])
+def test_many_sequences(n):
+    rows = [i * 13 % 200 for i in range(n)] if n < 1000 else [i % 7 for i in range(n)]
+    budget = 70 if n < 1000 else 4
+    e = Evict(rows, 2, 16, True, sum(min(n, budget) for n in rows) - (n == 150))
+    e.run(budget, 1, 30 if n < 1000 else 2)
+    e.check(budget, 1, 30 if n < 1000 else 2)
 
 
 def test_offsets_that_are_no_offsets_read_and_write_inside():

@@ -175,3 +175,18 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(p.w, want), turn
+
+
+def test_offsets_past_32_bits():
+    """Queries and keys of 2^20 elements a token, 2^32 in all, and heads of weights 2^31 elements apart."""
+    T, H, K, D = 4200, 2, 2, 8
+    big = torch.zeros(T * 2 ** 20, dtype=torch.bfloat16, device="cuda").view(T, 2 ** 20)
+    p = Prompt((4200 - BEHIND,), (4200 - BEHIND,), H, K, D)
+    q, k = big[:, -H * D:].view(T, H, D), big[:, :K * D].view(T, K, D)
+    q.copy_(p.q)
+    k.copy_(p.k)
+    p.q, p.k = q, k
+    p.w = torch.full((2 ** 31 + T,), 7.0, device="cuda").as_strided((K, T), (2 ** 31, 1))
+    p.attend(True, 0.35)
+    p.receive(True, 0.35)
+    p.check(True, 0.35)
