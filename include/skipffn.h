@@ -383,7 +383,7 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
  *                   left as they were.  Not read or written where suffix_capacity == 0
  * Both are overwritten, or += with SKIPFFN_FLAG_DW_ACCUMULATE (the only flag); what they span does not meet.  `out` has the bits that skipffn_attn_decode gives; all else as
  * there.  A sequence whose row of `out` is NaN for its scores makes NaN of the weights of the rows it sees.  Deterministic.
- * Tp + 36 n_groups and suffix_capacity < 2^24 - 64.
+ * Tp + 36 n_groups and suffix_capacity < 2^24 - 64, (Tp / 64 + n_groups + n_seq (suffix_capacity / 256 + 1)) Hkv + n_seq Hq / 4 < 2^24 - 1.
  * workspace: at least skipffn_attn_decode_weights_workspace_bytes(...): about 4 Hq (most_shared Tp + n_seq suffix_capacity) and what decode takes. */
 size_t skipffn_attn_decode_weights_workspace_bytes(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp,
                                                    int64_t suffix_capacity, int64_t most_shared);
@@ -407,7 +407,8 @@ int skipffn_attn_decode_weights(int64_t n_seq, int64_t n_groups, int64_t Hq, int
  *             SKIPFFN_FLAG_DW_ACCUMULATE (the only flag).  Keys that no query sees get 0; keys of no sequence are left as they were
  *   workspace at least skipffn_attn_key_weights_workspace_bytes(...) bytes (NULL where that is 0)
  * A query whose scores are not finite where it sees (its log-sum-exp is NaN or minus infinity) makes NaN of the keys it
- * sees, and of no others.  fp32 throughout.  weights meets neither q nor k.  Deterministic. */
+ * sees, and of no others.  fp32 throughout.  weights meets neither q nor k.  Shapes as skipffn_attn_forward, and
+ * (Tk / 256 + n_seq) Hkv < 2^24.  Deterministic. */
 size_t skipffn_attn_key_weights_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int64_t last);
 int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, const skipffn_heads* q,
                              const skipffn_heads* k, const int32_t* seg_q, const int32_t* seg_k, int causal, float scale, const void* saved,
@@ -430,7 +431,8 @@ int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, 
  *   keep            the kept rows' numbers, counted from their sequence's first row
  * Rows past a sequence's are left as they were, in every output.  Strides in elements; those of sequences are not read where packed.
  * What k_out and v_out span meets neither k nor v, weights_out not weights (kept rows would race); no two elements of an output are one.
- * Rows are copied bit for bit.  T, T_out < 2^30, D and strides of k, v as in skipffn_attn_forward.  Deterministic. */
+ * Rows are copied bit for bit.  T, T_out < 2^30, n_seq Hkv < 2^22, workgroups of 16 kept rows of a head fewer than 2^24; D and strides of k, v as
+ * in skipffn_attn_forward.  Deterministic. */
 int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T_out, int packed, const skipffn_heads* k, const skipffn_heads* v,
                      int64_t k_seq, int64_t v_seq, const float* weights, int64_t weights_head, int64_t weights_seq, const int32_t* seg,
                      int64_t n_keep, const int32_t* n_keep_dev, int64_t first, int64_t recent, const skipffn_heads* k_out,
@@ -455,7 +457,9 @@ int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T
  * An output may be its own input (same memory and strides, row == NULL); training with a norm needs the inputs again, so not then.
  * Otherwise it shares no element with an input or another output: what they span does not meet, or they are column ranges of
  * rows of one stride.  v is copied bit for bit.
- * D % 8 == 0, 8 <= D <= 128, rot % 8 == 0, 0 <= rot <= D, n_axes <= 4, T < 2^30.  eps >= 0, finite. */
+ * Own rows of skipffn_attn_decode, [n_seq, capacity, Hkv, D] or [Hkv, n_seq, capacity, D], are a cache of n_seq * capacity rows: a new
+ * token's is sequence * capacity + own length.
+ * D % 8 == 0, 8 <= D <= 128, rot % 8 == 0, 0 <= rot <= D, n_axes <= 4, T (Hq + 2 Hkv) < 2^27 (the forward call).  eps >= 0, finite. */
 int skipffn_qk_rope_forward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, int64_t n_axes, const skipffn_heads* q,
                             const skipffn_heads* k, const skipffn_heads* v, const int32_t* pos, const float* inv_freq, const uint8_t* axis,
                             const void* gain_q, const void* gain_k, float eps, const int32_t* row, int64_t rows_out,

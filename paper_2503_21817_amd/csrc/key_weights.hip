@@ -6,6 +6,10 @@
 // keys: its log-sum-exp is one number, and the sums of its keys stay in 16 registers until the end, where the lanes are joined.  No weight is
 // rounded below fp32 and every sum has one owner and a fixed order.  Where keys are few for the chip, or a causal prompt's pieces uneven, the
 // queries are cut into parts whose sums a second kernel adds.
+//
+// 32 / 8 heads of 128, us: 1 x 16384 tokens 1065-1080 (1018-1032 TFLOP/s of what the mask leaves, a library product of 8192^3 1178): matrix cores busy 48 % of the
+// time, the vector unit 60 % (three instructions a score), at 2.0-2.1 GHz.  16 x up to 616 tokens 33, of which 4.3 the second kernel: latency, 1.2 a step of 64
+// queries.  32768 keys by 64 queries 29-32 (67 MB of keys): loads and steps of a workgroup one after the other.
 #include <algorithm>
 #include <cmath>
 

@@ -152,7 +152,9 @@ __host__ __device__ inline int rope_heads_at_once(int lph, int heads) {
     return n;
 }
 
-// A wavefront has U times as many heads of its tokens as it works on at once; all of their loads are asked for first
+// A wavefront has U times as many heads of its tokens as it works on at once; all of their loads are asked for first.
+// Bound by bytes: 11776 tokens of 32 / 8 heads of 128 with their values into a cache 59.5-60.5 us (290 MB, 4.8 TB/s; a large copy 4.9), 9856 with the norm 49.8
+// (202 MB).  With loads under branches, which wait for one another, 68; with sincospif instead of the two instructions 74.
 template <int V, int LPH, int U, bool PAIRS, bool NORM>
 __global__ __launch_bounds__(ROPE_THREADS) void rope_fwd_kernel(const RopeArgs P, const int chunks) {
     typedef typename RopeVec<V>::type Vec;
@@ -221,8 +223,9 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_fwd_kernel(const RopeArgs P
 
 // A workgroup has either heads of q or heads of k and goes on through the tokens; the next heads' loads are under way while these are worked on.  With gain
 // gradients every lane keeps the sums of its columns, joined over the workgroup at the end: part [workgroup][D], q's first.
-// Measured, 9856 tokens of 32 / 8 heads of 128 with both gains, forward and backward, us: 113.7, of which this kernel about 62 (303 MB, 4.9 TB/s); without
-// the loads asked for early, heads of q and k in one workgroup and gains read where they are used 225; two heads at a time 144 (197 registers).
+// Bound by bytes: 9856 tokens of 32 / 8 heads of 128 with both gains 58.9 us (303 MB, 5.1 TB/s), the gains' second kernel 4.8; forward and backward 111.  Without
+// the loads asked for early, heads of q and k in one workgroup and gains read where they are used 225; two heads at a time 144 (197 registers); four
+// workgroups a compute unit, for which there are no registers, 120.
 template <int V, int LPH, bool PAIRS, bool NORM, bool GAINS>
 __global__ __launch_bounds__(ROPE_THREADS) void rope_bwd_kernel(const RopeArgs P, const int wgs_q, float* part) {
     typedef typename RopeVec<V>::type Vec;
@@ -319,12 +322,13 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_bwd_kernel(const RopeArgs P
         for (int j = 0; j < 2 * V; j += 4) lds[j / 4][threadIdx.x] = f32x4{sum[j], sum[j + 1], sum[j + 2], sum[j + 3]};
         __syncthreads();
         for (int e = threadIdx.x; e < LPH * 2 * V; e += ROPE_THREADS) {
-            const int l = e / (2 * V), j = e % (2 * V), s = j / V;
+            const int l = e / (2 * V), j = e % (2 * V);
             const RopeLane<V, LPH, PAIRS> M(l, P.D, P.rot);
-            if (!M.has[s]) continue;
+            const int col = j < V ? M.col[0] : M.col[1];
+            if (col >= P.D) continue;
             float v = 0.0f;
             for (int i = l; i < ROPE_THREADS; i += LPH) v += lds[j / 4][i][j % 4];
-            part[(int64_t)blockIdx.x * P.D + M.col[s] + j % V] = v;
+            part[(int64_t)blockIdx.x * P.D + col + j % V] = v;
         }
     }
 }
@@ -361,7 +365,7 @@ constexpr int ROPE_BWD_PER_CU = 3;                       // workgroups, by its r
 }  // namespace
 
 // Heads of a wavefront one after the other: one where that many wavefronts find room on the chip at once, otherwise three (us, 32 / 8 heads of 128: 64 tokens 5.0 /
-// 6.5, 11776 tokens into a cache 99 / 68; six 8.6 / 67)
+// 6.5, 11776 tokens into a cache 99 / 71; six 8.6 / 67; before loads without branches)
 template <class Launch>
 static void rope_forward_variant(const RopeArgs& a, int ncu, Launch&& go) {
     rope_variant(a, [&](auto v, auto lph) {
