@@ -13,7 +13,8 @@
 
 namespace skipffn {
 
-constexpr int EVICT_SCAN = 64;                           // packed sequences whose offsets every workgroup finds by itself
+// packed sequences whose offsets every workgroup finds by itself, a lane each; more take a kernel of their own (60 sequences 30.7 us so, 32.7 with it)
+constexpr int EVICT_SCAN = 64;
 
 // rows lo .. of sequence s and how many, how many of them stay, and the first of these among the rows that are kept
 struct EvictSeq { int lo, n, keep, to; };
@@ -338,6 +339,8 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictArgs P
     });
 }
 
+// Lists of up to 2048 rows take 512 threads, longer ones 1024 (us: 512 lists of up to 1000 rows 58.4 / 63.7, 512 of 300 19.3 / 23.9; 512 of 4000 by 1024 threads with the
+// list in registers 122.9, read again 123.1)
 constexpr int EVICT_ROWS = 16, EVICT_THREADS = 256, EVICT_SHORT = 2048, EVICT_LONG_THREADS = 1024;
 
 __global__ __launch_bounds__(EVICT_THREADS) void evict_gather_kernel(const EvictArgs P, const int chunks) {

@@ -21,6 +21,8 @@ def some_weights(rng, n, kind):
         return rng.integers(0, 3, n).astype(np.float32)
     if kind == "one value":
         return np.full(n, 0.25, dtype=np.float32)
+    if kind == "tiny":                                   # below the smallest normal number, zeros of both signs among them
+        return (rng.integers(-40, 40, n) * 1e-45).astype(np.float32) * np.where(rng.random(n) < 0.5, 1, -1).astype(np.float32)
     x = rng.standard_normal(n).astype(np.float32)        # "any": signs, infinities, NaN, zeros of both signs
     for v in (np.nan, np.inf, -np.inf, 0.0, -0.0):
         x[rng.random(n) < 0.1] = v
@@ -92,7 +94,7 @@ ROWS = [(1,), (40, 0, 300, 7), (1000, 1024, 1025, 3), (2049, 4096), (5000, 200)]
 @pytest.mark.parametrize("rows", ROWS, ids=str)
 @pytest.mark.parametrize("Hkv,D", [(1, 128), (3, 64), (2, 72), (8, 8)])
 @pytest.mark.parametrize("packed", [True, False], ids=["packed", "own"])
-@pytest.mark.parametrize("kind", ["sums", "few values", "one value", "any"])
+@pytest.mark.parametrize("kind", ["sums", "few values", "one value", "any", "tiny"])
 def test_rows_that_received_most_stay(rows, Hkv, D, packed, kind):
     print(f"evict {rows} heads {Hkv} D={D} packed={packed} {kind}", flush=True)
     for n_keep, first, recent in ((100, 4, 30), (1, 0, 0), (max(rows) // 2, 0, 0), (33, 50, 60)):
