@@ -106,7 +106,8 @@ __global__ __launch_bounds__(DW_THREADS) void decode_weights_kernel(const AttnDe
 }
 
 namespace {
-// by the products that a cache row has (one wavefront / four a row, whole calls, us): 4 of 80000 rows 77 / 89, 32 of 32000 60 / 64, 128 of 8800 36.8 / 32.7
+// By the products that a shared row of the cache has (shared rows; us of whole calls, one wavefront a row / four): 4 (71723 rows) 77.2 / 89.3, 8 (64000) 73.1 / 82.0,
+// 16 (32000) 46.0 / 49.8, 32 (32000) 60.0 / 63.8, 128 (3053) 36.8 / 32.7; between 32 and 128 nothing was timed
 int weight_ways(const AttnDecodeArgs& a) { return (int64_t)a.most_shared * (a.Hq / a.Hkv) > 64 ? 4 : 1; }
 int64_t prefix_chunks_of(const AttnDecodeArgs& a) {
     const int64_t ch = DW_THREADS / weight_ways(a);

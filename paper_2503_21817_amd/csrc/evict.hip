@@ -13,7 +13,7 @@
 
 namespace skipffn {
 
-// packed sequences whose offsets every workgroup finds by itself, a lane each; more take a kernel of their own (60 sequences 30.7 us so, 32.7 with it)
+// packed sequences whose offsets every workgroup finds by itself, a lane each; more take a kernel of their own (60 sequences of 616 rows 30.7 us so, 32.7 with it)
 constexpr int EVICT_SCAN = 64;
 
 // rows lo .. of sequence s and how many, how many of them stay, and the first of these among the rows that are kept
@@ -339,8 +339,8 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(const EvictArgs P
     });
 }
 
-// Lists of up to 2048 rows take 512 threads, longer ones 1024 (us: 512 lists of up to 1000 rows 58.4 / 63.7, 512 of 300 19.3 / 23.9; 512 of 4000 by 1024 threads with the
-// list in registers 122.9, read again 123.1)
+// Where no list can have more than 2048 rows a form of 512 threads that holds four a thread, otherwise one of 1024 that reads lists of more than 4096 again (us of whole calls, 512
+// threads / the other form: 512 lists of 300 rows 19.3 / 23.9, of up to 1000 58.4 / 63.7).  512 lists of 4000 take 123.1, by a form of 1024 threads that only holds them 122.9: there is none
 constexpr int EVICT_ROWS = 16, EVICT_THREADS = 256, EVICT_SHORT = 2048, EVICT_LONG_THREADS = 1024;
 
 __global__ __launch_bounds__(EVICT_THREADS) void evict_gather_kernel(const EvictArgs P, const int chunks) {

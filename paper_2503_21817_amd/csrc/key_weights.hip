@@ -171,8 +171,9 @@ __global__ __launch_bounds__(KW_KEYS) void key_weights_join_kernel(const AttnArg
 }
 
 // Parts that the queries are cut into.  A piece takes 1.2 us a step and 6 us to begin and end; the last ones leave the chip to themselves, so pieces are made
-// shorter until what that saves goes into beginning more of them; the second kernel takes about 4 us.  Us of whole calls, one part / as planned: 16 x up to 616 tokens 60.6 /
-// 33, 1 x 616 40 / 16.5; 1 x 2944 (2 parts / 14) 57 / 52-54, 1 x 16384 (2 / 14) 1116 / 1065-1080
+// shorter until what that saves goes into beginning more of them; the second kernel takes about 4 us..  Us of whole
+// calls (parts), as planned first: 16 sequences of up to 616, 5682 tokens together, 34.6 (3), 60.8 (1), 40.1 (6); 8 x 616 37.0 (4), 67.3 (1), 45.3 (2), 45.0 (9); 1 x 616 16.6 (10, all there
+// are), 65.4 (1), 19.4 (7); 1 x 2944 56.7 (14), 257 (1), 59.5 (7), 69.7 (28); 4 x 4096 324 (7), 397 (1), 316 (3), 363 (14); 1 x 16384 1074 (14), 1501 (1), 1059 (7), 1134 (28)
 KeyWeightsPlan key_weights_plan(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t last, int ncu) {
     KeyWeightsPlan p{};
     p.blocks = (Tk / KW_KEYS + n_seq) * Hkv;
