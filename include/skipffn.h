@@ -407,7 +407,7 @@ int skipffn_attn_decode_weights(int64_t n_seq, int64_t n_groups, int64_t Hq, int
  *             SKIPFFN_FLAG_DW_ACCUMULATE (the only flag).  Keys that no query sees get 0; keys of no sequence are left as they were
  *   workspace at least skipffn_attn_key_weights_workspace_bytes(...) bytes (NULL where that is 0)
  * A query whose scores are not finite where it sees (its log-sum-exp is NaN or minus infinity) makes NaN of the keys it
- * sees, and of no others.  fp32 throughout.  weights meets neither q nor k.  Shapes as skipffn_attn_forward, and
+ * sees, and of no others.  fp32 throughout.  weights meets none of q, k and saved.  Shapes as skipffn_attn_forward, and
  * (Tk / 256 + n_seq) Hkv < 2^24.  Deterministic. */
 size_t skipffn_attn_key_weights_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int64_t last);
 int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, const skipffn_heads* q,
@@ -430,7 +430,8 @@ int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, 
  *   weights_out     the kept rows' weights, or NULL
  *   keep            the kept rows' numbers, counted from their sequence's first row
  * Rows past a sequence's are left as they were, in every output.  Strides in elements; those of sequences are not read where packed.
- * What k_out and v_out span meets neither k nor v, weights_out not weights (kept rows would race); no two elements of an output are one.
+ * What k_out and v_out span meets neither k nor v, and keep, weights_out and seg_out meet neither weights, seg nor n_keep_dev (kept rows, and heads that
+ * still read, would race); no two elements of the outputs are one.
  * Rows are copied bit for bit.  T, T_out < 2^30, n_seq Hkv < 2^22, workgroups of 16 kept rows of a head fewer than 2^24; D and strides of k, v as
  * in skipffn_attn_forward.  Deterministic. */
 int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T_out, int packed, const skipffn_heads* k, const skipffn_heads* v,

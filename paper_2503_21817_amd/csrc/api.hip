@@ -1141,7 +1141,8 @@ int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, 
     if (bad_seg(seg_q) || (seg_k != nullptr && bad_seg(seg_k)) || (Tq > 0 && last != 0 && bad_ptr(saved)) || bad4(weights))
         return SKIPFFN_EINVAL;
     const int64_t w_bytes = ((Hkv - 1) * weights_head + Tk) * 4;
-    if (ranges_meet(weights, w_bytes, q->data, heads_span(q, Tq, Hq, D)) || ranges_meet(weights, w_bytes, k->data, heads_span(k, Tk, Hkv, D)))
+    if (ranges_meet(weights, w_bytes, q->data, heads_span(q, Tq, Hq, D)) || ranges_meet(weights, w_bytes, k->data, heads_span(k, Tk, Hkv, D)) ||
+        (last != 0 && ranges_meet(weights, w_bytes, saved, Hq * Tq * 4)))
         return SKIPFFN_EINVAL;
     const size_t need = key_weights_bytes(plan, Tk, Hkv);
     if (need > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < need)) return SKIPFFN_EWORKSPACE;
@@ -1345,11 +1346,23 @@ int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T
                                 heads_span(ins[i], T, Hkv, D) + (seqs - 1) * strides[i] * 2))
                     return SKIPFFN_EINVAL;
         }
-        auto span = [&](int64_t head, int64_t seq, int64_t rows) { return ((seqs - 1) * seq + (Hkv - 1) * head + rows) * 4; };
         if (!apart(T_out, {keep_head, Hkv}, {keep_seq, seqs}, {0, 1})) return SKIPFFN_EINVAL;
-        if (weights_out != nullptr && (!apart(T_out, {weights_out_head, Hkv}, {weights_out_seq, seqs}, {0, 1}) ||
-                                       (T > 0 && ranges_meet(weights_out, span(weights_out_head, weights_out_seq, T_out), weights,
-                                                             span(weights_head, weights_seq, T)))))
+        if (weights_out != nullptr && !apart(T_out, {weights_out_head, Hkv}, {weights_out_seq, seqs}, {0, 1}))
+            return SKIPFFN_EINVAL;
+    }
+    // a head's workgroup writes numbers and counts while others, and the second kernel, still read
+    {
+        const int64_t counts = (n_seq + (packed ? 1 : 0)) * 4;
+        auto span = [&](int64_t head, int64_t seq, int64_t rows) { return rows > 0 ? ((seqs - 1) * seq + (Hkv - 1) * head + rows) * 4 : 0; };
+        struct Range { const void* p; int64_t bytes; };
+        const Range outs[3] = {{seg_out, counts}, {keep, span(keep_head, keep_seq, T_out)},
+                               {weights_out, weights_out == nullptr ? 0 : span(weights_out_head, weights_out_seq, T_out)}};
+        const Range ins[3] = {{seg, counts}, {n_keep_dev, n_keep_dev == nullptr ? 0 : n_seq * 4}, {weights, span(weights_head, weights_seq, T)}};
+        for (const Range& o : outs)
+            for (const Range& i : ins)
+                if (ranges_meet(o.p, o.bytes, i.p, i.bytes)) return SKIPFFN_EINVAL;
+        if (ranges_meet(outs[0].p, outs[0].bytes, outs[1].p, outs[1].bytes) || ranges_meet(outs[0].p, outs[0].bytes, outs[2].p, outs[2].bytes) ||
+            (T_out > 0 && static_cast<const void*>(keep) == weights_out))
             return SKIPFFN_EINVAL;
     }
     const int64_t cap = (int64_t)1 << 30;

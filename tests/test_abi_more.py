@@ -155,7 +155,7 @@ def test_decode_weights_reject_bad_arguments():
 
 # ---- eviction ----------------------------------------------------------------------------------------
 def evict(n=2, H=4, D=64, T=64, T_out=32, packed=1, t=None, ks=1 << 14, vs=1 << 14, w=FARS[8], w_head=64, w_seq=256, seg=FAKE, keep_n=16, keep_dev=None,
-          first=0, recent=0, kos=1 << 14, vos=1 << 14, wo=FARS[9], wo_head=32, wo_seq=128, keep=FARS[10], keep_head=32, keep_seq=128, seg_out=FAKE):
+          first=0, recent=0, kos=1 << 14, vos=1 << 14, wo=FARS[9], wo_head=32, wo_seq=128, keep=FARS[10], keep_head=32, keep_seq=128, seg_out=FARS[11]):
     t = {**{i: heads(FAR[i]) for i in range(4)}, **(t or {})}            # k, v, their outputs
     return B.lib().skipffn_kv_evict(n, H, D, T, T_out, packed, t[0], t[1], ks, vs, w, w_head, w_seq, seg, keep_n, keep_dev, first, recent, t[2], t[3],
                                     kos, vos, wo, wo_head, wo_seq, keep, keep_head, keep_seq, seg_out, None)
@@ -177,6 +177,19 @@ def test_evict_rejects_bad_arguments(packed):
         for i in (0, 1):
             assert evict(packed=packed, t={o: heads(FAR[i] + 1024)}) == B.EINVAL       # in place kept rows would race
     assert evict(packed=packed, n=0, seg=None) == B.OK
+
+
+@pytest.mark.parametrize("packed", [0, 1])
+def test_evict_rejects_counts_and_numbers_over_what_it_reads(packed):
+    # a head's workgroup would write them while another's still reads
+    for bad in (dict(seg_out=FAKE), dict(seg_out=FAKE + 4), dict(seg=FARS[11]), dict(keep_dev=FARS[11]), dict(keep_dev=FARS[11] + 4), dict(seg_out=FARS[8]),
+                dict(keep=FARS[8]), dict(keep=FARS[8] + 64), dict(keep=FAKE), dict(keep=FARS[11]), dict(keep_dev=FARS[10]), dict(keep=FARS[9]),
+                dict(wo=FAKE), dict(wo=FARS[11]), dict(wo=FARS[5], keep_dev=FARS[5])):
+        assert evict(packed=packed, **bad) == B.EINVAL, bad
+
+
+def test_key_weights_reject_weights_over_the_saved_sums():
+    assert key_weights(w=FARS[9], saved=FARS[9]) == B.EINVAL and key_weights(w=FARS[9] + 64, saved=FARS[9]) == B.EINVAL
 
 
 def test_evict_rejects_sequences_that_lie_over_one_another():
