@@ -1066,6 +1066,7 @@ int decode_call(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_
     DecodeWeightsArgs w{};
     if (weights != nullptr) {
         a.most_shared = (int)std::min(weights->most_shared, n_seq);
+        a.ways = decode_weight_ways(Tg, Hq, Hkv, a.most_shared, num_cus());
         a.prefix_ld = (int)decode_prefix_ld(Tg, n_groups); a.own_ld = (int)decode_own_ld(cap);
         a.prefix_scores = reinterpret_cast<float*>(ws + ws_of.prefix);
         a.own_scores = reinterpret_cast<float*>(ws + ws_of.own);

@@ -106,15 +106,24 @@ __global__ __launch_bounds__(DW_THREADS) void decode_weights_kernel(const AttnDe
 }
 
 namespace {
-// By the products that a shared row of the cache has (shared rows; us of whole calls, one wavefront a row / four): 4 (71723 rows) 77.2 / 89.3, 8 (64000) 73.1 / 82.0,
-// 16 (32000) 46.0 / 49.8, 32 (32000) 60.0 / 63.8, 128 (3053) 36.8 / 32.7; between 32 and 128 nothing was timed
-int weight_ways(const AttnDecodeArgs& a) { return (int64_t)a.most_shared * (a.Hq / a.Hkv) > 64 ? 4 : 1; }
 int64_t prefix_chunks_of(const AttnDecodeArgs& a) {
-    const int64_t ch = DW_THREADS / weight_ways(a);
+    const int64_t ch = DW_THREADS / a.ways;
     return a.Tp > 0 ? (a.Tp + ch - 1) / ch + a.n_groups : 0;
 }
 int64_t joins_of(const AttnDecodeArgs& a) { return a.splits > 1 ? ((int64_t)a.n_seq * a.Hq + ATT_WAVES - 1) / ATT_WAVES : 0; }
 }  // namespace
+
+// Four wavefronts a shared row where one leaves compute units without work (32 / 8 heads, us of whole calls, one / four; products of a row beside its rows):
+//     rows      8              16             32             64             128
+//      1500   12.3 / 12.1    13.9 / 13.2    17.0 / 16.3    23.5 / 22.0    30.9 / 26.7
+//      4000   15.2 / 15.0    18.1 / 17.5    19.3 / 19.2    27.0 / 25.7    33.8 / 30.5
+//      8000   19.4 / 19.9    26.1 / 26.1    27.1 / 28.5    32.9 / 33.1    51.1 / 47.9
+//     16000   25.2 / 26.3    28.3 / 29.4    38.7 / 42.0    47.8 / 50.2    74.7 / 74.6
+//     24000   36.0 / 39.0    42.7 / 46.6    53.2 / 61.2    73.0 / 79.0   110.3 / 113.5
+int decode_weight_ways(int64_t Tp, int64_t Hq, int64_t Hkv, int64_t most_shared, int ncu) {
+    const int64_t products = most_shared * (Hq / Hkv), blocks = Tp / DW_THREADS * Hkv;
+    return products >= 8 && blocks <= (products > 64 ? ncu : ncu / 2) ? 4 : 1;
+}
 
 int64_t decode_weights_workgroups(const AttnDecodeArgs& a) {
     return joins_of(a) + (prefix_chunks_of(a) + (int64_t)a.n_seq * ((a.cap + DW_THREADS - 1) / DW_THREADS)) * a.Hkv;
@@ -122,7 +131,7 @@ int64_t decode_weights_workgroups(const AttnDecodeArgs& a) {
 
 template <int DP>
 static void launch_dw(const AttnDecodeArgs& a, const DecodeWeightsArgs& w, const AttnJoinArgs& j, uint32_t grid, hipStream_t s) {
-    if (weight_ways(a) == 1) decode_weights_kernel<DP, 1><<<grid, DW_THREADS, 0, s>>>(a, w, j, (int)joins_of(a), (int)prefix_chunks_of(a));
+    if (a.ways == 1) decode_weights_kernel<DP, 1><<<grid, DW_THREADS, 0, s>>>(a, w, j, (int)joins_of(a), (int)prefix_chunks_of(a));
     else decode_weights_kernel<DP, 4><<<grid, DW_THREADS, 0, s>>>(a, w, j, (int)joins_of(a), (int)prefix_chunks_of(a));
 }
 

@@ -218,7 +218,8 @@ struct AttnDecodeArgs {
     float* part; float* stat;                     // splits > 1: as in AttnJoinArgs
     // With weights: the products of a row and its keys, of the first most_shared sequences of a group [Hkv][most_shared][Hq / Hkv][prefix_ld], those of
     // group i from decode_score_at on, and of own rows [n_seq][Hq][own_ld], and with splits 1 every row's log-sum-exp [Hq][n_seq], as AttnArgs::lse
-    int most_shared, weigh, prefix_ld, own_ld; float* prefix_scores; float* own_scores; float* lse;      // weigh: set by the launch
+    // weigh: set by the launch; ways: wavefronts that share the products of a shared row in the second kernel, 1 or 4
+    int most_shared, weigh, ways, prefix_ld, own_ld; float* prefix_scores; float* own_scores; float* lse;
 };
 // Products leave in whole tiles of 32 keys: room for the last tile of every group, whose first product is 16-byte aligned.  Rows of p0 .. are at most
 // the next group's 36 - 3 before it
@@ -233,6 +234,7 @@ struct DecodeWeightsArgs {
     float* own_w; int64_t own_seq, own_head;
     int accumulate;
 };
+int decode_weight_ways(int64_t Tp, int64_t Hq, int64_t Hkv, int64_t most_shared, int ncu);
 int64_t decode_weights_workgroups(const AttnDecodeArgs& a);
 // the second kernel of a call with weights: joins the parts' rows (j) and takes the weights
 hipError_t launch_decode_weights(const AttnDecodeArgs& a, const DecodeWeightsArgs& w, const AttnJoinArgs& j, hipStream_t s);

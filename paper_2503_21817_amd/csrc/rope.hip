@@ -364,8 +364,8 @@ RopeGrid rope_grid(const RopeArgs& a, int lph, int heads, int u) {
 constexpr int ROPE_BWD_PER_CU = 3;                       // workgroups, by its registers
 }  // namespace
 
-// Heads of a wavefront one after the other: one where that many wavefronts find room on the chip at once, otherwise three (us, 32 / 8 heads of 128: 64 tokens 5.0 /
-// 6.5, 11776 tokens into a cache 99 / 71; six 8.6 / 67; before loads without branches)
+// Heads of a wavefront one after the other: one where that many wavefronts find room on the chip at once, otherwise three (us, 32 / 8 heads of 128 into a cache, one / three:
+// 64 tokens 4.5 / 6.3, 616 8.4 / 8.9, 1500 14.7 / 12.7, 2944 22.4 / 18.4, 11776 75.7 / 60.3)
 template <class Launch>
 static void rope_forward_variant(const RopeArgs& a, int ncu, Launch&& go) {
     rope_variant(a, [&](auto v, auto lph) {

@@ -156,6 +156,24 @@ def test_captured_and_replayed():
         assert all(torch.equal(w.sw[i, :, :n], want[1][i, :, :n]) for i, n in enumerate(d.own)), turn
 
 
+@pytest.mark.parametrize("prefix", [(900, 333), (3001, 3999), (5003, 2 ** 13)], ids=["few rows", "rows for the chip's half", "many rows"])
+@pytest.mark.parametrize("Hq", [8, 16, 32])              # of 8 key/value heads; products of a row 20 to 84
+def test_few_and_many_rows_with_few_and_many_products(prefix, Hq):
+    print(f"decode weights prefix {prefix} heads {Hq}", flush=True)
+    d = Decode((20, 21, 2), prefix, tuple(i * 5 % 37 for i in range(43)), Hq, 8, 40, True)
+    d.run(0.2)
+    alone = bits_of(d.out)
+    w = Weights(d)
+    w.run(0.2)
+    w.check(0.2)
+    assert np.array_equal(bits_of(d.out), alone)
+    w.run(0.2, B.FLAG_DW_ACCUMULATE)
+    w.check(0.2, times=2)
+    short = Weights(d, most=9)                           # those past the ninth of a group add nothing to its prefix
+    short.run(0.2)
+    short.check(0.2)
+
+
 def test_products_past_32_bits():
     """16 sequences on one prefix of 2^20 rows: 2^29 products of a head of the cache, 2^31 in all."""
     n, Hq, Hkv, D, Tp = 16, 128, 2, 8, 2 ** 20
