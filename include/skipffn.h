@@ -430,8 +430,8 @@ int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, 
  *   weights_out     the kept rows' weights, or NULL
  *   keep            the kept rows' numbers, counted from their sequence's first row
  * Rows past a sequence's are left as they were, in every output.  Strides in elements; those of sequences are not read where packed.
- * What k_out and v_out span meets neither k nor v, and keep, weights_out and seg_out meet neither weights, seg nor n_keep_dev (kept rows, and heads that
- * still read, would race); no two elements of the outputs are one.
+ * What k_out and v_out span meets neither k nor v, and what keep, weights_out and seg_out span meets neither weights, seg nor n_keep_dev (kept rows, and
+ * heads that still read, would race).  No element of an output is one of k, v or seg, or another output's.
  * Rows are copied bit for bit.  T, T_out < 2^30, n_seq Hkv < 2^22, workgroups of 16 kept rows of a head fewer than 2^24; D and strides of k, v as
  * in skipffn_attn_forward.  Deterministic. */
 int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T_out, int packed, const skipffn_heads* k, const skipffn_heads* v,

@@ -857,6 +857,47 @@ bool ranges_meet(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes)
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return a_bytes > 0 && b_bytes > 0 && x < y + (uintptr_t)b_bytes && y < x + (uintptr_t)a_bytes;
 }
+// Elements on a grid: runs of `run` bytes at up to three strides (bytes).  What they span may meet where they share none: heads of one tensor between
+// those of another, the parts of a sequence side by side.
+struct Dim { int64_t stride, n; };
+struct Grid {
+    const void* p;
+    int64_t run;
+    Dim d[3];                                            // the largest stride first
+    int dims;
+    int64_t span(int from) const {
+        int64_t e = run;
+        for (int i = from; i < dims; ++i) e += (d[i].n - 1) * d[i].stride;
+        return e;
+    }
+};
+Grid grid_of(const void* p, int64_t run, Dim a, Dim b = {0, 1}, Dim c = {0, 1}) {
+    Grid g{p, run, {}, 0};
+    for (const Dim& x : {a, b, c}) {
+        if (x.n <= 0) g.run = 0;
+        if (x.n > 1) g.d[g.dims++] = x;
+    }
+    std::sort(g.d, g.d + g.dims, [](const Dim& x, const Dim& y) { return x.stride > y.stride; });
+    return g;
+}
+// Whether a from its i-th stride on and b from its j-th on, which begins `ahead` bytes after a, share an element.  The larger stride is taken off both: they are in
+// steps of it, so only the distances around 0 count.  True where they are interleaved in another way than that.
+bool grids_share_from(int64_t ahead, const Grid& a, int i, const Grid& b, int j) {
+    if (ahead >= a.span(i) || -ahead >= b.span(j)) return false;
+    const int64_t sa = i < a.dims ? a.d[i].stride : 0, sb = j < b.dims ? b.d[j].stride : 0, step = std::max(sa, sb);
+    if (step == 0) return true;
+    const int in = i + (sa == step), jn = j + (sb == step);
+    if (a.span(in) > step || b.span(jn) > step) return true;
+    const int64_t r = (ahead % step + step) % step;
+    return grids_share_from(r, a, in, b, jn) || grids_share_from(r - step, a, in, b, jn);
+}
+bool grids_share(const Grid& a, const Grid& b) {
+    if (a.run <= 0 || b.run <= 0) return false;
+    return grids_share_from((int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)), a, 0, b, 0);
+}
+Grid heads_grid(const skipffn_heads* t, int64_t T, int64_t H, int64_t D, int64_t seq_stride = 0, int64_t n_seq = 1) {
+    return grid_of(t->data, D * 2, {t->token_stride * 2, T}, {t->head_stride * 2, H}, {seq_stride * 2, n_seq});
+}
 bool bad4(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 bool bad_seg(const int32_t* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 const bf16_t* in(const skipffn_heads* t) { return static_cast<const bf16_t*>(t->data); }
@@ -1297,7 +1338,6 @@ int skipffn_qk_rope_backward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int6
 // ---- eviction by what the rows received -------------------------------------------------------------------
 namespace {
 // Elements of `inner` in a row and of dimensions with these strides and sizes: none is another's
-struct Dim { int64_t stride, n; };
 bool apart(int64_t inner, Dim a, Dim b, Dim c) {
     Dim d[3] = {a, b, c};
     std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
@@ -1362,8 +1402,18 @@ int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T
         for (const Range& o : outs)
             for (const Range& i : ins)
                 if (ranges_meet(o.p, o.bytes, i.p, i.bytes)) return SKIPFFN_EINVAL;
-        if (ranges_meet(outs[0].p, outs[0].bytes, outs[1].p, outs[1].bytes) || ranges_meet(outs[0].p, outs[0].bytes, outs[2].p, outs[2].bytes) ||
-            (T_out > 0 && static_cast<const void*>(keep) == weights_out))
+        // and the second kernel copies rows by the numbers and counts: it writes none of them
+        const Dim by_head{keep_head * 4, Hkv}, by_seq{keep_seq * 4, seqs}, w_by_head{weights_out_head * 4, Hkv}, w_by_seq{weights_out_seq * 4, seqs};
+        const Grid kept[3] = {grid_of(seg_out, counts, {0, 1}), grid_of(keep, T_out * 4, by_head, by_seq),
+                              grid_of(weights_out, weights_out == nullptr ? 0 : T_out * 4, w_by_head, w_by_seq)};
+        const Grid rows[4] = {heads_grid(k, T, Hkv, D, k_seq, seqs), heads_grid(v, T, Hkv, D, v_seq, seqs), heads_grid(k_out, T_out, Hkv, D, k_out_seq, seqs),
+                              heads_grid(v_out, T_out, Hkv, D, v_out_seq, seqs)};
+        for (const Grid& o : kept)
+            for (const Grid& r : rows)
+                if (grids_share(o, r)) return SKIPFFN_EINVAL;
+        const Grid offsets = grid_of(seg, counts, {0, 1});
+        if (grids_share(kept[0], kept[1]) || grids_share(kept[0], kept[2]) || grids_share(kept[1], kept[2]) || grids_share(offsets, rows[2]) ||
+            grids_share(offsets, rows[3]))
             return SKIPFFN_EINVAL;
     }
     const int64_t cap = (int64_t)1 << 30;

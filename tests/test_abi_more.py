@@ -188,6 +188,42 @@ def test_evict_rejects_counts_and_numbers_over_what_it_reads(packed):
         assert evict(packed=packed, **bad) == B.EINVAL, bad
 
 
+@pytest.mark.parametrize("packed", [0, 1])
+def test_evict_rejects_numbers_weights_and_counts_over_the_rows(packed):
+    # the second kernel copies rows by the numbers and offsets that the first one wrote
+    last = 64 * 4 * 64 * 2 - 4                           # of a packed cache's keys, in bytes
+    for i in range(4):                                   # k, v, their outputs
+        for off in (0, 512, last if i < 2 else last // 2):
+            for name in ("keep", "wo", "seg_out") + (("seg",) if i >= 2 else ()):
+                assert evict(packed=packed, t={i: heads(FARS[12])}, **{name: FARS[12] + off}) == B.EINVAL, (i, off, name)
+    for off in (4, 64, -64):                             # a head's numbers over the weights of another
+        assert evict(packed=packed, wo=FARS[10] + off) == B.EINVAL, off
+
+
+def test_evict_takes_outputs_side_by_side():
+    """What counts is whether they share an element, not whether what they span meets.  n H 4 = 2^24 workgroups: more than a launch has, the last of
+    the checks, so that nothing is enqueued."""
+    n, H, T, D = 256, 1 << 14, 8, 8
+    k = H * T * D                                        # elements of a sequence's keys
+    w = H * T                                            # of its weights
+    slab = 4 * k + 4 * w                                 # of 2 bytes: k, v, k_out, v_out, then weights_out and keep of 4 bytes
+    t = {i: heads(FARS[12] + i * k * 2, token=D, head=T * D, H=H) for i in range(4)}
+    far = {i: heads(FARS[4 + i], token=D, head=T * D, H=H) for i in range(4)}
+
+    def call(wo, keep, head, seq, t=far, rows=k):
+        return evict(n, H, D, T, T, 0, t, rows, rows, FARS[8], T, w, wo=wo, wo_head=head, wo_seq=seq, keep=keep, keep_head=head, keep_seq=seq, kos=rows,
+                     vos=rows)
+    assert call(FARS[9], FARS[10], T, w) == B.ESHAPE                     # accepted
+    # weights and numbers of a head side by side; one of them a row on
+    assert call(FARS[9], FARS[9] + 4 * T, 2 * T, 2 * w) == B.ESHAPE and call(FARS[9], FARS[9] + 4 * w, T, 2 * w) == B.ESHAPE
+    assert call(FARS[9], FARS[9] + 4 * T - 4, 2 * T, 2 * w) == B.EINVAL and call(FARS[9], FARS[9] + 4 * w + 4, T, 2 * w) == B.EINVAL
+    # all of a sequence in one place
+    free = FARS[12] + 4 * k * 2
+    out = {0: far[0], 1: far[1], 2: t[2], 3: t[3]}
+    assert call(free, free + 4 * w, T, slab // 2, out, slab) == B.ESHAPE
+    assert call(free - 4, free + 4 * w, T, slab // 2, out, slab) == B.EINVAL and call(free, free + 4 * w + 4, T, slab // 2, {**out, 2: t[0]}, slab) == B.EINVAL
+
+
 def test_key_weights_reject_weights_over_the_saved_sums():
     assert key_weights(w=FARS[9], saved=FARS[9]) == B.EINVAL and key_weights(w=FARS[9] + 64, saved=FARS[9]) == B.EINVAL
 
