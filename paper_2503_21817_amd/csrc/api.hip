@@ -1083,6 +1083,20 @@ int decode_call(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_
     if (n_seq > 0 && (meets(q, n_seq, Hq, 0) || (Tg > 0 && (meets(prefix_k, Tg, Hkv, 0) || meets(prefix_v, Tg, Hkv, 0))) ||
         (cap > 0 && (meets(suffix_k, cap, Hkv, (n_seq - 1) * suffix_k_seq) || meets(suffix_v, cap, Hkv, (n_seq - 1) * suffix_v_seq)))))
         return SKIPFFN_EINVAL;
+    if (weights != nullptr) {
+        // a workgroup stores weights while others still read
+        const Grid received[2] = {grid_of(weights->prefix, Tg * 4, {weights->prefix_head * 4, Hkv}),
+                                  grid_of(weights->own, cap * 4, {weights->own_head * 4, Hkv}, {weights->own_seq * 4, n_seq})};
+        const Grid read[9] = {heads_grid(q, n_seq, Hq, D), heads_grid(out, n_seq, Hq, D),
+                              Tg > 0 ? heads_grid(prefix_k, Tg, Hkv, D) : Grid{}, Tg > 0 ? heads_grid(prefix_v, Tg, Hkv, D) : Grid{},
+                              cap > 0 ? heads_grid(suffix_k, cap, Hkv, D, suffix_k_seq, n_seq) : Grid{},
+                              cap > 0 ? heads_grid(suffix_v, cap, Hkv, D, suffix_v_seq, n_seq) : Grid{},
+                              grid_of(suffix_len, cap > 0 ? n_seq * 4 : 0, {0, 1}), grid_of(group_off, n_groups > 0 ? (n_groups + 1) * 4 : 0, {0, 1}),
+                              grid_of(prefix_seg, Tg > 0 ? (n_groups + 1) * 4 : 0, {0, 1})};
+        for (const Grid& w : received)
+            for (const Grid& r : read)
+                if (grids_share(w, r)) return SKIPFFN_EINVAL;
+    }
     const DecodeWs ws_of = decode_ws(n_seq, n_groups, Hq, Hkv, D, Tp, cap, weights != nullptr, weights != nullptr ? weights->most_shared : 0);
     const PartsWs& W = ws_of.parts;
     if (ws_of.total > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < ws_of.total)) return SKIPFFN_EWORKSPACE;

@@ -153,6 +153,29 @@ def test_decode_weights_reject_bad_arguments():
     assert B.skipffn_attn_decode_weights_workspace_bytes(4, 1, 4, 4, 64, 64, 64, -1) == 0
 
 
+def test_decode_weights_reject_weights_over_what_other_workgroups_read():
+    last = 64 * 4 * 64 * 2 - 4                           # of a tensor of 64 rows, in bytes; q and out have 4
+    for i in range(6):                                   # q, prefix k, v, own k, v, out
+        for off in (0, 256, 4 * 4 * 64 * 2 - 4 if i in (0, 5) else last):
+            for name in ("pw", "sw"):
+                assert dec(t={i: heads(FARS[12])}, ws=None, **{name: FARS[12] + off}) == B.EINVAL, (i, off, name)
+    for table, n in (("seg", 2), ("off", 2), ("lens", 4)):
+        for name in ("pw", "sw"):
+            assert dec(ws=None, **{table: FARS[12], name: FARS[12] + 4 * n - 4}) == B.EINVAL, (table, name)
+            assert dec(ws=None, **{table: FARS[12], name: FARS[12] + 4 * n}) == B.EWORKSPACE, (table, name)
+    # a prefix alone, own rows alone, a prefix that nobody reads
+    assert dec(G=0, Tp=0, pw=None, ws=None, sw=FARS[3]) == B.EINVAL and dec(cap=0, sw=None, ws=None, pw=FARS[2] + 64) == B.EINVAL
+    assert dec(n=0, cap=0, pw=FARS[1]) == B.EINVAL and dec(n=0, cap=0, pw=FARS[12], off=FARS[12]) == B.EINVAL
+    # every sequence's own keys, values and weights in one place of 64 rows of 4 heads: side by side, and a row too early
+    k, w = 64 * 4 * 64, 64 * 4
+    slab = 2 * k + 2 * w                                 # elements of 2 bytes
+    own = {3: heads(FARS[12]), 4: heads(FARS[12] + 2 * k)}
+    at = FARS[12] + 4 * k
+    assert dec(t=own, ks=slab, vs=slab, sw=at, sw_seq=slab // 2, ws=None) == B.EWORKSPACE
+    assert dec(t=own, ks=slab, vs=slab, sw=at - 4, sw_seq=slab // 2, ws=None) == B.EINVAL
+    assert dec(t=own, ks=slab, vs=slab, sw=at + 4, sw_seq=slab // 2, ws=None) == B.EINVAL
+
+
 # ---- eviction ----------------------------------------------------------------------------------------
 def evict(n=2, H=4, D=64, T=64, T_out=32, packed=1, t=None, ks=1 << 14, vs=1 << 14, w=FARS[8], w_head=64, w_seq=256, seg=FAKE, keep_n=16, keep_dev=None,
           first=0, recent=0, kos=1 << 14, vos=1 << 14, wo=FARS[9], wo_head=32, wo_seq=128, keep=FARS[10], keep_head=32, keep_seq=128, seg_out=FARS[11]):
