@@ -179,7 +179,9 @@ KeyWeightsPlan key_weights_plan(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t H
     p.blocks = (Tk / KW_KEYS + n_seq) * Hkv;
     const int64_t rows = n_seq > 0 ? std::min(Tq / n_seq, last) : 0, steps = (rows + KW_ROWS - 1) / KW_ROWS * (Hq / Hkv);
     const double piece = 1.2 * (double)steps, begin = 6.0 * (double)p.blocks / (2.0 * ncu);
-    const int64_t parts = std::min<int64_t>({steps / 4, (int64_t)std::lround(std::sqrt(piece / std::max(begin, 1e-3))), KEY_WEIGHTS_MAX_PARTS});
+    // a launch has fewer than 2^24 workgroups
+    const int64_t fit = (((int64_t)1 << 24) - 1) / std::max<int64_t>(p.blocks, 1);
+    const int64_t parts = std::min<int64_t>({steps / 4, (int64_t)std::lround(std::sqrt(piece / std::max(begin, 1e-3))), KEY_WEIGHTS_MAX_PARTS, fit});
     p.parts = parts > 1 && piece - piece / (double)parts > 5.0 ? (int)parts : 1;
     return p;
 }

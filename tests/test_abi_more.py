@@ -122,6 +122,18 @@ def test_key_weights_reject_bad_arguments():
     assert many(255) == B.EINVAL and many(257) == B.ESHAPE
 
 
+def test_key_weights_take_all_that_a_launch_holds():
+    """(Tk / 256 + n_seq) Hkv < 2^24 is the bound: the parts that the queries are cut into have to fit it, not the call."""
+    lib = B.lib().skipffn_attn_key_weights
+    for H, T in ((16, (1 << 26) - 128), (1, (1 << 30) - 128), (25, (1 << 30) // 25 - 256)):
+        assert (T // 256 + 1) * H < 1 << 24
+        need = B.skipffn_attn_key_weights_workspace_bytes(T, T, 1, H, H, 8)
+        assert need >= 2 * H * T * 4, (H, T)
+        # no saved sums: refused past the shapes
+        t = heads(FAR[0], token=8 * H, head=8, H=H), heads(FAR[1], token=8 * H, head=8, H=H)
+        assert lib(T, T, 1, H, H, 8, *t, FAKE, None, 1, 0.125, None, -1, FARS[9], T, None, 0, 0, None) == B.EINVAL, (H, T)
+
+
 # ---- single tokens with weights ------------------------------------------------------------------------
 def dec(n=4, G=1, Hq=4, Hkv=4, D=64, Tp=64, cap=64, t=None, seg=FAKE, off=FAKE, ks=1 << 14, vs=1 << 14, lens=FAKE, scale=0.125, most=4, pw=FARS[8],
         pw_head=64, sw=FARS[9], sw_seq=256, sw_head=64, ws=FAKE, ws_bytes=BIG, flags=0):
