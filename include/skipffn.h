@@ -382,8 +382,9 @@ int skipffn_attn_decode(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv
  *   suffix_weights  f32 [n_seq, Hkv, suffix_capacity] OUT by strides of sequence and head (no element shared); rows past suffix_len are
  *                   left as they were.  Not read or written where suffix_capacity == 0
  * Both are overwritten, or += with SKIPFFN_FLAG_DW_ACCUMULATE (the only flag).  What they span does not meet, and no weight is an element of q, out, the
- * cache or the offsets and lengths, which other workgroups still read.  `out` has the bits that skipffn_attn_decode gives; all else as there.  A sequence whose row of `out` is NaN for its scores makes NaN of the weights of the rows it sees.  Deterministic.
- * Tp + 36 n_groups and suffix_capacity < 2^24 - 64, (Tp / 64 + n_groups + n_seq (suffix_capacity / 256 + 1)) Hkv + n_seq Hq / 4 < 2^24 - 1.
+ * cache or the offsets and lengths, which other workgroups still read.  `out` has the bits that skipffn_attn_decode gives; all else as there.
+ * A sequence whose row of `out` is NaN for its scores makes NaN of the weights of the rows it sees.  Deterministic.
+ * Tp + 36 n_groups and suffix_capacity < 2^24 - 64, (Tp / 64 + 1 + n_groups + n_seq (suffix_capacity / 256 + 1)) Hkv + n_seq Hq / 4 < 2^24 - 1.
  * workspace: at least skipffn_attn_decode_weights_workspace_bytes(...): about 4 Hq (most_shared Tp + n_seq suffix_capacity) and what decode takes. */
 size_t skipffn_attn_decode_weights_workspace_bytes(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_t D, int64_t Tp,
                                                    int64_t suffix_capacity, int64_t most_shared);
