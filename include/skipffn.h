@@ -408,7 +408,8 @@ int skipffn_attn_decode_weights(int64_t n_seq, int64_t n_groups, int64_t Hq, int
  *             SKIPFFN_FLAG_DW_ACCUMULATE (the only flag).  Keys that no query sees get 0; keys of no sequence are left as they were
  *   workspace at least skipffn_attn_key_weights_workspace_bytes(...) bytes (NULL where that is 0)
  * A query whose scores are not finite where it sees (its log-sum-exp is NaN or minus infinity) makes NaN of the keys it
- * sees, and of no others.  fp32 throughout.  weights meets none of q, k and saved.  Shapes as skipffn_attn_forward, and
+ * sees, and of no others.  fp32 throughout.  What weights spans meets none of q, k and saved, no weight is an
+ * element of seg_q or seg_k.  Shapes as skipffn_attn_forward, and
  * (Tk / 256 + n_seq) Hkv < 2^24.  Deterministic. */
 size_t skipffn_attn_key_weights_workspace_bytes(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, int64_t last);
 int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t D, const skipffn_heads* q,

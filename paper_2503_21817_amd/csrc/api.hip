@@ -1200,6 +1200,10 @@ int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, 
     if (ranges_meet(weights, w_bytes, q->data, heads_span(q, Tq, Hq, D)) || ranges_meet(weights, w_bytes, k->data, heads_span(k, Tk, Hkv, D)) ||
         (last != 0 && ranges_meet(weights, w_bytes, saved, Hq * Tq * 4)))
         return SKIPFFN_EINVAL;
+    // a workgroup stores weights while others still find their sequence
+    const Grid received = grid_of(weights, Tk * 4, {weights_head * 4, Hkv});
+    for (const int32_t* offsets : {seg_q, seg_k})
+        if (offsets != nullptr && grids_share(received, grid_of(offsets, (n_seq + 1) * 4, {0, 1}))) return SKIPFFN_EINVAL;
     const size_t need = key_weights_bytes(plan, Tk, Hkv);
     if (need > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < need)) return SKIPFFN_EWORKSPACE;
     hipStream_t s = (hipStream_t)stream;

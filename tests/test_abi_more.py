@@ -134,6 +134,17 @@ def test_key_weights_take_all_that_a_launch_holds():
         assert lib(T, T, 1, H, H, 8, *t, FAKE, None, 1, 0.125, None, -1, FARS[9], T, None, 0, 0, None) == B.EINVAL, (H, T)
 
 
+def test_key_weights_reject_weights_over_the_offsets():
+    # a workgroup would store them while others still find their sequence by these; parts without a workspace: nothing is enqueued
+    parts = dict(Tq=1 << 16, q=heads(FAR[2]), ws=None)
+    for bad in (dict(w=FAKE, sk=FARS[12]), dict(w=FAKE + 4, sk=FARS[12]), dict(w=FARS[12], sk=FARS[12]), dict(w=FARS[12] + 4, sk=FARS[12])):
+        assert key_weights(**parts, **bad) == B.EINVAL, bad
+    assert key_weights(**parts, w=FARS[12] + 8, sk=FARS[12]) == B.EWORKSPACE
+    assert key_weights(**parts, w=FARS[12] - 64 * 4, w_head=64 + 2, sk=FARS[12]) == B.EWORKSPACE       # between two heads'
+    assert key_weights(**parts, w=FARS[12] - 64 * 4, w_head=64 + 1, sk=FARS[12]) == B.EINVAL
+    assert key_weights(w=FAKE) == B.EINVAL               # one table for both
+
+
 # ---- single tokens with weights ------------------------------------------------------------------------
 def dec(n=4, G=1, Hq=4, Hkv=4, D=64, Tp=64, cap=64, t=None, seg=FAKE, off=FAKE, ks=1 << 14, vs=1 << 14, lens=FAKE, scale=0.125, most=4, pw=FARS[8],
         pw_head=64, sw=FARS[9], sw_seq=256, sw_head=64, ws=FAKE, ws_bytes=BIG, flags=0):
