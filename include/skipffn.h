@@ -458,8 +458,8 @@ int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T
  *             [0, rows_out) (a padded batch); rows that no token has are left as they were.  Two tokens with the same row: each 16 bytes
  *             of it come from one of them.  NULL: row t (rows_out is not read)
  * An output may be its own input (same memory and strides, row == NULL); training with a norm needs the inputs again, so not then.
- * Otherwise it shares no element with an input or another output: what they span does not meet, or they are column ranges of
- * rows of one stride.  v is copied bit for bit.
+ * Otherwise it shares no element with an input (positions, frequencies, rows and gains are read by all workgroups) or another output: what
+ * heads span does not meet, or they are column ranges of rows of one stride.  v is copied bit for bit.
  * Own rows of skipffn_attn_decode, [n_seq, capacity, Hkv, D] or [Hkv, n_seq, capacity, D], are a cache of n_seq * capacity rows: a new
  * token's is sequence * capacity + own length.
  * D % 8 == 0, 8 <= D <= 128, rot % 8 == 0, 0 <= rot <= D, n_axes <= 4, T (Hq + 2 Hkv) < 2^27 (the forward call).  eps >= 0, finite. */
@@ -474,7 +474,8 @@ int skipffn_qk_rope_forward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64
  *   q, k             what the forward call read; NULL (not read) without SKIPFFN_FLAG_QK_NORM
  *   grad_q, grad_k   OUT, as q and k; may be grad_q_out, grad_k_out themselves, else as the outputs above
  *   d_gain_q, d_gain_k  NULL, or f32 [D] OUT (with the norm; also where the gain is NULL), overwritten, or += with
- *                    SKIPFFN_FLAG_DW_ACCUMULATE.  Summed in a fixed order that depends on the sizes of the call.
+ *                    SKIPFFN_FLAG_DW_ACCUMULATE.  Summed in a fixed order that depends on the sizes of the call.  Neither shares an
+ *                    element with another output
  *   workspace        for gain gradients alone: at least skipffn_qk_rope_backward_workspace_bytes(...) */
 size_t skipffn_qk_rope_backward_workspace_bytes(int64_t T, int64_t Hq, int64_t Hkv, int64_t D);
 int skipffn_qk_rope_backward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, int64_t n_axes, const skipffn_heads* q,

@@ -1263,6 +1263,15 @@ RopeArgs rope_args(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, i
     a.gain_q = static_cast<const bf16_t*>(gain_q); a.gain_k = static_cast<const bf16_t*>(gain_k);
     return a;
 }
+// whether elements of a result are what every workgroup reads beside the heads
+bool rope_reads(const RopeArgs& a, const Grid& result) {
+    const int64_t gain = a.D * 2;
+    return grids_share(result, grid_of(a.pos, (int64_t)a.n_axes * a.T * 4, {0, 1})) ||
+           grids_share(result, grid_of(a.inv_freq, a.T > 0 ? a.rot * 2 : 0, {0, 1})) ||
+           grids_share(result, grid_of(a.gain_q, a.gain_q != nullptr ? gain : 0, {0, 1})) ||
+           grids_share(result, grid_of(a.gain_k, a.gain_k != nullptr ? gain : 0, {0, 1})) ||
+           grids_share(result, grid_of(a.row, a.row != nullptr ? (int64_t)a.T * 4 : 0, {0, 1}));
+}
 }  // namespace
 
 int skipffn_qk_rope_forward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, int64_t n_axes, const skipffn_heads* q,
@@ -1300,6 +1309,8 @@ int skipffn_qk_rope_forward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64
         a.v_out = rope_out(v_out);
     }
     a.row = row; a.rows_out = To;
+    for (int o = 0; o < 3; ++o)
+        if (outs[o] != nullptr && rope_reads(a, heads_grid(outs[o], o == 0 ? T : To, o == 0 ? Hq : Hkv, D))) return SKIPFFN_EINVAL;
     if (rope_forward_workgroups(a, num_cus()) >= ((int64_t)1 << 24)) return SKIPFFN_ESHAPE;             // a launch has fewer than 2^32 threads
     hipStream_t s = (hipStream_t)stream;
     profile_mark_begin(KC_ROPE_FWD, s);
@@ -1321,8 +1332,7 @@ int skipffn_qk_rope_backward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int6
     int st = check_rope(T, Hq, Hkv, D, rot, n_axes, pos, inv_freq, axis, gain_q, gain_k, eps, flags);
     if (st != SKIPFFN_OK) return st;
     const bool norm = (flags & SKIPFFN_FLAG_QK_NORM) != 0, gains = d_gain_q != nullptr || d_gain_k != nullptr;
-    if ((gains && !norm) || (reinterpret_cast<uintptr_t>(d_gain_q) & 3u) || (reinterpret_cast<uintptr_t>(d_gain_k) & 3u) ||
-        (gains && d_gain_q == d_gain_k))
+    if ((gains && !norm) || (reinterpret_cast<uintptr_t>(d_gain_q) & 3u) || (reinterpret_cast<uintptr_t>(d_gain_k) & 3u))
         return SKIPFFN_EINVAL;
     if (norm && ((st = check_heads(q, T, Hq, D, false)) || (st = check_heads(k, T, Hkv, D, false)))) return st;
     if ((st = check_heads(grad_q_out, T, Hq, D, false)) || (st = check_heads(grad_k_out, T, Hkv, D, false)) ||
@@ -1336,10 +1346,15 @@ int skipffn_qk_rope_backward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int6
             if (heads_share(outs[o], T, o == 0 ? Hq : Hkv, ins[i], T, (i & 1) == 0 ? Hq : Hkv, D)) return SKIPFFN_EINVAL;
         }
     if (T > 0 && heads_share(grad_q, T, Hq, grad_k, T, Hkv, D)) return SKIPFFN_EINVAL;
+    RopeArgs a = rope_args(T, Hq, Hkv, D, rot, n_axes, pos, inv_freq, axis, gain_q, gain_k, eps, flags);
+    const Grid grads[2] = {heads_grid(grad_q, T, Hq, D), heads_grid(grad_k, T, Hkv, D)};
+    const Grid d_gains[2] = {grid_of(d_gain_q, d_gain_q != nullptr ? D * 4 : 0, {0, 1}), grid_of(d_gain_k, d_gain_k != nullptr ? D * 4 : 0, {0, 1})};
+    for (const Grid& g : grads)
+        if (rope_reads(a, g) || grids_share(g, d_gains[0]) || grids_share(g, d_gains[1])) return SKIPFFN_EINVAL;
+    if (grids_share(d_gains[0], d_gains[1])) return SKIPFFN_EINVAL;
     if (gains && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < skipffn_qk_rope_backward_workspace_bytes(T, Hq, Hkv, D)))
         return SKIPFFN_EWORKSPACE;
     if (T == 0 && !gains) return SKIPFFN_OK;
-    RopeArgs a = rope_args(T, Hq, Hkv, D, rot, n_axes, pos, inv_freq, axis, gain_q, gain_k, eps, flags);
     if (norm) {
         a.q = rope_in(q);
         a.k = rope_in(k);

@@ -89,6 +89,39 @@ def test_rope_backward_refuses_what_it_cannot_do():
         assert B.skipffn_qk_rope_backward_workspace_bytes(*bad) == 0
 
 
+def test_rope_refuses_outputs_over_what_other_workgroups_read():
+    wide = [FAKE + (i << 42) for i in range(16)]
+    many = 1 << 29                                       # tokens: more than a launch takes, the last of the checks, so that nothing is enqueued
+    t = {i: heads(wide[i]) for i in range(6)}
+    tables = dict(pos=wide[8], freq=wide[9], row=wide[10], gq=wide[11], gk=wide[12])
+    fwd = lambda **more: rope_fwd(T=many, rows=many, v=True, **{**dict(t=t), **tables, **more})
+    assert fwd() == B.ESHAPE
+    size = dict(pos=many * 4, freq=32 * 4, row=many * 4, gq=64 * 2, gk=64 * 2)
+    for o in (3, 4, 5):
+        end = wide[o] + many * 4 * 64 * 2
+        for name, n in size.items():
+            assert fwd(**{name: wide[o]}) == B.EINVAL and fwd(**{name: end - 16}) == B.EINVAL and fwd(**{name: end}) == B.ESHAPE, (o, name)
+            assert fwd(**{name: wide[o] - n + 16}) == B.EINVAL and fwd(**{name: wide[o] - n}) == B.ESHAPE, (o, name)
+    # a column range of rows that the frequencies lie between
+    gap = {**t, 3: heads(wide[3], token=4 * 64 + 64)}
+    assert fwd(t=gap, freq=wide[3] + 4 * 64 * 2) == B.ESHAPE and fwd(t=gap, freq=wide[3] + 4 * 64 * 2 - 4) == B.EINVAL
+    # the gradients; a workspace that is missing is the last of their checks
+    del tables["row"]
+    bwd = lambda **more: rope_bwd(ws=None, **{**dict(t=t, dq=wide[13], dk=wide[14]), **tables, **more})
+    assert bwd() == B.EWORKSPACE
+    for o in (4, 5):
+        end = wide[o] + 64 * 4 * 64 * 2
+        for name in tables:
+            assert bwd(**{name: wide[o]}) == B.EINVAL and bwd(**{name: end - 16}) == B.EINVAL and bwd(**{name: end}) == B.EWORKSPACE, (o, name)
+        for name in ("dq", "dk"):
+            assert bwd(**{name: wide[o] + 64}) == B.EINVAL and bwd(**{name: end}) == B.EWORKSPACE, (o, name)
+    # two gains' gradients: none the other's
+    assert bwd(dk=wide[13] + 63 * 4) == B.EINVAL and bwd(dq=wide[14] + 4) == B.EINVAL and bwd(dk=wide[13] + 64 * 4) == B.EWORKSPACE
+    assert bwd(dq=None) == B.EWORKSPACE and bwd(dk=None) == B.EWORKSPACE
+    # nothing is rotated: neither positions nor frequencies are read
+    assert fwd(rot=0, pos=wide[3], freq=wide[3]) == B.ESHAPE and bwd(rot=0, pos=wide[4], freq=wide[5]) == B.EWORKSPACE
+
+
 # ---- what keys receive -------------------------------------------------------------------------------
 def key_weights(Tq=64, Tk=64, n=1, Hq=4, Hkv=4, D=64, q=None, k=None, sq=FAKE, sk=None, scale=0.125, saved=FAKE, last=-1, w=FARS[9], w_head=64,
                 ws=FAKE, ws_bytes=BIG, flags=0):
