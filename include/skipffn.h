@@ -455,7 +455,7 @@ int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T
  *   axis      u8 [rot / 2] HOST, every one below n_axes, or NULL: axis 0 for all
  *   q_out [T, Hq, D]; k_out, v_out OUT: [T, Hkv, D], or with row != NULL the rows of a cache [rows_out, Hkv, D]:
  *   row       i32 [T] device: token t's key and value go to row row[t] of k_out and v_out, and nowhere if that is outside
- *             [0, rows_out) (a padded batch); rows that no token has are left as they were.  Two tokens with the same row: each 16 bytes
+ *             [0, rows_out) (a padded batch); rows that no token has are left as they were.  Two tokens with the same row: each 8 bytes
  *             of it come from one of them.  NULL: row t (rows_out is not read)
  * An output may be its own input (same memory and strides, row == NULL); training with a norm needs the inputs again, so not then.
  * Otherwise it shares no element with an input (positions, frequencies, rows and gains are read by all workgroups) or another output: what
