@@ -236,3 +236,93 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(want, (q_out, k_out, dq, dk, *d))), turn
+
+
+# ---- more wavefronts than the chip holds -----------------------------------------------------------------
+# Beyond 32 a compute unit a forward wavefront works on three heads one after the other; a backward one goes on through the tokens.
+def lanes_of_a_head(D, rot, pairs):
+    wide = pairs or rot % 16 == 0                        # slots of 8 columns, otherwise of 4
+    return (4 if wide else 8) * (1 if D <= 64 else 2)
+
+
+def wavefronts(T, heads, D, rot, pairs):
+    """Of T tokens where each has one round of heads."""
+    lanes, at_once = lanes_of_a_head(D, rot, pairs), 1
+    while at_once * 2 * lanes <= 64 and at_once < heads:
+        at_once *= 2
+    return -(-T // (64 // lanes // at_once)) * -(-heads // at_once)
+
+
+def chip():
+    return torch.cuda.get_device_properties(0).multi_processor_count
+
+
+MANY = [(1800, 32, 8, 128, 128), (1800, 28, 4, 128, 128), (4300, 10, 2, 72, 72), (8400, 9, 3, 40, 40), (4200, 20, 5, 64, 32), (70001, 1, 1, 8, 8),
+        (3000, 6, 6, 96, 0)]
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,D,rot", MANY)
+@pytest.mark.parametrize("norm", [False, True], ids=["bare", "norm"])
+@pytest.mark.parametrize("pairs", [False, True], ids=["halves", "neighbours"])
+def test_many_tokens_into_the_rows_of_a_cache(T, Hq, Hkv, D, rot, norm, pairs):
+    print(f"many tokens T={T} heads {Hq}/{Hkv} D={D} rot={rot} norm={norm} pairs={pairs}", flush=True)
+    assert wavefronts(T, Hq + 2 * Hkv, D, rot, pairs) > 32 * chip()
+    p = Rope(T, Hq, Hkv, D, rot, 3 if rot else 1, 1000, norm, True, pairs)
+    rows = T + 77
+    kc, vc = (torch.full((Hkv, rows, D), 7.0, dtype=torch.bfloat16, device="cuda").transpose(0, 1) for _ in range(2))
+    row = p.rng.permutation(rows)[:T].astype(np.int32)
+    row[::5] = [(-1, rows, -2 ** 31, 2 ** 31 - 1)[i % 4] for i in range(len(row[::5]))]
+    q_out = torch.full((T, Hq + 1, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    p.forward(q_out[:, :Hq], kc, v=p.v, v_out=vc, row=torch.from_numpy(row).cuda())
+    torch.cuda.synchronize()
+    p.check(q_out[:, :Hq], p.q, p.gq, "q")
+    assert bool((q_out[:, Hq] == 7.0).all())
+    ok = (row >= 0) & (row < rows)
+    y, n = p.want(p.k, p.gk)
+    assert_within(f64_of(kc)[row[ok]], y[ok], forward_bound(y, n, rot, pairs)[ok], "k")
+    at = torch.from_numpy(row[ok]).long().cuda()
+    assert torch.equal(vc[at].view(torch.int16), p.v[torch.from_numpy(ok).cuda()].view(torch.int16))
+    rest = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    assert bool((kc[rest] == 7.0).all() and (vc[rest] == 7.0).all())
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,D,rot,pairs", [(2100, 28, 4, 128, 128, False), (3100, 9, 2, 72, 72, False), (9000, 7, 2, 64, 64, True)])
+def test_many_tokens_in_place(T, Hq, Hkv, D, rot, pairs):
+    print(f"many tokens in place T={T} heads {Hq}/{Hkv} D={D}", flush=True)
+    assert wavefronts(T, Hq + Hkv, D, rot, pairs) > 32 * chip()
+    p = Rope(T, Hq, Hkv, D, rot, pairs=pairs)
+    q_out, k_out = (torch.empty(T, h, D, dtype=torch.bfloat16, device="cuda") for h in (Hq, Hkv))
+    p.forward(q_out, k_out)
+    p.check(q_out, p.q, p.gq, "q")
+    p.check(k_out, p.k, p.gk, "k")
+    v = p.v.clone()
+    p.forward(p.q, p.k)
+    assert torch.equal(p.q, q_out) and torch.equal(p.k, k_out) and torch.equal(p.v, v)
+
+
+@pytest.mark.parametrize("T,Hq,Hkv,D,rot,pairs", [(30000, 16, 4, 16, 16, False), (30001, 16, 4, 16, 8, True), (6000, 8, 2, 72, 72, False), (4001, 12, 3, 128, 64, False)])
+@pytest.mark.parametrize("norm", [False, True], ids=["bare", "norm"])
+def test_gradients_of_many_tokens(T, Hq, Hkv, D, rot, pairs, norm):
+    """Rounds of a wavefront: 4 to 13 (units over the wavefronts of three workgroups a compute unit), which its gains' sums go through."""
+    print(f"gradients of many tokens T={T} heads {Hq}/{Hkv} D={D} norm={norm}", flush=True)
+    for H in (Hq, Hkv):
+        assert wavefronts(T, H, D, rot, pairs) > 3 * 12 * chip() * H / (Hq + Hkv)
+    p = Rope(T, Hq, Hkv, D, rot, 1, 0, norm, True, pairs)
+    grads = rand(p.rng, T, Hq, D), rand(p.rng, T, Hkv, D)
+    ws = room(B.skipffn_qk_rope_backward_workspace_bytes(T, Hq, Hkv, D))
+    want = [O.rope_backward_real(f64_of(x), p.angle, pairs, norm, None if gain is None else f64_of(gain), EPS, f64_of(g))
+            for x, gain, g in ((p.q, p.gq, grads[0]), (p.k, p.gk, grads[1]))]
+    bound = [backward_bounds(f64_of(x), norm, None if gain is None else f64_of(gain), EPS, f64_of(g), rot, pairs, w[0])
+             for x, gain, g, w in ((p.q, p.gq, grads[0], want[0]), (p.k, p.gk, grads[1], want[1]))]
+    for gains in (True, False) if norm else (False,):
+        dqkv = torch.full((T, Hq + 2 * Hkv, D), 7.0, dtype=torch.bfloat16, device="cuda")
+        d_gain = [torch.full((D,), 7.0, device="cuda") for _ in range(2)] if gains else [None, None]
+        B.skipffn_qk_rope_backward(*grads, dqkv[:, :Hq], dqkv[:, Hq:Hq + Hkv], p.pos, p.freq, q=p.q, k=p.k, d_gain_q=d_gain[0], d_gain_k=d_gain[1],
+                                   workspace=ws, **p.common)
+        torch.cuda.synchronize()
+        for name, dx, dg, w, e in (("q", dqkv[:, :Hq], d_gain[0], want[0], bound[0]), ("k", dqkv[:, Hq:Hq + Hkv], d_gain[1], want[1], bound[1])):
+            assert_within(f64_of(dx), w[0], e[0], f"grad_{name}")
+            if gains:
+                assert_within(f64_of(dg), w[1], e[1], f"d_gain_{name}")
+        assert bool((dqkv[:, Hq + Hkv:] == 7.0).all())
