@@ -103,6 +103,7 @@ def test_rows_that_received_most_stay(rows, Hkv, D, packed, kind):
         e.check(n_keep, first, recent)
 
 
+# (An earlier form of the kernel held these in registers; today's reads every list of more than 4096 rows again for each step.)
 @pytest.mark.parametrize("rows", [(20000,), (33000, 17), (65536,), (70000, 5)], ids=str)
 @pytest.mark.parametrize("kind", ["sums", "few values", "any"])
 def test_long_caches(rows, kind):
@@ -206,3 +207,47 @@ def test_captured_and_replayed():
         torch.cuda.synchronize()
         graph.replay()
         e.check(450, 4, 100)
+
+
+# ---- lengths at which the form of the search changes -------------------------------------------------------
+# A thread holds four weights.  512 threads a list where no list can have more than 2048 rows (T), otherwise 1024, which read lists of more than 4096 rows again for
+# every step; keys that share the digits of the cut are collected where there are 4096 of them at most.
+@pytest.mark.parametrize("T", [2048, 2049])
+@pytest.mark.parametrize("packed", [True, False], ids=["packed", "own"])
+def test_room_for_as_many_rows_as_the_short_form_takes(T, packed):
+    rows = (T - 3,) if packed else (T - 2, T - 3, 5)
+    for kind in ("sums", "few values", "any"):
+        e = Evict(rows, 3, 16, packed, 1000, kind)
+        assert e.T == T
+        e.run(1000, 4, 300)
+        e.check(1000, 4, 300)
+
+
+@pytest.mark.parametrize("n", [4095, 4096, 4097, 8191, 8193])
+@pytest.mark.parametrize("kind", ["sums", "few values", "any"])
+def test_lists_as_long_as_the_long_form_holds(n, kind):
+    for n_keep, first, recent in ((n - 1, 0, 0), (n // 2, 5, 100), (n // 2, 0, n // 2 - 1), (1, 0, 0)):
+        e = Evict((n, 10), 2, 8, True, n_keep + 10, kind)
+        e.run(n_keep, first, recent)
+        e.check(n_keep, first, recent)
+
+
+@pytest.mark.parametrize("same", [4095, 4096, 4097])
+@pytest.mark.parametrize("bits", [11, 22], ids=["first digit", "two digits"])
+def test_as_many_keys_at_the_cut_as_are_collected(same, bits):
+    """`same` keys that share their first 11 or 22 bits with the cut, larger and smaller ones around them; with 22 the others share the first 11 as well."""
+    n, more, less = 12000, 3000, 12000 - 3000 - same
+    rng = np.random.default_rng(same)
+    if bits == 11:                                       # the sign, the exponent and two bits of the mantissa: [1, 1.25)
+        at, high, low = 1 + rng.permutation(2 ** 21)[:same] * 2.0 ** -23, 1.25 + rng.random(more), rng.random(less) * 0.99
+    else:                                                # [1, 1 + 2^-13), 1024 numbers
+        at = 1 + rng.integers(0, 1024, same) * 2.0 ** -23
+        high, low = 1 + 2.0 ** -13 + rng.integers(0, 2 ** 20, more) * 2.0 ** -23, rng.random(less) * 0.99
+    values = np.concatenate([at, high, low]).astype(np.float32)
+    for n_keep in (more + 1, more + same // 2, more + same - 1, more + same, more):
+        e = Evict((n,), 2, 8, True, n_keep)
+        for h in range(2):
+            e.w_host[h, :n] = rng.permutation(values)
+        e.w.copy_(torch.from_numpy(e.w_host))
+        e.run(n_keep)
+        e.check(n_keep)
