@@ -865,6 +865,7 @@ struct Grid {
     int64_t run;
     Dim d[3];                                            // the largest stride first
     int dims;
+    int64_t whole;                                       // span(0), no element: run is 0
     int64_t span(int from) const {
         int64_t e = run;
         for (int i = from; i < dims; ++i) e += (d[i].n - 1) * d[i].stride;
@@ -872,12 +873,15 @@ struct Grid {
     }
 };
 Grid grid_of(const void* p, int64_t run, Dim a, Dim b = {0, 1}, Dim c = {0, 1}) {
-    Grid g{p, run, {}, 0};
+    Grid g{p, run, {}, 0, run};
     for (const Dim& x : {a, b, c}) {
-        if (x.n <= 0) g.run = 0;
-        if (x.n > 1) g.d[g.dims++] = x;
+        if (x.n <= 0) return Grid{};
+        if (x.n == 1) continue;
+        g.whole += (x.n - 1) * x.stride;
+        int i = g.dims++;
+        for (; i > 0 && g.d[i - 1].stride < x.stride; --i) g.d[i] = g.d[i - 1];
+        g.d[i] = x;
     }
-    std::sort(g.d, g.d + g.dims, [](const Dim& x, const Dim& y) { return x.stride > y.stride; });
     return g;
 }
 // Whether a from its i-th stride on and b from its j-th on, which begins `ahead` bytes after a, share an element.  The larger stride is taken off both: they are in
@@ -892,11 +896,19 @@ bool grids_share_from(int64_t ahead, const Grid& a, int i, const Grid& b, int j)
     return grids_share_from(r, a, in, b, jn) || grids_share_from(r - step, a, in, b, jn);
 }
 bool grids_share(const Grid& a, const Grid& b) {
-    if (a.run <= 0 || b.run <= 0) return false;
-    return grids_share_from((int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p)), a, 0, b, 0);
+    const int64_t ahead = (int64_t)(reinterpret_cast<uintptr_t>(b.p) - reinterpret_cast<uintptr_t>(a.p));
+    return a.run > 0 && b.run > 0 && ahead < a.whole && -ahead < b.whole && grids_share_from(ahead, a, 0, b, 0);
 }
 Grid heads_grid(const skipffn_heads* t, int64_t T, int64_t H, int64_t D, int64_t seq_stride = 0, int64_t n_seq = 1) {
     return grid_of(t->data, D * 2, {t->token_stride * 2, T}, {t->head_stride * 2, H}, {seq_stride * 2, n_seq});
+}
+// the same for bytes in one piece, and for heads; what they span is compared first, without a grid
+bool shares_bytes(const Grid& g, const void* p, int64_t bytes) {
+    return g.run > 0 && ranges_meet(g.p, g.whole, p, bytes) && grids_share(g, Grid{p, bytes, {}, 0, bytes});
+}
+bool shares_heads(const Grid& g, const skipffn_heads* t, int64_t T, int64_t H, int64_t D, int64_t seq_stride = 0, int64_t n_seq = 1) {
+    return g.run > 0 && T > 0 && n_seq > 0 && ranges_meet(g.p, g.whole, t->data, heads_span(t, T, H, D) + (n_seq - 1) * seq_stride * 2) &&
+           grids_share(g, heads_grid(t, T, H, D, seq_stride, n_seq));
 }
 bool bad4(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 bool bad_seg(const int32_t* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
@@ -1087,15 +1099,13 @@ int decode_call(int64_t n_seq, int64_t n_groups, int64_t Hq, int64_t Hkv, int64_
         // a workgroup stores weights while others still read
         const Grid received[2] = {grid_of(weights->prefix, Tg * 4, {weights->prefix_head * 4, Hkv}),
                                   grid_of(weights->own, cap * 4, {weights->own_head * 4, Hkv}, {weights->own_seq * 4, n_seq})};
-        const Grid read[9] = {heads_grid(q, n_seq, Hq, D), heads_grid(out, n_seq, Hq, D),
-                              Tg > 0 ? heads_grid(prefix_k, Tg, Hkv, D) : Grid{}, Tg > 0 ? heads_grid(prefix_v, Tg, Hkv, D) : Grid{},
-                              cap > 0 ? heads_grid(suffix_k, cap, Hkv, D, suffix_k_seq, n_seq) : Grid{},
-                              cap > 0 ? heads_grid(suffix_v, cap, Hkv, D, suffix_v_seq, n_seq) : Grid{},
-                              grid_of(suffix_len, cap > 0 ? n_seq * 4 : 0, {0, 1}), grid_of(group_off, n_groups > 0 ? (n_groups + 1) * 4 : 0, {0, 1}),
-                              grid_of(prefix_seg, Tg > 0 ? (n_groups + 1) * 4 : 0, {0, 1})};
         for (const Grid& w : received)
-            for (const Grid& r : read)
-                if (grids_share(w, r)) return SKIPFFN_EINVAL;
+            if (shares_heads(w, q, n_seq, Hq, D) || shares_heads(w, out, n_seq, Hq, D) ||
+                (Tg > 0 && (shares_heads(w, prefix_k, Tg, Hkv, D) || shares_heads(w, prefix_v, Tg, Hkv, D))) ||
+                (cap > 0 && (shares_heads(w, suffix_k, cap, Hkv, D, suffix_k_seq, n_seq) || shares_heads(w, suffix_v, cap, Hkv, D, suffix_v_seq, n_seq) ||
+                             shares_bytes(w, suffix_len, n_seq * 4))) ||
+                (n_groups > 0 && (shares_bytes(w, group_off, (n_groups + 1) * 4) || shares_bytes(w, prefix_seg, (n_groups + 1) * 4))))
+                return SKIPFFN_EINVAL;
     }
     const DecodeWs ws_of = decode_ws(n_seq, n_groups, Hq, Hkv, D, Tp, cap, weights != nullptr, weights != nullptr ? weights->most_shared : 0);
     const PartsWs& W = ws_of.parts;
@@ -1203,7 +1213,7 @@ int skipffn_attn_key_weights(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, 
     // a workgroup stores weights while others still find their sequence
     const Grid received = grid_of(weights, Tk * 4, {weights_head * 4, Hkv});
     for (const int32_t* offsets : {seg_q, seg_k})
-        if (offsets != nullptr && grids_share(received, grid_of(offsets, (n_seq + 1) * 4, {0, 1}))) return SKIPFFN_EINVAL;
+        if (offsets != nullptr && shares_bytes(received, offsets, (n_seq + 1) * 4)) return SKIPFFN_EINVAL;
     const size_t need = key_weights_bytes(plan, Tk, Hkv);
     if (need > 0 && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < need)) return SKIPFFN_EWORKSPACE;
     hipStream_t s = (hipStream_t)stream;
@@ -1266,11 +1276,9 @@ RopeArgs rope_args(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int64_t rot, i
 // whether elements of a result are what every workgroup reads beside the heads
 bool rope_reads(const RopeArgs& a, const Grid& result) {
     const int64_t gain = a.D * 2;
-    return grids_share(result, grid_of(a.pos, (int64_t)a.n_axes * a.T * 4, {0, 1})) ||
-           grids_share(result, grid_of(a.inv_freq, a.T > 0 ? a.rot * 2 : 0, {0, 1})) ||
-           grids_share(result, grid_of(a.gain_q, a.gain_q != nullptr ? gain : 0, {0, 1})) ||
-           grids_share(result, grid_of(a.gain_k, a.gain_k != nullptr ? gain : 0, {0, 1})) ||
-           grids_share(result, grid_of(a.row, a.row != nullptr ? (int64_t)a.T * 4 : 0, {0, 1}));
+    return shares_bytes(result, a.pos, (int64_t)a.n_axes * a.T * 4) || shares_bytes(result, a.inv_freq, a.T > 0 ? a.rot * 2 : 0) ||
+           (a.gain_q != nullptr && shares_bytes(result, a.gain_q, gain)) || (a.gain_k != nullptr && shares_bytes(result, a.gain_k, gain)) ||
+           (a.row != nullptr && shares_bytes(result, a.row, (int64_t)a.T * 4));
 }
 }  // namespace
 
@@ -1348,10 +1356,10 @@ int skipffn_qk_rope_backward(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int6
     if (T > 0 && heads_share(grad_q, T, Hq, grad_k, T, Hkv, D)) return SKIPFFN_EINVAL;
     RopeArgs a = rope_args(T, Hq, Hkv, D, rot, n_axes, pos, inv_freq, axis, gain_q, gain_k, eps, flags);
     const Grid grads[2] = {heads_grid(grad_q, T, Hq, D), heads_grid(grad_k, T, Hkv, D)};
-    const Grid d_gains[2] = {grid_of(d_gain_q, d_gain_q != nullptr ? D * 4 : 0, {0, 1}), grid_of(d_gain_k, d_gain_k != nullptr ? D * 4 : 0, {0, 1})};
+    const int64_t dq_bytes = d_gain_q != nullptr ? D * 4 : 0, dk_bytes = d_gain_k != nullptr ? D * 4 : 0;
     for (const Grid& g : grads)
-        if (rope_reads(a, g) || grids_share(g, d_gains[0]) || grids_share(g, d_gains[1])) return SKIPFFN_EINVAL;
-    if (grids_share(d_gains[0], d_gains[1])) return SKIPFFN_EINVAL;
+        if (rope_reads(a, g) || shares_bytes(g, d_gain_q, dq_bytes) || shares_bytes(g, d_gain_k, dk_bytes)) return SKIPFFN_EINVAL;
+    if (ranges_meet(d_gain_q, dq_bytes, d_gain_k, dk_bytes)) return SKIPFFN_EINVAL;
     if (gains && (workspace == nullptr || !aligned16(workspace) || workspace_bytes < skipffn_qk_rope_backward_workspace_bytes(T, Hq, Hkv, D)))
         return SKIPFFN_EWORKSPACE;
     if (T == 0 && !gains) return SKIPFFN_OK;
@@ -1437,17 +1445,17 @@ int skipffn_kv_evict(int64_t n_seq, int64_t Hkv, int64_t D, int64_t T, int64_t T
                 if (ranges_meet(o.p, o.bytes, i.p, i.bytes)) return SKIPFFN_EINVAL;
         // and the second kernel copies rows by the numbers and counts: it writes none of them
         const Dim by_head{keep_head * 4, Hkv}, by_seq{keep_seq * 4, seqs}, w_by_head{weights_out_head * 4, Hkv}, w_by_seq{weights_out_seq * 4, seqs};
-        const Grid kept[3] = {grid_of(seg_out, counts, {0, 1}), grid_of(keep, T_out * 4, by_head, by_seq),
-                              grid_of(weights_out, weights_out == nullptr ? 0 : T_out * 4, w_by_head, w_by_seq)};
-        const Grid rows[4] = {heads_grid(k, T, Hkv, D, k_seq, seqs), heads_grid(v, T, Hkv, D, v_seq, seqs), heads_grid(k_out, T_out, Hkv, D, k_out_seq, seqs),
-                              heads_grid(v_out, T_out, Hkv, D, v_out_seq, seqs)};
+        const Grid kept[2] = {grid_of(keep, T_out * 4, by_head, by_seq), grid_of(weights_out, weights_out == nullptr ? 0 : T_out * 4, w_by_head, w_by_seq)};
         for (const Grid& o : kept)
-            for (const Grid& r : rows)
-                if (grids_share(o, r)) return SKIPFFN_EINVAL;
-        const Grid offsets = grid_of(seg, counts, {0, 1});
-        if (grids_share(kept[0], kept[1]) || grids_share(kept[0], kept[2]) || grids_share(kept[1], kept[2]) || grids_share(offsets, rows[2]) ||
-            grids_share(offsets, rows[3]))
+            if (shares_heads(o, k, T, Hkv, D, k_seq, seqs) || shares_heads(o, v, T, Hkv, D, v_seq, seqs) ||
+                shares_heads(o, k_out, T_out, Hkv, D, k_out_seq, seqs) || shares_heads(o, v_out, T_out, Hkv, D, v_out_seq, seqs) ||
+                shares_bytes(o, seg_out, counts))
+                return SKIPFFN_EINVAL;
+        const Grid sums = grid_of(seg_out, counts, {0, 1}), offsets = grid_of(seg, counts, {0, 1});
+        if (grids_share(kept[0], kept[1]) || shares_heads(sums, k, T, Hkv, D, k_seq, seqs) || shares_heads(sums, v, T, Hkv, D, v_seq, seqs))
             return SKIPFFN_EINVAL;
+        for (const Grid& o : {sums, offsets})
+            if (shares_heads(o, k_out, T_out, Hkv, D, k_out_seq, seqs) || shares_heads(o, v_out, T_out, Hkv, D, v_out_seq, seqs)) return SKIPFFN_EINVAL;
     }
     const int64_t cap = (int64_t)1 << 30;
     EvictArgs a{};
