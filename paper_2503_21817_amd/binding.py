@@ -413,25 +413,25 @@ def skipffn_attn_decode_workspace_bytes(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_
 
 
 def _decode(where, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, scale, workspace):
-    """The library's arguments up to the scale, the workspace's two and the stream; the sizes (Hkv, Tp, capacity), the device, and what has to live
-    until the call."""
+    """The library's arguments of skipffn_attn_decode, and what has to live until the call.  Flat: what it returns is a call's latency (single tokens are bound by
+    the host)."""
     dev = _device(q, where)
-    n_seq, Hq, D = q.shape
-    if prefix_k is None and suffix_k is None:
-        raise ValueError(f"{where}: a prefix or own rows are wanted")
+    qs = n_seq, Hq, D = q.shape
     bare, alone = prefix_k is None, suffix_k is None
+    if bare and alone:
+        raise ValueError(f"{where}: a prefix or own rows are wanted")
     if bare != (prefix_v is None) or bare != (prefix_seg is None) or bare != (group_off is None) or \
             alone != (suffix_v is None) or alone != (suffix_len is None):
         raise ValueError(f"{where}: a prefix, or own rows, come with all that belongs to them")
-    Hkv = (suffix_k if prefix_k is None else prefix_k).shape[-2]
+    Hkv = (suffix_k if bare else prefix_k).shape[-2]
     Tp = n_groups = cap = seq_k = seq_v = 0
-    seg = off = lens = None
-    given = [(q, q.shape), (out, q.shape)]
-    if prefix_k is not None:
+    seg = off = lens = pk = pv = sk = sv = None
+    given = [(q, qs), (out, qs)]
+    if not bare:
         Tp, n_groups = prefix_k.shape[0], group_off.numel() - 1
         seg, off = _ints(prefix_seg, n_groups + 1, where, dev), _ints(group_off, n_groups + 1, where, dev)
         given += [(prefix_k, (Tp, Hkv, D)), (prefix_v, (Tp, Hkv, D))]
-    if suffix_k is not None and n_seq > 0:
+    if not alone and n_seq > 0:
         cap = suffix_k.shape[1]
         lens = _ints(suffix_len, n_seq, where, dev)
         if n_seq > 1:
@@ -439,12 +439,13 @@ def _decode(where, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffi
         own = (n_seq, cap, Hkv, D)
         given += [(suffix_k, own), (suffix_v, own)]
     hold, at = _heads(where, dev, *given)
-    pk, pv = at[2:4] if prefix_k is not None else (None, None)
-    sk, sv = at[-2:] if suffix_k is not None and n_seq > 0 else (None, None)
+    if not bare:
+        pk, pv = at[2], at[3]
+    if lens is not None:
+        sk, sv = at[-2], at[-1]
     ws, ws_bytes = _buffer(workspace, 0, where, dev)
-    args = (n_seq, n_groups, Hq, Hkv, D, Tp, cap, at[0], pk, pv, seg, off, sk, sv, seq_k, seq_v, lens, at[1],
-            D ** -0.5 if scale is None else scale)
-    return args, (ws, ws_bytes), _stream(dev), (Hkv, Tp, cap), dev, hold
+    return (n_seq, n_groups, Hq, Hkv, D, Tp, cap, at[0], pk, pv, seg, off, sk, sv, seq_k, seq_v, lens, at[1],
+            D ** -0.5 if scale is None else scale, ws, ws_bytes, _stream(dev)), hold
 
 
 def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, *, scale=None,
@@ -453,9 +454,8 @@ def skipffn_attn_decode(q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, 
     four None; suffix_k, suffix_v bf16 [n_seq, capacity, Hkv, D] with suffix_len i32 [n_seq], or all three None.
     scale: None is 1 / sqrt(D)."""
     where = "skipffn_attn_decode"
-    args, ws, stream, _, _, hold = _decode(where, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, scale,
-                                           workspace)
-    _check(lib().skipffn_attn_decode(*args, *ws, stream), where)
+    args, hold = _decode(where, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, scale, workspace)
+    _check(lib().skipffn_attn_decode(*args), where)
 
 
 def skipffn_attn_decode_weights_workspace_bytes(n_seq, n_groups, Hq, Hkv, D, Tp, suffix_capacity, most_shared) -> int:
@@ -467,16 +467,16 @@ def skipffn_attn_decode_weights(q, prefix_k, prefix_v, prefix_seg, group_off, su
     """skipffn_attn_decode, and what the rows receive: prefix_weights f32 [Hkv, Tp] and suffix_weights f32 [n_seq, Hkv, capacity] (None with
     the rows they belong to).  most_shared: most sequences of a group.  flags: FLAG_DW_ACCUMULATE."""
     where = "skipffn_attn_decode_weights"
-    args, ws, stream, (Hkv, Tp, cap), dev, hold = _decode(where, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len,
-                                                          out, scale, workspace)
+    args, hold = _decode(where, q, prefix_k, prefix_v, prefix_seg, group_off, suffix_k, suffix_v, suffix_len, out, scale, workspace)
+    (n_seq, _, _, Hkv, _, Tp, cap), dev = args[:7], q.get_device()
     if (prefix_k is None) != (prefix_weights is None) or (suffix_k is None) != (suffix_weights is None):
         raise ValueError(f"{where}: a prefix, or own rows, come with their weights")
     pw, sw = (None, 0), (None, 0, 0)
     if prefix_weights is not None:
         pw = _weights(prefix_weights, (Hkv, Tp), where, dev)
-    if suffix_weights is not None and q.shape[0] > 0:
-        sw = _weights(suffix_weights, (q.shape[0], Hkv, cap), where, dev)
-    _check(lib().skipffn_attn_decode_weights(*args, most_shared, *pw, *sw, *ws, flags, stream), where)
+    if suffix_weights is not None and n_seq > 0:
+        sw = _weights(suffix_weights, (n_seq, Hkv, cap), where, dev)
+    _check(lib().skipffn_attn_decode_weights(*args[:19], most_shared, *pw, *sw, *args[19:21], flags, args[21]), where)
 
 
 def _weights(t, shape, where, device, dtype=torch.float32):
