@@ -7,7 +7,7 @@
 // rounded below fp32 and every sum has one owner and a fixed order.  Where keys are few for the chip, or a causal prompt's pieces uneven, the
 // queries are cut into parts whose sums a second kernel adds.
 //
-// 32 / 8 heads of 128, us: 1 x 16384 tokens 1065-1080 (1018-1032 TFLOP/s of what the mask leaves, a library product of 8192^3 1178): matrix cores busy 48 % of the
+// 32 / 8 heads of 128, us: 1 x 16384 tokens 1064-1127 by the card (975-1032 TFLOP/s of what the mask leaves, a library product of 8192^3 1178): matrix cores busy 48 % of the
 // time, the vector unit 60 % (three instructions a score), at 2.0-2.1 GHz.  16 x up to 616 tokens 33, of which 4.3 the second kernel: latency, 1.2 a step of 64
 // queries.  32768 keys by 64 queries 29-32 (67 MB of keys): loads and steps of a workgroup one after the other.
 #include <algorithm>
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(KW_KEYS) void key_weights_join_kernel(const AttnArg
 }
 
 // Parts that the queries are cut into.  A piece takes 1.2 us a step and 6 us to begin and end; the last ones leave the chip to themselves, so pieces are made
-// shorter until what that saves goes into beginning more of them; the second kernel takes about 4 us..  Us of whole
+// shorter until what that saves goes into beginning more of them; the second kernel takes about 4 us.  Us of whole
 // calls (parts), as planned first: 16 sequences of up to 616, 5682 tokens together, 34.6 (3), 60.8 (1), 40.1 (6); 8 x 616 37.0 (4), 67.3 (1), 45.3 (2), 45.0 (9); 1 x 616 16.6 (10, all there
 // are), 65.4 (1), 19.4 (7); 1 x 2944 56.7 (14), 257 (1), 59.5 (7), 69.7 (28); 4 x 4096 324 (7), 397 (1), 316 (3), 363 (14); 1 x 16384 1074 (14), 1501 (1), 1059 (7), 1134 (28)
 KeyWeightsPlan key_weights_plan(int64_t Tq, int64_t Tk, int64_t n_seq, int64_t Hq, int64_t Hkv, int64_t last, int ncu) {

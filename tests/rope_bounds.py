@@ -1,8 +1,8 @@
 """How far the norm and rotation of queries and keys may be from the exact ones, element by element.
 
-A result is rounded to bf16 once: u = 2^-8 of it.  Before that all is fp32.  An angle in half turns is rounded to 2^-25 (pi 2^-25 radians), sine and cosine
-are off by two units of 2^-24; a sum of up to 128 squares over 8 or 16 lanes adds at most 20 roundings, halved by the root, the root itself two;
-two products with the gain, two and a sum in the rotation: fewer than 2^5 units of 2^-24 of |n_a| + |n_b| in all, F = 2^-18.
+A result is rounded to bf16 once: u = 2^-8 of it.  Before that all is fp32.  An angle of at most half a turn is rounded to 2^-25 turns (2^-22.3 radians), sine
+and cosine of it are off by 2^-22.9 more: under 6 units of 2^-24; a sum of up to 128 squares over 8 or 16 lanes adds at most 20 roundings, halved by
+the root, the root itself two; two products with the gain, two and a sum in the rotation: fewer than 2^5 units of 2^-24 of |n_a| + |n_b| in all, F = 2^-18.
 Backward the same for the gradient rotated back, once more for the norm's term: 2 F of r (G gain + |x| r^2 mean(G gain |x|)), G the sum of a pair's
 |g|.  Gain gradients: F of every term, and a sum of fp32 terms, fewer than 2^8 of them one after the other: 2^-16 of the sum of |terms|."""
 import numpy as np
